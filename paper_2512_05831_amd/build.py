@@ -4,8 +4,10 @@
 ``csrc/eb.hip`` (with ``csrc/eb_gather.h``), ``csrc/eb_gather_weighted.hip``,
 ``csrc/eb_gather_narrow.hip``, ``csrc/eb_gather_narrow_weighted.hip``,
 ``csrc/eb_gather_wave.hip``, ``csrc/eb_gather_wave_weighted.hip``,
-``csrc/eb_exchange.hip`` and ``csrc/eb_ceiling.hip`` (the bandwidth probe the
-benchmark uses) and writes ``libeb.so`` next to this file.
+``csrc/eb_exchange.hip``, ``csrc/eb_ceiling.hip`` (the bandwidth probe the
+benchmark uses) and the experts' operators (``csrc/eb_route_experts.hip``,
+``csrc/eb_quantize_fp8.hip``, ``csrc/eb_expert_product*.hip``) and writes
+``libeb.so`` next to this file.
 """
 from __future__ import annotations
 
@@ -18,7 +20,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 SRCS = [os.path.join(HERE, "csrc", f)
         for f in ("eb.hip", "eb_gather_weighted.hip", "eb_gather_narrow.hip",
                   "eb_gather_narrow_weighted.hip", "eb_gather_wave.hip",
-                  "eb_gather_wave_weighted.hip", "eb_exchange.hip", "eb_ceiling.hip")]
+                  "eb_gather_wave_weighted.hip", "eb_exchange.hip", "eb_ceiling.hip",
+                  "eb_route_experts.hip", "eb_quantize_fp8.hip", "eb_expert_product.hip",
+                  "eb_expert_product_stream.hip")]
 LIB = os.path.join(HERE, "libeb.so")
 ARCH = "gfx950"
 

@@ -1,0 +1,108 @@
+// eb_expert_product (include/eb_experts.h): checks of arguments and the choice
+// of its kernel.
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <limits>
+
+#include "eb_expert_product.h"
+#include "eb_internal.h"
+
+namespace {
+
+using namespace eb_product;
+using eb_detail::fail;
+
+constexpr int64_t kMostSize = (int64_t)1 << 30;
+
+int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1 : 2; }
+
+int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
+                 const float *x_scales, int64_t ldxs, const int32_t *tokens, const void *w, int64_t ldw,
+                 const float *w_scales, const int32_t *offsets, const float *bias, int32_t act, int32_t out_type, void *out,
+                 int64_t ldo, float *out_scales, int64_t ldos, void *stream)
+{
+    constexpr int64_t kMax = std::numeric_limits<int64_t>::max();
+    if (M < 0 || E < 1 || N < 1 || K < 1 || x_rows < 0) return fail(EB_ERR_INVALID, "%s: M or x_rows below 0, or E, N or K below 1", who);
+    if (act != EB_ACT_NONE && act != EB_ACT_RELU && act != EB_ACT_SILU_GATE) return fail(EB_ERR_INVALID, "%s: unknown act", who);
+    if (out_type != EB_F32 && out_type != EB_F16 && out_type != EB_BF16 && out_type != EB_FP8)
+        return fail(EB_ERR_INVALID, "%s: unknown out_type", who);
+    const bool gate = act == EB_ACT_SILU_GATE, fp8 = out_type == EB_FP8;
+    if (gate && N % 2 != 0) return fail(EB_ERR_INVALID, "%s: a gate needs an even N", who);
+    if (!offsets && E != 1) return fail(EB_ERR_INVALID, "%s: several experts need offsets", who);
+    if (M > std::numeric_limits<int32_t>::max() || N > kMostSize || K > kMostSize)
+        return fail(EB_ERR_UNSUPPORTED, "%s: M of 2^31 and more, or N or K above 2^30", who);
+    if (M == 0) return EB_OK;
+    if (!x || !x_scales || !w || !w_scales || !out || (fp8 && !out_scales))
+        return fail(EB_ERR_INVALID, "%s: NULL x, w, out or their scales", who);
+    if (!tokens && x_rows < M) return fail(EB_ERR_INVALID, "%s: x has fewer rows than M", who);
+    if (ldx < K || ldw < K || ldx % 16 != 0 || ldw % 16 != 0 || (uintptr_t)x % 16 != 0 || (uintptr_t)w % 16 != 0)
+        return fail(EB_ERR_INVALID, "%s: x, w, ldx and ldw must be multiples of 16 bytes, ldx and ldw at least K", who);
+    const int64_t width = gate ? N / 2 : N;
+    if (ldo < width || ldxs < x_rows || (fp8 && ldos < M)) return fail(EB_ERR_INVALID, "%s: ldo, ldxs or ldos too small", who);
+    if (fp8 && (ldo % 16 != 0 || (uintptr_t)out % 16 != 0)) return fail(EB_ERR_INVALID, "%s: 8-bit out and ldo must be multiples of 16", who);
+    if ((uintptr_t)out % element_bytes(out_type) != 0) return fail(EB_ERR_INVALID, "%s: out is not aligned to its elements", who);
+    const int64_t k_blocks = (K + kBlock - 1) / kBlock, row_blocks = (width + kBlock - 1) / kBlock;
+    if (ldo > kMax / 4 / M || ldos > kMax / 4 / row_blocks || ldxs > kMax / 4 / k_blocks || (x_rows > 0 && ldx > kMax / x_rows) ||
+        ldw > kMax / N / E || row_blocks > kMax / 16 / E / k_blocks)
+        return fail(EB_ERR_UNSUPPORTED, "%s: a buffer exceeds 2^63 bytes", who);
+
+    ProductArgs a{};
+    a.x = (const char *)x;
+    a.w = (const char *)w;
+    a.x_scales = x_scales;
+    a.w_scales = w_scales;
+    a.bias = bias;
+    a.tokens = tokens;
+    a.offsets = offsets;
+    a.out = out;
+    a.out_scales = out_scales;
+    a.ldx = ldx;
+    a.ldxs = ldxs;
+    a.ldw = ldw;
+    a.ldo = ldo;
+    a.ldos = ldos;
+    a.x_rows = x_rows;
+    a.M = (int32_t)M;
+    a.E = E;
+    a.N = (int32_t)N;
+    a.K = (int32_t)K;
+    a.width = (int32_t)width;
+    a.k_blocks = (int32_t)k_blocks;
+    a.row_blocks = (int32_t)row_blocks;
+    a.w_blocks = (int32_t)row_blocks * (gate ? 2 : 1);
+    a.relu = act == EB_ACT_RELU;
+    a.out_type = out_type;
+    const int es = element_bytes(out_type);
+    a.vector_out = ldo % 4 == 0 && (uintptr_t)out % (4 * es) == 0;
+
+    const int64_t mean = (M + E - 1) / E;
+    const KernelPlan plan = stream_kernel((int32_t)mean, gate, fp8);
+    a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
+    // At most one tile per expert is not full.
+    const int64_t slot_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);
+    if (slot_tiles > std::numeric_limits<int32_t>::max() / a.column_tiles)
+        return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", who);
+    void *args[] = {&a};
+    const hipError_t err = hipLaunchKernel((void *)plan.kernel, dim3((unsigned)(slot_tiles * a.column_tiles)), dim3((unsigned)plan.threads),
+                                           args, 0, (hipStream_t)stream);
+    return err == hipSuccess ? EB_OK : fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
+}
+
+} // namespace
+
+extern "C" int eb_expert_product(int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
+                                 const float *x_scales, int64_t ldxs, const int32_t *tokens, const void *w, int64_t ldw,
+                                 const float *w_scales, const int32_t *offsets, const float *bias, int32_t act,
+                                 int32_t out_type, void *out, int64_t ldo, float *out_scales, int64_t ldos, void *stream)
+{
+    try {
+        return product_impl("eb_expert_product", M, E, N, K, x, ldx, x_rows, x_scales, ldxs, tokens, w, ldw, w_scales, offsets,
+                            bias, act, out_type, out, ldo, out_scales, ldos, stream);
+    } catch (...) {
+        return eb_detail::unexpected_exception("eb_expert_product");
+    }
+}

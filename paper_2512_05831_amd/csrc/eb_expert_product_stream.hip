@@ -1,0 +1,152 @@
+// eb_expert_product for few slots per expert: bound by reading the weights.
+//
+// A workgroup of eight waves takes up to 16 * kTokens slots of an expert and a
+// run of its weight rows: kAcross waves side by side, each with kRows tiles of
+// 16 rows, kWaves / kAcross waves along K with every such block of 128 each,
+// joined in LDS in a fixed order.  The products are taken in the 16-bit unit,
+// exact: its rate does not matter here.  Both operands come straight from global
+// memory into the registers of the matrix instructions; each weight is read
+// once per kTokens tiles, and a wave's 16 rows of 128 bytes are whole lines.
+
+#include "eb_expert_product.h"
+
+namespace eb_product {
+
+namespace {
+
+constexpr int kWaves = 8;
+
+template <int kTokens, int kRows, int kAcross, bool kGate, bool kFp8>
+__global__ __launch_bounds__(kWaves *kWave) void eb_product_stream(ProductArgs a)
+{
+    constexpr int kAlong = kWaves / kAcross; // waves along K
+    constexpr int kOut = kGate ? kRows / 2 : kRows;
+    constexpr int kColumns = kAcross * kOut * 16;
+    constexpr int kHeight = kTokens * 16;
+    static_assert(!kFp8 || kColumns == kBlock, "a scale needs its whole block in the workgroup");
+    __shared__ f32x4 part_of[kAlong > 1 ? (kAlong - 1) * kAcross * kRows * kTokens * kWave : 1];
+    __shared__ int most[kFp8 ? kHeight : 1];
+
+    const SlotTile tile = slot_tile<kHeight>(a, blockIdx.x / a.column_tiles);
+    if (tile.expert < 0) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int across = wave % kAcross, along = wave / kAcross;
+    const int32_t column = (blockIdx.x % a.column_tiles) * kColumns + across * kOut * 16;
+    const int chunk = lane / 16;
+
+    const char *wrow[kRows];
+    const float *wscale[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const bool up = kGate && r >= kOut;
+        const int32_t c = column + (up ? r - kOut : r) * 16;
+        const int64_t n = (up ? a.width : 0) + min(c + lane % 16, a.width - 1);
+        wrow[r] = a.w + ((int64_t)tile.expert * a.N + n) * a.ldw;
+        const int32_t b = min(c / kBlock, a.row_blocks - 1) + (up ? a.row_blocks : 0);
+        wscale[r] = a.w_scales + ((int64_t)tile.expert * a.w_blocks + b) * a.k_blocks;
+    }
+    const char *xrow[kTokens];
+    const float *xscale[kTokens];
+    int32_t slot[kTokens];
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+        const int32_t m = tile.first + t * 16 + lane % 16;
+        const int32_t s = min(m, tile.end - 1);
+        const int32_t row = a.tokens ? a.tokens[s] : s;
+        const bool fits = row >= 0 && row < a.x_rows;
+        slot[t] = m < tile.end && fits ? m : -1;
+        xrow[t] = a.x + (fits ? row : 0) * a.ldx;
+        xscale[t] = a.x_scales + (fits ? row : 0);
+    }
+    f32x4 sum[kRows][kTokens] = {};
+    if (a.x_rows > 0) {
+        for (int32_t kb = along; kb < a.k_blocks; kb += kAlong) {
+            const int32_t k0 = kb * kBlock;
+            const int left = a.K - k0; // bytes of this block
+            // A chunk past the end is read at the block's start and cleared.
+            const int lo = chunk * 16 < left ? chunk * 16 : 0, hi = chunk * 16 + 64 < left ? chunk * 16 + 64 : 0;
+            i32x8 w[kRows], x[kTokens];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                w[r] = operand(*(const i32x4 *)(wrow[r] + k0 + lo), *(const i32x4 *)(wrow[r] + k0 + hi));
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t)
+                x[t] = operand(*(const i32x4 *)(xrow[t] + k0 + lo), *(const i32x4 *)(xrow[t] + k0 + hi));
+            if (left < kBlock) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+                    w[r] = operand(first_bytes(w[r].lo, left - chunk * 16), first_bytes(w[r].hi, left - chunk * 16 - 64));
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t)
+                    x[t] = operand(first_bytes(x[t].lo, left - chunk * 16), first_bytes(x[t].hi, left - chunk * 16 - 64));
+            }
+            Wide wide[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) wide[r] = widen8(w[r]);
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) {
+                const float sx = xscale[t][kb * a.ldxs];
+                const Wide xt = widen8(x[t]);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const f32x4 p = block_product(wide[r], xt);
+                    const float f = sx * wscale[r][kb];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[r][t][i] = fmaf(p[i], f, sum[r][t][i]);
+                }
+            }
+        }
+    }
+    if constexpr (kAlong > 1) {
+        auto place = [&](int w, int r, int t) { return (((w - 1) * kAcross + across) * kRows + r) * kTokens + t; };
+        if (along > 0) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) part_of[place(along, r, t) * kWave + lane] = sum[r][t];
+        }
+        __syncthreads();
+        if (along == 0) {
+            for (int w = 1; w < kAlong; ++w)
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                    for (int t = 0; t < kTokens; ++t) sum[r][t] += part_of[place(w, r, t) * kWave + lane];
+        }
+    }
+    if (along == 0) finish<kRows, kTokens, kGate>(a, tile.expert, column, sum);
+    if constexpr (kFp8) {
+        if (threadIdx.x < kHeight) most[threadIdx.x] = 0;
+        __syncthreads();
+        if (along == 0) most_of_outputs<kOut>(a, column, sum, most);
+        __syncthreads();
+        if (along == 0) store_fp8<kOut>(a, column, slot, sum, most, across == 0);
+    } else {
+        if (along == 0) store_floats<kOut>(a, column, slot, sum);
+    }
+}
+
+template <int kTokens, int kRows, int kAcross, bool kGate, bool kFp8>
+KernelPlan plan()
+{
+    return {eb_product_stream<kTokens, kRows, kAcross, kGate, kFp8>, kTokens * 16, kAcross * (kGate ? kRows / 2 : kRows) * 16,
+            kWaves * kWave};
+}
+
+template <int kTokens>
+KernelPlan plan_of(bool gate, bool fp8)
+{
+    if (gate) return fp8 ? plan<kTokens, 2, 8, true, true>() : plan<kTokens, 2, 1, true, false>();
+    return fp8 ? plan<kTokens, 2, 4, false, true>() : plan<kTokens, 1, 1, false, false>();
+}
+
+} // namespace
+
+KernelPlan stream_kernel(int32_t tokens, bool gate, bool fp8)
+{
+    if (tokens <= 16) return plan_of<1>(gate, fp8);
+    if (tokens <= 32) return plan_of<2>(gate, fp8);
+    return plan_of<4>(gate, fp8);
+}
+
+} // namespace eb_product

@@ -1,0 +1,436 @@
+// Routing to experts: eb_route_experts (include/eb_experts.h).
+//
+// For token n with router outputs x (E of them):
+//   s_e = softmax(x)_e or 1 / (1 + exp(-x_e)),  c_e = s_e + bias_e (or x_e,
+//   which orders the same), the K largest c_e of the best groups, w = s there.
+// Then a stable counting sort of the N * K pairs by expert.
+//
+// Three launches, on chunks of kTokens consecutive tokens:
+//   choose   L = 16 lanes (64 for many experts) hold a token's E values in
+//            registers, V each.  K rounds find the largest value left: a
+//            maximum over registers and lanes, then the lowest expert that has
+//            it.  Values are compared as integers that order like the floats:
+//            an integer maximum takes its other operand straight from another
+//            lane (DPP).  Each workgroup counts its pairs per expert.
+//   scan     exclusive prefix of the counts over the chunks.
+//   place    each workgroup ranks its pairs within their experts (in pair
+//            order: the lanes of a wave that hold the same expert find each
+//            other by ballots over the expert's bits) and writes them.
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <limits>
+
+#include "../../include/eb.h"
+#include "../../include/eb_experts.h"
+#include "eb_experts.h"
+#include "eb_internal.h"
+
+namespace {
+
+using namespace eb_experts;
+using eb_detail::fail;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kTokens = 32;        // tokens of a chunk
+constexpr int kMostExperts = 1024;
+constexpr int kMostTop = 64;
+constexpr int kMostGroups = 32;
+
+constexpr int kNoneKey = (int)0x807FFFFF; // the key of -infinity
+constexpr float kInf = __builtin_inff();
+
+struct RouteArgs {
+    const void *scores;
+    const float *bias;
+    int64_t ld;
+    int64_t N;
+    int32_t E, K;
+    int32_t sigmoid, renormalize, pair;
+    int32_t groups, top_groups, group_size;
+    uint32_t group_magic; // e / group_size == e * group_magic >> 20 for e < 1024
+    float scale;
+    int32_t lo, held; // this GPU's experts [lo, lo + held)
+    int32_t *ids;
+    float *weights;
+    int32_t *offsets, *tokens, *slots;
+    uint32_t *counts; // [chunks][held], then [held] totals
+    int64_t chunks;
+};
+
+// An integer that orders like the float (no NaNs; both zeros are equal).
+__device__ __forceinline__ int order_key(float v)
+{
+    const int b = __float_as_int(v + 0.f);
+    return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+
+__device__ __forceinline__ float key_value(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+template <int L, int V, typename T>
+__global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
+{
+    constexpr int kPerWave = kWave / L;
+    constexpr int kPass = kWaves * kPerWave; // tokens a workgroup takes at a time
+    __shared__ uint32_t count[kMostExperts];
+    // Judged scores of the tokens in work, a word of padding per group.
+    __shared__ float judged_of[kPass][L * V + kMostGroups];
+    __shared__ int group_key[kPass][kMostGroups];
+
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % L;
+    const int mine = wave * kPerWave + threadIdx.x % kWave / L; // token of a pass
+    if (a.offsets) {
+        for (int j = threadIdx.x; j < a.held; j += kThreads) count[j] = 0;
+        __syncthreads();
+    }
+    for (int p = 0; p < kTokens; p += kPass) {
+        const int64_t n = (int64_t)blockIdx.x * kTokens + p + mine;
+        if (n >= a.N) break; // ends for whole lane groups; no barrier in the loop
+        const T *row = (const T *)a.scores + n * a.ld;
+        float x[V];
+        int most = kNoneKey;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane;
+            float f = e < a.E ? widen(row[e]) : -kInf;
+            f = f == f ? f : -kInf;
+            x[v] = f < kInf ? f : __FLT_MAX__;
+            most = max(most, order_key(x[v]));
+        }
+        float top_x = 0.f, total = 1.f;
+        int key[V];
+        const bool scored = a.bias || a.pair; // the choice needs the scores themselves
+        if (!a.sigmoid) {
+            top_x = key_value(max_lanes<L>(most));
+            float t = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) t += x[v] > -kInf ? expf(x[v] - top_x) : 0.f;
+            total = sum_lanes<L>(t);
+        }
+        if (!scored) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = order_key(x[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = v * L + lane;
+                float s = a.sigmoid ? sigmoid(x[v]) : expf(x[v] - top_x) / total;
+                if (a.bias) s += e < a.E ? a.bias[e] : 0.f;
+                // A NaN bias makes its expert unfit, as a NaN score does.
+                s = x[v] > -kInf && s == s ? s : -kInf;
+                if (a.pair && e < a.E) judged_of[mine][e + (e * a.group_magic >> 20)] = s;
+                key[v] = a.bias ? order_key(s) : order_key(x[v]);
+            }
+        }
+        if (a.groups > 1) {
+            if (!a.pair) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int e = v * L + lane;
+                    if (e < a.E) judged_of[mine][e + (e * a.group_magic >> 20)] = key_value(key[v]);
+                }
+            }
+            wave_fence();
+            for (int g = lane; g < a.groups; g += L) {
+                float best = -kInf, next = -kInf;
+                for (int i = 0; i < a.group_size; ++i) {
+                    const float s = judged_of[mine][g * (a.group_size + 1) + i];
+                    next = fmaxf(next, fminf(best, s));
+                    best = fmaxf(best, s);
+                }
+                group_key[mine][g] = order_key(!a.pair ? best : next > -kInf ? best + next : -kInf);
+            }
+            wave_fence();
+            int kept = 0;
+            for (int g = lane; g < a.groups; g += L) {
+                const int k = group_key[mine][g];
+                int better = 0;
+                for (int h = 0; h < a.groups; ++h) {
+                    const int o = group_key[mine][h];
+                    better += o > k || (o == k && h < g);
+                }
+                kept |= better < a.top_groups ? 1 << g : 0;
+            }
+            kept = or_lanes<L>(kept);
+            wave_fence(); // the next pass writes the same LDS
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t e = v * L + lane;
+                if (!(kept >> ((e * a.group_magic >> 20) & 31) & 1)) key[v] = kNoneKey;
+            }
+        }
+        // K rounds; lane k of the group keeps round k's result.
+        int id = -1;
+        float x_of = -kInf;
+        for (int k = 0; k < a.K; ++k) {
+            int m = key[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) m = max(m, key[v]);
+            m = max_lanes<L>(m);
+            if (m == kNoneKey) break; // the same for all lanes of a group
+            int e = 0x7FFFFFFF;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) e = key[v] == m ? v * L + lane : e;
+            e = min_lanes<L>(e);
+            float xe = -kInf;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool it = e == v * L + lane;
+                xe = it ? x[v] : xe;
+                key[v] = it ? kNoneKey : key[v];
+            }
+            xe = key_value(max_lanes<L>(order_key(xe))); // only the owner's is above -infinity
+            if (lane == k) {
+                id = e;
+                x_of = xe;
+            }
+        }
+        float w = id < 0 ? 0.f : a.sigmoid ? sigmoid(x_of) : expf(x_of - top_x);
+        if (a.renormalize) {
+            if (a.sigmoid) { // e^-m / (1 + e^-x): no underflow where all x are low
+                const float m = fminf(key_value(max_lanes<L>(order_key(x_of))), 0.f);
+                w = id < 0 ? 0.f : 1.f / (expf(m) + expf(m - x_of));
+            }
+            const float t = sum_lanes<L>(w);
+            w = t > 0.f ? w / t : 0.f;
+        } else if (!a.sigmoid) {
+            w = id < 0 ? 0.f : w / total;
+        }
+        if (lane < a.K) {
+            a.ids[n * a.K + lane] = id;
+            a.weights[n * a.K + lane] = w * a.scale;
+            if (a.offsets && id >= a.lo && id - a.lo < a.held) atomicAdd(&count[id - a.lo], 1u);
+        }
+    }
+    if (!a.offsets) return;
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.held; j += kThreads) a.counts[(int64_t)blockIdx.x * a.held + j] = count[j];
+}
+
+// counts[c][j] becomes the pairs of expert j in the chunks before c; the totals
+// follow the last chunk.  A workgroup takes 64 experts (a lane each), its waves
+// a run of chunks each.
+constexpr int kScanWaves = 16;
+
+__global__ __launch_bounds__(kScanWaves *kWave) void eb_route_scan(RouteArgs a)
+{
+    __shared__ uint32_t sum_of[kScanWaves][kWave];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int j = blockIdx.x * kWave + lane;
+    const int64_t run = (a.chunks + kScanWaves - 1) / kScanWaves;
+    const int64_t c0 = min(a.chunks, wave * run), c1 = min(a.chunks, c0 + run);
+    uint32_t sum = 0;
+    if (j < a.held)
+        for (int64_t c = c0; c < c1; ++c) sum += a.counts[c * a.held + j];
+    sum_of[wave][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (int w = 0; w < kScanWaves; ++w) {
+        before += w < wave ? sum_of[w][lane] : 0;
+        all += sum_of[w][lane];
+    }
+    if (j >= a.held) return;
+    for (int64_t c = c0; c < c1; ++c) {
+        const uint32_t n = a.counts[c * a.held + j];
+        a.counts[c * a.held + j] = before;
+        before += n;
+    }
+    if (wave == 0) a.counts[a.chunks * a.held + j] = all;
+}
+
+__global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
+{
+    __shared__ uint32_t next[kWaves][kMostExperts]; // counts, then the next slot, per wave and expert
+    __shared__ uint32_t wave_sum[kWaves];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t n0 = (int64_t)blockIdx.x * kTokens;
+    const int64_t pairs = a.N * a.K;
+    // This wave's pairs: a quarter of the chunk's tokens.
+    constexpr int kMine = kTokens / kWaves;
+    const int64_t p0 = min(pairs, (n0 + wave * kMine) * a.K), p1 = min(pairs, p0 + (int64_t)kMine * a.K);
+    for (int j = lane; j < a.held; j += kWave) next[wave][j] = 0;
+    wave_fence();
+    for (int64_t p = p0 + lane; p < p1; p += kWave) {
+        const int j = a.ids[p] - a.lo;
+        if (a.ids[p] >= 0 && j >= 0 && j < a.held) atomicAdd(&next[wave][j], 1u);
+    }
+    __syncthreads();
+    // Slots of the experts before mine: an exclusive prefix over the totals,
+    // kThreads experts at a time.
+    const uint32_t *total = a.counts + a.chunks * a.held;
+    uint32_t base = 0;
+    for (int j0 = 0; j0 < a.held; j0 += kThreads) {
+        const int j = j0 + threadIdx.x;
+        const uint32_t mine = j < a.held ? total[j] : 0;
+        uint32_t sum = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const uint32_t o = __shfl_up(sum, d);
+            sum += lane >= d ? o : 0;
+        }
+        if (lane == kWave - 1) wave_sum[wave] = sum;
+        __syncthreads();
+        uint32_t before = base + sum - mine;
+        for (int w = 0; w < wave; ++w) before += wave_sum[w];
+        for (int w = 0; w < kWaves; ++w) base += wave_sum[w];
+        if (j < a.held) {
+            if (blockIdx.x == 0) a.offsets[j] = (int32_t)before;
+            uint32_t at = before + a.counts[(int64_t)blockIdx.x * a.held + j];
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t n = next[w][j];
+                next[w][j] = at;
+                at += n;
+            }
+        }
+        __syncthreads();
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[a.held] = (int32_t)base;
+    const int bits = 32 - __clz(a.held | 1);
+    for (int64_t q = p0; q < p1; q += kWave) {
+        const int64_t p = q + lane;
+        int j = -1;
+        if (p < p1) {
+            const int id = a.ids[p];
+            j = id >= a.lo && id - a.lo < a.held ? id - a.lo : -1;
+        }
+        // The lanes with this lane's expert.
+        uint64_t same = __ballot(j >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot(j >> b & 1);
+            same &= j >> b & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        uint32_t at = 0;
+        if (j >= 0) at = next[wave][j] + rank;
+        wave_fence();
+        if (j >= 0 && rank == 0) next[wave][j] += __popcll(same);
+        wave_fence();
+        if (p < p1) a.slots[p] = j >= 0 ? (int32_t)at : -1;
+        if (j >= 0) a.tokens[at] = (int32_t)(p / a.K);
+        if (p < p1 && p >= base) a.tokens[p] = -1; // past the last slot
+    }
+}
+
+__global__ void eb_route_none(int32_t *offsets, int32_t n)
+{
+    for (int j = threadIdx.x; j < n; j += blockDim.x) offsets[j] = 0;
+}
+
+template <typename T>
+void *choose_kernel(int32_t E, int32_t K)
+{
+    if (K <= 16 && E <= 256) {
+        if (E <= 32) return (void *)eb_route_choose<16, 2, T>;
+        if (E <= 64) return (void *)eb_route_choose<16, 4, T>;
+        if (E <= 128) return (void *)eb_route_choose<16, 8, T>;
+        return (void *)eb_route_choose<16, 16, T>;
+    }
+    if (E <= 256) return (void *)eb_route_choose<64, 4, T>;
+    if (E <= 512) return (void *)eb_route_choose<64, 8, T>;
+    return (void *)eb_route_choose<64, 16, T>;
+}
+
+int64_t chunks_of(int64_t N) { return (N + kTokens - 1) / kTokens; }
+
+size_t workspace_of(int64_t N, int32_t held) { return (size_t)(chunks_of(N) + 1) * (size_t)held * 4; }
+
+int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *scores, int32_t dtype, int64_t ld,
+               const float *bias, int32_t mode, int32_t groups, int32_t top_groups, float scale, int32_t shard_lo,
+               int32_t shard_hi, int32_t *ids, float *weights, int32_t *offsets, int32_t *tokens, int32_t *slots,
+               void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (N < 0 || E < 1 || K < 1 || K > E) return fail(EB_ERR_INVALID, "%s: needs N >= 0 and 1 <= K <= E", who);
+    if (dtype != EB_F32 && dtype != EB_F16 && dtype != EB_BF16) return fail(EB_ERR_INVALID, "%s: unknown dtype", who);
+    const int32_t function = mode & 0xFF;
+    if ((function != EB_SOFTMAX && function != EB_SIGMOID) || (mode & ~(0xFF | EB_RENORMALIZE | EB_GROUP_PAIR)) != 0)
+        return fail(EB_ERR_INVALID, "%s: unknown mode", who);
+    if (groups < 1 || top_groups < 1 || top_groups > groups || E % groups != 0)
+        return fail(EB_ERR_INVALID, "%s: groups must divide E, with 1 <= top_groups <= groups", who);
+    if ((mode & EB_GROUP_PAIR) && E / groups < 2) return fail(EB_ERR_INVALID, "%s: pairs need groups of two or more experts", who);
+    if (shard_lo < 0 || shard_hi < shard_lo || shard_hi > E) return fail(EB_ERR_INVALID, "%s: bad shard range", who);
+    if (!offsets && (tokens || slots)) return fail(EB_ERR_INVALID, "%s: tokens or slots without offsets", who);
+    if (E > kMostExperts || K > kMostTop || groups > kMostGroups)
+        return fail(EB_ERR_UNSUPPORTED, "%s: more than 1024 experts, 64 per token or 32 groups", who);
+    if (N > (int64_t)std::numeric_limits<int32_t>::max() / K) return fail(EB_ERR_UNSUPPORTED, "%s: N * K exceeds 2^31 - 1", who);
+    if (N > 1 && ld < E) return fail(EB_ERR_INVALID, "%s: ld below E", who);
+    if (N > 0 && (!scores || !ids || !weights)) return fail(EB_ERR_INVALID, "%s: NULL scores, ids or weights", who);
+    if (N > 0 && offsets && (!tokens || !slots)) return fail(EB_ERR_INVALID, "%s: NULL tokens or slots", who);
+    const int32_t held = shard_hi - shard_lo;
+    if (N > 0 && offsets && (!workspace || workspace_bytes < workspace_of(N, held) || (uintptr_t)workspace % 4))
+        return fail(EB_ERR_INVALID, "%s: workspace missing, too small or misaligned", who);
+
+    const hipStream_t s = (hipStream_t)stream;
+    if (N == 0) {
+        if (!offsets) return EB_OK;
+        hipLaunchKernelGGL(eb_route_none, dim3(1), dim3(kThreads), 0, s, offsets, held + 1);
+        const hipError_t err = hipGetLastError();
+        return err == hipSuccess ? EB_OK : fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
+    }
+    RouteArgs a{};
+    a.scores = scores;
+    a.bias = bias;
+    a.ld = ld;
+    a.N = N;
+    a.E = E;
+    a.K = K;
+    a.sigmoid = function == EB_SIGMOID;
+    a.renormalize = (mode & EB_RENORMALIZE) != 0;
+    a.pair = (mode & EB_GROUP_PAIR) != 0 && groups > 1;
+    a.groups = groups;
+    a.top_groups = top_groups;
+    a.group_size = E / groups;
+    a.group_magic = (1u << 20) / (uint32_t)a.group_size + 1;
+    a.scale = scale;
+    a.lo = shard_lo;
+    a.held = held;
+    a.ids = ids;
+    a.weights = weights;
+    a.offsets = offsets;
+    a.tokens = tokens;
+    a.slots = slots;
+    a.counts = (uint32_t *)workspace;
+    a.chunks = chunks_of(N);
+    void *kernel = dtype == EB_F32 ? choose_kernel<float>(E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(E, K) : choose_kernel<Bf16>(E, K);
+    void *args[] = {&a};
+    hipError_t err = hipLaunchKernel(kernel, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
+    if (err == hipSuccess && offsets) {
+        if (held > 0) err = hipLaunchKernel((void *)eb_route_scan, dim3((unsigned)((held + kWave - 1) / kWave)), dim3(kScanWaves * kWave), args, 0, s);
+        if (err == hipSuccess) err = hipLaunchKernel((void *)eb_route_place, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
+    }
+    if (err != hipSuccess) return fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
+    return EB_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+int eb_route_experts_workspace(int64_t N, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes)
+{
+    if (!bytes || N < 0 || K < 1 || shard_lo < 0 || shard_hi < shard_lo || shard_hi > kMostExperts ||
+        N > (int64_t)std::numeric_limits<int32_t>::max())
+        return fail(EB_ERR_INVALID, "eb_route_experts_workspace: NULL bytes or a bad size");
+    const size_t n = workspace_of(N, shard_hi - shard_lo);
+    *bytes = n > 0 ? n : 1;
+    return EB_OK;
+}
+
+int eb_route_experts(int64_t N, int32_t E, int32_t K, const void *scores, int32_t dtype, int64_t ld, const float *bias,
+                     int32_t mode, int32_t groups, int32_t top_groups, float scale, int32_t shard_lo, int32_t shard_hi,
+                     int32_t *ids, float *weights, int32_t *offsets, int32_t *tokens, int32_t *slots, void *workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    try {
+        return route_impl("eb_route_experts", N, E, K, scores, dtype, ld, bias, mode, groups, top_groups, scale, shard_lo,
+                          shard_hi, ids, weights, offsets, tokens, slots, workspace, workspace_bytes, stream);
+    } catch (...) {
+        return eb_detail::unexpected_exception("eb_route_experts");
+    }
+}
+
+} // extern "C"
