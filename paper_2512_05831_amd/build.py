@@ -22,7 +22,7 @@ SRCS = [os.path.join(HERE, "csrc", f)
                   "eb_gather_narrow_weighted.hip", "eb_gather_wave.hip",
                   "eb_gather_wave_weighted.hip", "eb_exchange.hip", "eb_ceiling.hip",
                   "eb_route_experts.hip", "eb_quantize_fp8.hip", "eb_expert_product.hip",
-                  "eb_expert_product_stream.hip")]
+                  "eb_expert_product_stream.hip", "eb_expert_product_tile.hip")]
 LIB = os.path.join(HERE, "libeb.so")
 ARCH = "gfx950"
 

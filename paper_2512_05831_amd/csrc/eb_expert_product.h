@@ -141,6 +141,12 @@ __device__ __forceinline__ f32x4 block_product(const Wide &w, const Wide &x)
     return p;
 }
 
+// The same in the 8-bit unit.
+__device__ __forceinline__ f32x4 block_product(i32x8 w, i32x8 x)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+
 __device__ __forceinline__ uint16_t bf16_bits(float v)
 {
     const uint32_t b = __float_as_uint(v);
@@ -296,8 +302,10 @@ struct KernelPlan {
     int32_t height;  // slots of a workgroup
     int32_t columns; // outputs of a workgroup
     int32_t threads;
+    int32_t band;    // the grid holds a multiple of so many slot tiles
 };
 
 KernelPlan stream_kernel(int32_t tokens, bool gate, bool fp8);
+KernelPlan tile_kernel(bool gate, int32_t out_type);
 
 } // namespace eb_product

@@ -80,10 +80,16 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     a.vector_out = ldo % 4 == 0 && (uintptr_t)out % (4 * es) == 0;
 
     const int64_t mean = (M + E - 1) / E;
-    const KernelPlan plan = stream_kernel((int32_t)mean, gate, fp8);
+    // The tile kernel addresses x (a slot tile's rows, or all where they are
+    // gathered) and an expert's weights with 32 bits.
+    constexpr int64_t kMost32 = (int64_t)1 << 32;
+    const bool reachable = N * ldw < kMost32 && (tokens ? x_rows : 256) * ldx < kMost32 && x_rows > 0;
+    const bool tiles = reachable && mean > 64;
+    const KernelPlan plan = tiles ? tile_kernel(gate, out_type) : stream_kernel((int32_t)mean, gate, fp8);
     a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
     // At most one tile per expert is not full.
-    const int64_t slot_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);
+    const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);
+    const int64_t slot_tiles = (most_tiles + plan.band - 1) / plan.band * plan.band;
     if (slot_tiles > std::numeric_limits<int32_t>::max() / a.column_tiles)
         return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", who);
     void *args[] = {&a};

@@ -130,7 +130,7 @@ template <int kTokens, int kRows, int kAcross, bool kGate, bool kFp8>
 KernelPlan plan()
 {
     return {eb_product_stream<kTokens, kRows, kAcross, kGate, kFp8>, kTokens * 16, kAcross * (kGate ? kRows / 2 : kRows) * 16,
-            kWaves * kWave};
+            kWaves * kWave, 1};
 }
 
 template <int kTokens>

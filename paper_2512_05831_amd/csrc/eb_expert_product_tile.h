@@ -1,0 +1,277 @@
+// eb_expert_product for many slots per expert: bound by the matrix units.
+//
+// A workgroup takes kTokens16 * kAcrossT * 16 slots of an expert by
+// kRows16 * kAcrossR * 16 weight rows, a wave kTokens16 x kRows16 tiles of
+// 16 x 16.  A block of 128 of both operands (and the tokens' scales) goes from
+// global memory straight into LDS, double-buffered: the next block is under way
+// while this one is multiplied, and one barrier parts the two.  In LDS a row is
+// its 128 bytes, chunk c of 16 bytes at place c ^ (row % 8): the eight lanes
+// that an LDS access serves at a time then read eight different chunks of the
+// 128-byte line of banks.  (The place in LDS follows from the lane, so it is the
+// global addresses that are permuted.)
+#pragma once
+
+#include <type_traits>
+
+#include "eb_expert_product.h"
+#include "eb_internal.h"
+
+namespace eb_product {
+
+typedef __amdgpu_buffer_rsrc_t Buffer;
+
+__device__ __forceinline__ Buffer buffer_of(const void *p, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000);
+}
+
+// kBytes per lane from a buffer to LDS, lane after lane from `to`.
+template <int kBytes>
+__device__ __forceinline__ void copy_to_lds(Buffer from, void *to, uint32_t lane_offset, uint32_t offset)
+{
+    static_assert(kBytes == 16 || kBytes == 4, "");
+    const auto lds = (__attribute__((address_space(3))) void *)to;
+    if constexpr (kBytes == 16)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, lane_offset, offset, 0, 0);
+    else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, lane_offset, offset, 0, 0);
+}
+
+template <int kTokens16_, int kRows16_, int kAcrossT_, int kAcrossR_, bool kWide_, bool kGate_, bool kFp8_>
+struct TileShape {
+    static constexpr int kTokens16 = kTokens16_, kRows16 = kRows16_, kAcrossT = kAcrossT_, kAcrossR = kAcrossR_;
+    static constexpr bool kWide = kWide_, kGate = kGate_, kFp8 = kFp8_;
+    static constexpr int kWaves = kAcrossT * kAcrossR;
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int kHeight = kTokens16 * kAcrossT * 16; // slots
+    static constexpr int kLines = kRows16 * kAcrossR * 16;    // weight rows
+    static constexpr int kOut16 = kGate ? kRows16 / 2 : kRows16;
+    static constexpr int kColumns = kOut16 * kAcrossR * 16;   // outputs
+    static constexpr int kCopiesX = kHeight / 8 / kWaves, kCopiesW = kLines / 8 / kWaves; // per wave and block
+    static constexpr int kOutBlocks = kColumns / kBlock;
+    static_assert(kHeight % (8 * kWaves) == 0 && kLines % (8 * kWaves) == 0, "whole copies");
+    static_assert(!kFp8 || kColumns % kBlock == 0, "a scale needs its whole block in the workgroup");
+    static_assert(kBlock % (kOut16 * 16) == 0, "a wave's outputs lie in one block");
+};
+
+struct alignas(16) Chunk {
+    char byte[16];
+};
+
+// One block of K of both operands.
+template <typename S>
+struct Stage {
+    Chunk x[S::kHeight][8], w[S::kLines][8];
+    float x_scale[S::kHeight];
+};
+
+// Workgroups are dealt to the 8 XCDs in turn.  Each takes runs of 32 tiles (its
+// compute units), the runs in turn, so that tiles that share operands share an
+// L2 and the empty tiles at the end spread over all.
+__device__ __forceinline__ uint32_t tile_in_order(uint32_t index, uint32_t count)
+{
+    constexpr uint32_t kXcds = 8, kRun = 32;
+    const uint32_t whole = count / (kXcds * kRun) * (kXcds * kRun);
+    if (index >= whole) return index;
+    const uint32_t xcd = index % kXcds, nth = index / kXcds;
+    return (nth / kRun * kXcds + xcd) * kRun + nth % kRun;
+}
+
+constexpr uint32_t kBand = 4; // slot tiles that take their columns together
+
+template <typename S>
+__global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
+{
+    constexpr int T = S::kTokens16, R = S::kRows16;
+    __shared__ Stage<S> stage0, stage1;
+    __shared__ int most[S::kFp8 ? S::kOutBlocks * S::kHeight : 1];
+
+    const uint32_t at = tile_in_order(blockIdx.x, gridDim.x);
+    // kBand slot tiles by all columns: a run of 32 covers 4 x 8 tiles.
+    const uint32_t band = at / (kBand * a.column_tiles), in_band = at % (kBand * a.column_tiles);
+    const SlotTile tile = slot_tile<S::kHeight>(a, (int32_t)(band * kBand + in_band % kBand));
+    if (tile.expert < 0) return;
+    const int32_t column0 = (int32_t)(in_band / kBand) * S::kColumns;
+
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int across_t = wave % S::kAcrossT, across_r = wave / S::kAcrossT;
+
+    // Copies: the i-th of a wave fills rows (i * kWaves + wave) * 8 + lane / 8.
+    const int64_t x_first = a.tokens ? 0 : tile.first; // the buffer's first row
+    const int64_t x_end = a.tokens ? a.x_rows : tile.end;
+    const int64_t row_bytes = ((int64_t)a.K + 15) / 16 * 16; // of the last row; past it a buffer reads as zeros
+    const Buffer x_buffer = buffer_of(a.x + x_first * a.ldx, (uint32_t)((x_end - x_first - 1) * a.ldx + row_bytes));
+    const Buffer w_buffer = buffer_of(a.w + (int64_t)tile.expert * a.N * a.ldw, (uint32_t)((a.N - 1) * a.ldw + row_bytes));
+    const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+    uint32_t x_at[S::kCopiesX], w_at[S::kCopiesW];
+#pragma unroll
+    for (int i = 0; i < S::kCopiesX; ++i) {
+        const int32_t m = min(tile.first + (i * S::kWaves + wave) * 8 + lane / 8, tile.end - 1);
+        int32_t row = m - (int32_t)x_first;
+        if (a.tokens) {
+            row = a.tokens[m];
+            row = row >= 0 && row < a.x_rows ? row : 0;
+        }
+        x_at[i] = (uint32_t)row * (uint32_t)a.ldx + chunk;
+    }
+#pragma unroll
+    for (int i = 0; i < S::kCopiesW; ++i) {
+        const int line = (i * S::kWaves + wave) * 8 + lane / 8;
+        int32_t n = column0 + line;
+        if constexpr (S::kGate) { // a wave's rows: those of the gate, then those it gates
+            constexpr int kHalf = S::kOut16 * 16;
+            const int in_wave = line % (2 * kHalf);
+            n = min(column0 + line / (2 * kHalf) * kHalf + in_wave % kHalf, a.width - 1) + (in_wave >= kHalf ? a.width : 0);
+        } else {
+            n = min(n, a.width - 1);
+        }
+        w_at[i] = (uint32_t)n * (uint32_t)a.ldw + chunk;
+    }
+    // Scales: wave w < kHeight / 64 copies those of slots w * 64 + lane.
+    const bool copies_scales = wave < S::kHeight / kWave;
+    uint32_t scale_at = 0;
+    if (copies_scales) {
+        const int32_t m = min(tile.first + wave * kWave + lane, tile.end - 1);
+        int32_t row = m - (int32_t)x_first;
+        if (a.tokens) {
+            row = a.tokens[m];
+            row = row >= 0 && row < a.x_rows ? row : 0;
+        }
+        scale_at = (uint32_t)row * 4;
+    }
+
+    auto fill = [&](Stage<S> &s, int32_t kb) {
+        const uint32_t k0 = (uint32_t)kb * kBlock;
+#pragma unroll
+        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i], k0);
+#pragma unroll
+        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i], k0);
+        if (copies_scales)
+            copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.x_scale[wave * kWave], scale_at, 0);
+    };
+    // K's last block: what was copied from past a row's end becomes zeros.
+    auto cut = [&](Stage<S> &s, int left) {
+        for (int i = threadIdx.x; i < S::kHeight + S::kLines; i += S::kThreads) {
+            const int row = i < S::kHeight ? i : i - S::kHeight;
+            Chunk *line = i < S::kHeight ? s.x[row] : s.w[row];
+            for (int c = left / 16; c < 8; ++c) {
+                i32x4 *p = (i32x4 *)&line[c ^ row % 8];
+                *p = first_bytes(*p, left - c * 16);
+            }
+        }
+        __syncthreads();
+    };
+
+    const int32_t column = column0 + across_r * S::kOut16 * 16;
+    const int32_t block = min(column / kBlock, a.row_blocks - 1);
+    const float *w_scale = a.w_scales + ((int64_t)tile.expert * a.w_blocks + block) * a.k_blocks;
+    const float *w_scale2 = w_scale + (S::kGate ? (int64_t)a.row_blocks * a.k_blocks : 0);
+
+    f32x4 sum[R][T] = {};
+    auto multiply = [&](const Stage<S> &s, int32_t kb) {
+        const float sw = eb_detail::scalar_load(w_scale + kb), sw2 = S::kGate ? eb_detail::scalar_load(w_scale2 + kb) : sw;
+        const int p = lane / 16 ^ lane % 8;
+        const Chunk(*ws)[8] = &s.w[across_r * R * 16 + lane % 16], (*xs)[8] = &s.x[across_t * T * 16 + lane % 16];
+        const float *scales = &s.x_scale[across_t * T * 16 + lane % 16];
+        auto read = [&](const Chunk(*from)[8], int tile16) {
+            return operand(*(const i32x4 *)&from[tile16 * 16][p], *(const i32x4 *)&from[tile16 * 16][p ^ 4]);
+        };
+        // The sums take a token tile's products while the next tile's are made.
+        using Operand = std::conditional_t<S::kWide, Wide, i32x8>;
+        auto fit = [](i32x8 v) {
+            if constexpr (S::kWide) return widen8(v);
+            else return v;
+        };
+        Operand w[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
+        f32x4 before[R];
+        i32x8 next = read(xs, 0);
+        float f = 0.f, f2 = 0.f;
+#pragma unroll
+        for (int t = 0; t <= T; ++t) {
+            f32x4 now[R];
+            float sx = 0.f;
+            if (t < T) {
+                const Operand x = fit(next);
+                if (t + 1 < T) next = read(xs, t + 1);
+                sx = scales[t * 16];
+#pragma unroll
+                for (int r = 0; r < R; ++r) now[r] = block_product(w[r], x);
+            }
+            if (t > 0) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[r][t - 1][i] = fmaf(before[r][i], r < S::kOut16 ? f : f2, sum[r][t - 1][i]);
+                // Here, not where the sums are next read: the compiler would keep every product until then.
+#pragma unroll
+                for (int r = 0; r < R; ++r) asm volatile("" : "+v"(sum[r][t - 1]));
+            }
+            f = sx * sw;
+            f2 = S::kGate ? sx * sw2 : f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) before[r] = now[r];
+            // A matrix instruction, then vector instructions enough to be done with by the next.
+#pragma unroll
+            for (int i = 0; i < (S::kWide ? 4 * R : R); ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, S::kWide ? 2 : 4, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // This block's copies have landed for all waves, and all are done with the
+    // block before it.
+    auto arrive = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0F70); // vmcnt(0)
+        __syncthreads();
+    };
+    const int tail = a.K % kBlock;
+    fill(stage0, 0);
+    int32_t kb = 0;
+    for (; kb + 1 < a.k_blocks; kb += 2) {
+        arrive();
+        fill(stage1, kb + 1);
+        multiply(stage0, kb);
+        arrive();
+        if (kb + 2 < a.k_blocks) fill(stage0, kb + 2);
+        else if (tail) cut(stage1, tail);
+        multiply(stage1, kb + 1);
+    }
+    if (kb < a.k_blocks) {
+        arrive();
+        if (tail) cut(stage0, tail);
+        multiply(stage0, kb);
+    }
+
+    int32_t slot[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int32_t m = tile.first + (across_t * T + t) * 16 + lane % 16;
+        slot[t] = m < tile.end ? m : -1;
+        if (a.tokens && slot[t] >= 0) {
+            const int32_t row = a.tokens[m];
+            if (row < 0 || row >= a.x_rows) slot[t] = -1;
+        }
+    }
+    finish<R, T, S::kGate>(a, tile.expert, column, sum);
+    if constexpr (S::kFp8) {
+        int *mine = &most[(across_r * S::kOut16 * 16 / kBlock) * S::kHeight + across_t * T * 16];
+        for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) most[i] = 0;
+        __syncthreads();
+        most_of_outputs<S::kOut16>(a, column, sum, mine);
+        __syncthreads();
+        store_fp8<S::kOut16>(a, column, slot, sum, mine, column % kBlock == 0);
+    } else {
+        store_floats<S::kOut16>(a, column, slot, sum);
+    }
+}
+
+template <typename S>
+KernelPlan tile_plan()
+{
+    return {eb_product_tile<S>, S::kHeight, S::kColumns, S::kThreads, kBand};
+}
+
+} // namespace eb_product

@@ -5,6 +5,9 @@ and the sum over the blocks take at most 128 + 2 + blocks additions and
 multiplications, each within 2^-23 (a matrix instruction may truncate) of the
 sum of magnitudes, the bias one more.  Then the activation (exp, a sum, a
 division, two products: 8 roundings), and one rounding to the output's type.
+16-bit outputs may come from the 8-bit matrix unit, which cuts each of eight
+products 13 bits below the largest of them: 8 * 2^-13 of that one for each eight,
+at most 2^-10 of the sum of magnitudes.
 """
 import pytest
 import torch
@@ -54,7 +57,7 @@ class Case:
         return ex.product(self.x, self.xs, self.w, self.ws, offsets=self.offsets, tokens=self.tokens, bias=self.bias,
                           act=self.act, **kw)
 
-    def exact(self):
+    def exact(self, cut=0.0):
         """The outputs of all slots in 64 bits, how far fp32 may be from them, and which slots are written."""
         dev, K = self.x.device, self.K
         col = torch.arange(K, device=dev) // 128
@@ -76,7 +79,7 @@ class Case:
             if self.bias is not None:
                 y[a:b] += self.bias.view(self.E, -1)[e].double()
                 size[a:b] += self.bias.view(self.E, -1)[e].double().abs()
-        off = (128 + 3 + blocks(K)) * 2.0 ** -23 * size
+        off = ((128 + 3 + blocks(K)) * 2.0 ** -23 + cut) * size
         if self.act == ex.EB_ACT_RELU:
             y = y.clamp(min=0)
         if self.gate:
@@ -89,7 +92,7 @@ class Case:
 
 
 def close(got, case, dtype):
-    y, off, written = case.exact()
+    y, off, written = case.exact(2.0 ** -10 if dtype in (torch.float16, torch.bfloat16) else 0.0)
     off = off + UNIT[dtype] * (y.abs() + off) + TINY[dtype]
     bad = ((got.double() - y).abs() > off)[written]
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} outputs, worst {float(((got.double() - y).abs() / off)[written].max()):.2f} bounds off"
