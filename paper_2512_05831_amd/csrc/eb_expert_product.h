@@ -24,6 +24,8 @@
 
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/eb.h"
 #include "../../include/eb_experts.h"
 #include "eb_experts.h"
@@ -47,7 +49,7 @@ struct ProductArgs {
     int32_t w_blocks;    // of a whole expert
     int32_t relu;
     int32_t out_type;
-    int32_t vector_out;  // four neighbouring outputs may be stored at once
+    int32_t vector_out;  // rows of out start at multiples of 16 bytes
     int32_t column_tiles;
 };
 
@@ -147,59 +149,49 @@ __device__ __forceinline__ f32x4 block_product(i32x8 w, i32x8 x)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
 
-__device__ __forceinline__ uint16_t bf16_bits(float v)
+// Four values rounded to nearest even in 16 bits.
+template <typename T>
+__device__ __forceinline__ uint2 pack16(f32x4 v)
 {
-    const uint32_t b = __float_as_uint(v);
-    if ((b & 0x7FFFFFFF) > 0x7F800000) return (uint16_t)(b >> 16 | 0x40); // a NaN stays one
-    return (uint16_t)((b + 0x7FFF + (b >> 16 & 1)) >> 16);
+    typedef T pair __attribute__((ext_vector_type(2)));
+    return make_uint2(__builtin_bit_cast(uint32_t, pair{(T)v[0], (T)v[1]}), __builtin_bit_cast(uint32_t, pair{(T)v[2], (T)v[3]}));
 }
 
-__device__ __forceinline__ uint16_t f16_bits(float v)
+// Four outputs of a slot from `column`, as bits of kSize bytes each.
+template <int kSize, typename Bits>
+__device__ __forceinline__ void store4(const ProductArgs &a, int64_t slot, int32_t column, Bits bits)
 {
-    const _Float16 h = (_Float16)v;
-    return __builtin_bit_cast(uint16_t, h);
-}
-
-// Four outputs of a slot from `column`.
-__device__ __forceinline__ void store4(const ProductArgs &a, int64_t slot, int32_t column, f32x4 v)
-{
-    const int64_t at = slot * a.ldo + column;
-    const int n = min(4, a.width - column);
-    if (n <= 0) return;
-    if (a.out_type == EB_F32) {
-        float *p = (float *)a.out + at;
-        if (n == 4 && a.vector_out) {
-            *(f32x4 *)p = v;
-        } else {
-            for (int i = 0; i < 4; ++i)
-                if (i < n) p[i] = v[i];
-        }
-        return;
-    }
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = a.out_type == EB_F16 ? f16_bits(v[i]) : bf16_bits(v[i]);
-    uint16_t *p = (uint16_t *)a.out + at;
-    if (n == 4 && a.vector_out) {
-        *(uint2 *)p = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+    static_assert(sizeof(Bits) == 4 * kSize, "four outputs");
+    using Element = std::conditional_t<kSize == 4, uint32_t, std::conditional_t<kSize == 2, uint16_t, uint8_t>>;
+    Element *p = (Element *)a.out + slot * a.ldo + column;
+    if (a.vector_out && column + 4 <= a.width) {
+        *(Bits *)p = bits;
     } else {
+        Element e[4];
+        __builtin_memcpy(e, &bits, sizeof e);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = h[i];
+            if (column + i < a.width) p[i] = e[i];
     }
 }
 
-__device__ __forceinline__ f32x4 bias4(const ProductArgs &a, int32_t expert, int32_t row, int32_t end)
+__device__ __forceinline__ f32x4 bias4(const float *bias, int32_t row, int32_t end)
 {
-    f32x4 b = {0.f, 0.f, 0.f, 0.f};
-    if (a.bias) {
+    f32x4 b;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = row + i < end ? a.bias[(int64_t)expert * a.N + row + i] : 0.f;
-    }
+    for (int i = 0; i < 4; ++i) b[i] = bias[min(row + i, end - 1)]; // any past the end: they are not stored
     return b;
 }
 
-__device__ __forceinline__ float silu(float g) { return g / (1.f + expf(-g)); }
+// g / (1 + exp(-g)).  exp(-g) = 2^h (1 + l ln 2) with h + l = -g log2(e) in
+// twice fp32's precision; the hardware's 2^h and reciprocal are within an ulp.
+__device__ __forceinline__ float silu(float g)
+{
+    const float h = g * -1.44269502f, l = fmaf(g, -1.44269502f, -h) + g * -1.92596303e-8f;
+    float e = __builtin_amdgcn_exp2f(h);
+    e = fabsf(h) < 126.f ? fmaf(e, l * 0.693147181f, e) : e; // past it e or 1 does not count
+    return g * __builtin_amdgcn_rcpf(1.f + e);
+}
 
 // The sums of kRows x kTokens tiles (weight rows of one wave) to outputs: bias,
 // activation; under a gate rows [0, kRows / 2) of the tiles are the gate's and
@@ -209,24 +201,30 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int32_t expert, int
 {
     constexpr int kOut = kGate ? kRows / 2 : kRows;
     const int part = threadIdx.x % kWave / 16 * 4;
+    if (a.bias) {
+        const float *bias = a.bias + (int64_t)expert * a.N;
 #pragma unroll
-    for (int r = 0; r < kOut; ++r) {
-        const int32_t c = column + r * 16 + part;
-        const f32x4 b = bias4(a, expert, c, a.width);
-        f32x4 b2 = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (kGate) b2 = bias4(a, expert, a.width + c, a.N);
+        for (int r = 0; r < kRows; ++r) {
+            const bool up = kGate && r >= kOut;
+            const f32x4 b = bias4(up ? bias + a.width : bias, column + (up ? r - kOut : r) * 16 + part, a.width);
 #pragma unroll
-        for (int t = 0; t < kTokens; ++t) {
-            f32x4 v = s[r][t] + b;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (kGate)
-                    v[i] = silu(v[i]) * (s[kOut + r][t][i] + b2[i]);
-                else if (a.relu)
-                    v[i] = v[i] < 0.f ? 0.f : v[i]; // a NaN stays one
-            }
-            s[r][t] = v;
+            for (int t = 0; t < kTokens; ++t) s[r][t] += b;
         }
+    }
+    if constexpr (kGate) {
+#pragma unroll
+        for (int r = 0; r < kOut; ++r)
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][t][i] = silu(s[r][t][i]) * s[kOut + r][t][i];
+    } else if (a.relu) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][t][i] = s[r][t][i] < 0.f ? 0.f : s[r][t][i]; // a NaN stays one
     }
 }
 
@@ -237,12 +235,19 @@ __device__ __forceinline__ void store_floats(const ProductArgs &a, int32_t colum
                                              const f32x4 (&s)[kRows][kTokens])
 {
     const int part = threadIdx.x % kWave / 16 * 4;
+    auto store = [&](auto size, auto bits) {
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t) {
-        if (slot[t] < 0) continue;
+        for (int t = 0; t < kTokens; ++t) {
+            if (slot[t] < 0) continue;
 #pragma unroll
-        for (int r = 0; r < kOut; ++r) store4(a, slot[t], column + r * 16 + part, s[r][t]);
-    }
+            for (int r = 0; r < kOut; ++r) store4<decltype(size)::value>(a, slot[t], column + r * 16 + part, bits(s[r][t]));
+        }
+    };
+    using Four = std::integral_constant<int, 4>;
+    using Two = std::integral_constant<int, 2>;
+    if (a.out_type == EB_F32) store(Four(), [](f32x4 v) { return v; });
+    else if (a.out_type == EB_F16) store(Two(), [](f32x4 v) { return pack16<_Float16>(v); });
+    else store(Two(), [](f32x4 v) { return pack16<__bf16>(v); });
 }
 
 // The largest magnitude of this wave's outputs for each of its tokens into
@@ -267,6 +272,13 @@ __device__ __forceinline__ void most_of_outputs(const ProductArgs &a, int32_t co
     }
 }
 
+// Four outputs in 8 bits under a scale.
+__device__ __forceinline__ int pack_fp8(f32x4 v, float scale)
+{
+    const float f = 1.f / scale; // a product with it: within an ulp of the quotient
+    return eb_experts::pack_fp8(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+}
+
 // 8-bit outputs of one wave, once `most` is complete; `scales`: whether this
 // wave writes the block's scales.
 template <int kOut, int kRows, int kTokens>
@@ -279,18 +291,7 @@ __device__ __forceinline__ void store_fp8(const ProductArgs &a, int32_t column, 
         if (slot[t] < 0) continue;
         const float f = block_scale(most[t * 16 + lane % 16]);
 #pragma unroll
-        for (int r = 0; r < kOut; ++r) {
-            const int32_t c = column + r * 16 + part;
-            const int n = min(4, a.width - c);
-            if (n <= 0) continue;
-            const int q = pack_fp8(s[r][t][0] / f, s[r][t][1] / f, s[r][t][2] / f, s[r][t][3] / f);
-            char *p = (char *)a.out + slot[t] * a.ldo + c;
-            if (n == 4) {
-                *(int *)p = q;
-            } else {
-                for (int i = 0; i < n; ++i) p[i] = (char)(q >> 8 * i);
-            }
-        }
+        for (int r = 0; r < kOut; ++r) store4<1>(a, slot[t], column + r * 16 + part, pack_fp8(s[r][t], f));
         if (scales && lane < 16) a.out_scales[(int64_t)(column / kBlock) * a.ldos + slot[t]] = f;
     }
 }

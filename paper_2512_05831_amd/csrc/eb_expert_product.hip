@@ -77,7 +77,7 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     a.relu = act == EB_ACT_RELU;
     a.out_type = out_type;
     const int es = element_bytes(out_type);
-    a.vector_out = ldo % 4 == 0 && (uintptr_t)out % (4 * es) == 0;
+    a.vector_out = ldo * es % 16 == 0 && (uintptr_t)out % 16 == 0;
 
     const int64_t mean = (M + E - 1) / E;
     // The tile kernel addresses x (a slot tile's rows, or all where they are

@@ -49,6 +49,10 @@ struct TileShape {
     static constexpr int kColumns = kOut16 * kAcrossR * 16;   // outputs
     static constexpr int kCopiesX = kHeight / 8 / kWaves, kCopiesW = kLines / 8 / kWaves; // per wave and block
     static constexpr int kOutBlocks = kColumns / kBlock;
+    // Parts in which 16- and 8-bit outputs pass through the LDS of one stage.
+    static constexpr int kOutBytes = kWide && !kFp8 ? 0 : kHeight * kColumns * (kFp8 ? 1 : 2), kStageBytes = (kHeight + kLines) * kBlock;
+    static constexpr int kPasses = kOutBytes <= kStageBytes ? 1 : kOutBytes <= 2 * kStageBytes ? 2 : 4;
+    static_assert(kOutBytes <= kPasses * kStageBytes && kTokens16 % kPasses == 0, "whole passes");
     static_assert(kHeight % (8 * kWaves) == 0 && kLines % (8 * kWaves) == 0, "whole copies");
     static_assert(!kFp8 || kColumns % kBlock == 0, "a scale needs its whole block in the workgroup");
     static_assert(kBlock % (kOut16 * 16) == 0, "a wave's outputs lie in one block");
@@ -84,6 +88,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
 {
     constexpr int T = S::kTokens16, R = S::kRows16;
     __shared__ Stage<S> stage0, stage1;
+    char *const out_tile = (char *)&stage0; // after the last block
     __shared__ int most[S::kFp8 ? S::kOutBlocks * S::kHeight : 1];
 
     const uint32_t at = tile_in_order(blockIdx.x, gridDim.x);
@@ -168,8 +173,11 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     const float *w_scale2 = w_scale + (S::kGate ? (int64_t)a.row_blocks * a.k_blocks : 0);
 
     f32x4 sum[R][T] = {};
+    // The weights' scales of a block, loaded when the block before has been read
+    // from LDS: with a scalar load among them a wave waits for all its reads.
+    float sw_next = eb_detail::scalar_load(w_scale), sw2_next = eb_detail::scalar_load(w_scale2);
     auto multiply = [&](const Stage<S> &s, int32_t kb) {
-        const float sw = eb_detail::scalar_load(w_scale + kb), sw2 = S::kGate ? eb_detail::scalar_load(w_scale2 + kb) : sw;
+        const float sw = sw_next, sw2 = S::kGate ? sw2_next : sw;
         const int p = lane / 16 ^ lane % 8;
         const Chunk(*ws)[8] = &s.w[across_r * R * 16 + lane % 16], (*xs)[8] = &s.x[across_t * T * 16 + lane % 16];
         const float *scales = &s.x_scale[across_t * T * 16 + lane % 16];
@@ -183,15 +191,20 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
             else return v;
         };
         Operand w[R];
+        i32x8 next = read(xs, 0);
 #pragma unroll
         for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
         f32x4 before[R];
-        i32x8 next = read(xs, 0);
         float f = 0.f, f2 = 0.f;
 #pragma unroll
         for (int t = 0; t <= T; ++t) {
             f32x4 now[R];
             float sx = 0.f;
+            if (t == T) {
+                const int32_t after = min(kb + 1, a.k_blocks - 1);
+                sw_next = eb_detail::scalar_load(w_scale + after);
+                if constexpr (S::kGate) sw2_next = eb_detail::scalar_load(w_scale2 + after);
+            }
             if (t < T) {
                 const Operand x = fit(next);
                 if (t + 1 < T) next = read(xs, t + 1);
@@ -245,26 +258,92 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         multiply(stage0, kb);
     }
 
-    int32_t slot[T];
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-        const int32_t m = tile.first + (across_t * T + t) * 16 + lane % 16;
-        slot[t] = m < tile.end ? m : -1;
-        if (a.tokens && slot[t] >= 0) {
-            const int32_t row = a.tokens[m];
-            if (row < 0 || row >= a.x_rows) slot[t] = -1;
-        }
-    }
     finish<R, T, S::kGate>(a, tile.expert, column, sum);
+    if constexpr (S::kWide && !S::kFp8) {
+        // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.
+        int32_t slot[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int32_t m = tile.first + (across_t * T + t) * 16 + lane % 16;
+            slot[t] = m < tile.end ? m : -1;
+            if (a.tokens && slot[t] >= 0 && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) slot[t] = -1;
+        }
+        store_floats<S::kOut16>(a, column, slot, sum);
+        return;
+    }
+    // Through LDS, so that rows are written in whole lines: token after token of
+    // kColumns outputs, chunk c of 16 bytes at place c ^ token % 16 (a wave's 16
+    // tokens on all banks).  kPasses parts of the tokens where all do not fit.
+    __syncthreads();
+    constexpr int kSize = S::kFp8 ? 1 : 2, kChunks = S::kColumns * kSize / 16;
+    constexpr int kPasses = S::kPasses;
+    auto chunk_of = [&](int token, int c) { return out_tile + (token * kChunks + (c ^ token % (kChunks < 16 ? kChunks : 16))) * 16; };
+    auto to_slots = [&](int pass) {
+        const int left = min(a.width - column0, S::kColumns) * kSize; // bytes of a row
+        for (int i = threadIdx.x; i < S::kHeight / kPasses * kChunks; i += S::kThreads) {
+            // Of each kAcrossT-th of the tile's tokens a pass takes T / kPasses tiles of 16.
+            constexpr int kPart = T / kPasses * 16;
+            const int j = i / kChunks, c = i % kChunks;
+            const int32_t m = tile.first + j / kPart * T * 16 + pass * kPart + j % kPart;
+            if (c * 16 >= left || m >= tile.end) continue;
+            if (a.tokens) {
+                const int32_t row = a.tokens[m];
+                if (row < 0 || row >= a.x_rows) continue;
+            }
+            const char *from = chunk_of(j, c);
+            char *to = (char *)a.out + ((int64_t)m * a.ldo + column0) * kSize + c * 16;
+            if (a.vector_out && c * 16 + 16 <= left) {
+                *(i32x4 *)to = *(const i32x4 *)from;
+            } else {
+                using Element = std::conditional_t<kSize == 2, int16_t, char>;
+                const int n = min(16, left - c * 16) / kSize;
+                for (int k = 0; k < n; ++k) ((Element *)to)[k] = ((const Element *)from)[k];
+            }
+        }
+    };
+    const int part = lane / 16 * 4, in_row = across_r * S::kOut16 * 16;
     if constexpr (S::kFp8) {
-        int *mine = &most[(across_r * S::kOut16 * 16 / kBlock) * S::kHeight + across_t * T * 16];
+        int *mine = &most[in_row / kBlock * S::kHeight + across_t * T * 16];
         for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) most[i] = 0;
         __syncthreads();
         most_of_outputs<S::kOut16>(a, column, sum, mine);
         __syncthreads();
-        store_fp8<S::kOut16>(a, column, slot, sum, mine, column % kBlock == 0);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int token = (across_t * T + t) * 16 + lane % 16;
+            const float f = block_scale(mine[t * 16 + lane % 16]);
+#pragma unroll
+            for (int r = 0; r < S::kOut16; ++r)
+                *(int *)(chunk_of(token, in_row / 16 + r) + part) = pack_fp8(sum[r][t], f);
+        }
+        __syncthreads();
+        to_slots(0);
+        for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) {
+            const int32_t m = tile.first + i % S::kHeight, b = column0 / kBlock + i / S::kHeight;
+            if (m >= tile.end || b >= a.row_blocks) continue;
+            if (a.tokens && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) continue;
+            a.out_scales[(int64_t)b * a.ldos + m] = block_scale(most[i]);
+        }
     } else {
-        store_floats<S::kOut16>(a, column, slot, sum);
+#pragma unroll
+        for (int pass = 0; pass < kPasses; ++pass) {
+            if (pass > 0) __syncthreads();
+            auto to_lds = [&](auto bits) {
+#pragma unroll
+                for (int u = 0; u < T / kPasses; ++u) {
+                    const int t = pass * (T / kPasses) + u, token = (across_t * (T / kPasses) + u) * 16 + lane % 16;
+#pragma unroll
+                    for (int r = 0; r < S::kOut16; ++r) {
+                        const int c = in_row + r * 16 + part;
+                        *(uint2 *)(chunk_of(token, c / 8) + c % 8 * 2) = bits(sum[r][t]);
+                    }
+                }
+            };
+            if (a.out_type == EB_F16) to_lds([](f32x4 v) { return pack16<_Float16>(v); });
+            else to_lds([](f32x4 v) { return pack16<__bf16>(v); });
+            __syncthreads();
+            to_slots(pass);
+        }
     }
 }
 
