@@ -44,12 +44,12 @@ enum { EB_RENORMALIZE = 0x100, EB_GROUP_PAIR = 0x200 };
 enum { EB_ACT_NONE = 0, EB_ACT_RELU = 1, EB_ACT_SILU_GATE = 2 };
 
 /*
- * eb_route_experts_workspace -- device workspace, in bytes (at least 1), of
- * eb_route_experts for N tokens, K experts per token and a shard of
- * shard_hi - shard_lo experts.  Returns EB_ERR_INVALID for NULL bytes or bad
- * sizes.  Touches no device state.
+ * eb_route_experts_workspace -- device workspace, in bytes, of eb_route_experts
+ * for N tokens, K of E experts per token and the shard [shard_lo, shard_hi): 0
+ * for few tokens.  Returns EB_ERR_INVALID for NULL bytes or bad sizes,
+ * EB_ERR_UNSUPPORTED beyond eb_route_experts' limits.  Touches no device state.
  */
-int eb_route_experts_workspace(int64_t N, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes);
+int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes);
 
 /*
  * eb_route_experts -- choose K of E experts for each of N tokens, and group the
@@ -90,7 +90,7 @@ int eb_route_experts_workspace(int64_t N, int32_t K, int32_t shard_lo, int32_t s
  *   slots        device int32 [N, K]: the slot of each pair, or -1.
  *   workspace    device scratch of at least eb_route_experts_workspace()
  *                bytes, 4-byte aligned, owned by the caller; contents not
- *                kept.  May be NULL where offsets is.
+ *                kept.  May be NULL where that is 0, or offsets NULL.
  *
  * Scores, sums and weights are fp32 whatever the type of x.  Equal calls give
  * equal bits.  Errors: EB_ERR_INVALID for an argument outside the above,

@@ -192,47 +192,51 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         };
         Operand w[R];
         i32x8 next = read(xs, 0);
+        float next_scale = scales[0];
 #pragma unroll
         for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
-        f32x4 before[R];
-        float f = 0.f, f2 = 0.f;
+        // Products on their way to the sums: those of the kDelay tiles of 16 x 16
+        // (in the order of tokens, then rows) before the one in work.
+        constexpr int kDelay = S::kWide ? 2 : R;
+        f32x4 product[kDelay];
+        float f[2], f2[2]; // factors of even and odd token tiles
+        auto add = [&](int i) {
+            const int t = i / R, r = i % R;
+            const float factor = r < S::kOut16 ? f[t % 2] : f2[t % 2];
 #pragma unroll
-        for (int t = 0; t <= T; ++t) {
-            f32x4 now[R];
-            float sx = 0.f;
-            if (t == T) {
-                const int32_t after = min(kb + 1, a.k_blocks - 1);
-                sw_next = eb_detail::scalar_load(w_scale + after);
-                if constexpr (S::kGate) sw2_next = eb_detail::scalar_load(w_scale2 + after);
+            for (int j = 0; j < 4; ++j) sum[r][t][j] = fmaf(product[i % kDelay][j], factor, sum[r][t][j]);
+            // Here, not where the sums are next read: the compiler would keep every product until then.
+            asm volatile("" : "+v"(sum[r][t]));
+        };
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const Operand x = fit(next);
+            f[t % 2] = next_scale * sw;
+            f2[t % 2] = S::kGate ? next_scale * sw2 : f[t % 2];
+            if (t + 1 < T) {
+                next = read(xs, t + 1);
+                next_scale = scales[(t + 1) * 16];
             }
-            if (t < T) {
-                const Operand x = fit(next);
-                if (t + 1 < T) next = read(xs, t + 1);
-                sx = scales[t * 16];
 #pragma unroll
-                for (int r = 0; r < R; ++r) now[r] = block_product(w[r], x);
+            for (int r = 0; r < R; ++r) {
+                const int i = t * R + r;
+                if (i >= kDelay) add(i - kDelay);
+                product[i % kDelay] = block_product(w[r], x);
             }
-            if (t > 0) {
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[r][t - 1][i] = fmaf(before[r][i], r < S::kOut16 ? f : f2, sum[r][t - 1][i]);
-                // Here, not where the sums are next read: the compiler would keep every product until then.
-#pragma unroll
-                for (int r = 0; r < R; ++r) asm volatile("" : "+v"(sum[r][t - 1]));
-            }
-            f = sx * sw;
-            f2 = S::kGate ? sx * sw2 : f;
-#pragma unroll
-            for (int r = 0; r < R; ++r) before[r] = now[r];
-            // A matrix instruction, then vector instructions enough to be done with by the next.
+            // The vector instructions evenly between the matrix instructions.
 #pragma unroll
             for (int i = 0; i < (S::kWide ? 4 * R : R); ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, S::kWide ? 2 : 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        const int32_t after = min(kb + 1, a.k_blocks - 1);
+        sw_next = eb_detail::scalar_load(w_scale + after);
+        if constexpr (S::kGate) sw2_next = eb_detail::scalar_load(w_scale2 + after);
+#pragma unroll
+        for (int i = R * T - kDelay; i < R * T; ++i) add(i);
+        __builtin_amdgcn_sched_barrier(0);
     };
     // This block's copies have landed for all waves, and all are done with the
     // block before it.

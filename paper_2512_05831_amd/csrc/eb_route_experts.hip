@@ -5,17 +5,22 @@
 //   which orders the same), the K largest c_e of the best groups, w = s there.
 // Then a stable counting sort of the N * K pairs by expert.
 //
-// Three launches, on chunks of kTokens consecutive tokens:
-//   choose   L = 16 lanes (64 for many experts) hold a token's E values in
-//            registers, V each.  K rounds find the largest value left: a
-//            maximum over registers and lanes, then the lowest expert that has
-//            it.  Values are compared as integers that order like the floats:
-//            an integer maximum takes its other operand straight from another
-//            lane (DPP).  Each workgroup counts its pairs per expert.
-//   scan     exclusive prefix of the counts over the chunks.
-//   place    each workgroup ranks its pairs within their experts (in pair
-//            order: the lanes of a wave that hold the same expert find each
-//            other by ballots over the expert's bits) and writes them.
+// choose  L = 16 lanes (64 for many experts) hold a token's E values in
+//         registers, V each, as integers that order like the floats (an
+//         integer maximum takes its other operand straight from another lane).
+//         With 16 lanes and K <= 8: the K-th largest of the lanes' maxima
+//         bounds the K best values from below, those above it (eleven or so
+//         where K is 8) go to LDS, a lane takes one each and counts the better
+//         ones: about 220 instructions, where K rounds of "largest value left,
+//         lowest expert that has it, out with it" are 680 (16 values a lane).
+//         Those rounds are taken where more than 16 values reach the bound, and
+//         for other K and L.  Each workgroup counts its pairs per expert.
+// scan    exclusive prefix of the counts over the chunks of kTokens tokens.
+// place   each workgroup ranks its pairs within their experts (in pair order:
+//         the lanes of a wave that hold the same expert find each other by
+//         ballots over the expert's bits) and writes them.
+// Up to kFewTokens tokens and kFewPairs pairs one workgroup does all of it in
+// one launch, the pairs and counts in LDS.
 
 #include <hip/hip_runtime.h>
 
@@ -36,6 +41,9 @@ using eb_detail::fail;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTokens = 32;        // tokens of a chunk
+constexpr int kFewWaves = 16;      // of the workgroup that does all
+constexpr int kFewTokens = 256, kFewPairs = 2048;
+constexpr int kFilterTop = 8;      // most experts per token for the filter
 constexpr int kMostExperts = 1024;
 constexpr int kMostTop = 64;
 constexpr int kMostGroups = 32;
@@ -70,7 +78,215 @@ __device__ __forceinline__ int order_key(float v)
 
 __device__ __forceinline__ float key_value(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
 
+// Rounded as torch's 1 / (1 + exp(-x)) is: choices rest on its last bit.
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+// exp(v) of v <= 0 within 2 ulp: 2^h (1 + l ln 2), h + l = v log2(e).
+__device__ __forceinline__ float exp_of(float v)
+{
+    const float h = v * 1.44269502f, l = fmaf(v, 1.44269502f, -h) + v * 1.92596303e-8f, e = __builtin_amdgcn_exp2f(h);
+    return h > -126.f ? fmaf(e, l * 0.693147181f, e) : 0.f;
+}
+
+struct Candidate {
+    int key, expert;
+};
+
+// What a lane group has in LDS for one token.
+template <int L, int V>
+struct TokenSpace {
+    union {
+        struct {
+            float judged[L * V + kMostGroups]; // scores, a word of padding per group
+            int group_key[kMostGroups];
+        };
+        struct {
+            Candidate found[16 + L]; // from 16 on: what is not wanted
+            Candidate best[16];
+        };
+    };
+};
+
+// The K best of a token's experts, of which lane k gets the k-th: its expert
+// (-1: none left) and key.  key[v] of lane i is expert v * L + i's.
+template <int L, int V>
+__device__ __forceinline__ void best_by_rounds(int (&key)[V], int lane, int K, int &id, int &id_key)
+{
+    for (int k = 0; k < K; ++k) {
+        int m = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) m = max(m, key[v]);
+        m = max_lanes<L>(m);
+        if (m == kNoneKey) break; // the same for all lanes of a group
+        int e = 0x7FFFFFFF;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v) e = key[v] == m ? v * L + lane : e;
+        e = min_lanes<L>(e);
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = e == v * L + lane ? kNoneKey : key[v];
+        if (lane == k) {
+            id = e;
+            id_key = m;
+        }
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void best_by_filter(int (&key)[V], int lane, int K, TokenSpace<16, V> &space, int &id, int &id_key)
+{
+    int m = key[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) m = max(m, key[v]);
+    int greater = 0;
+#define EB_COUNT(S) greater += rotate16<S>(m) > m;
+    EB_COUNT(1) EB_COUNT(2) EB_COUNT(3) EB_COUNT(4) EB_COUNT(5) EB_COUNT(6) EB_COUNT(7) EB_COUNT(8)
+    EB_COUNT(9) EB_COUNT(10) EB_COUNT(11) EB_COUNT(12) EB_COUNT(13) EB_COUNT(14) EB_COUNT(15)
+#undef EB_COUNT
+    const int bound = max(min_lanes<16>(greater < K ? m : 0x7FFFFFFF), kNoneKey + 1);
+    int mine = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine += key[v] >= bound;
+    int upto = mine; // inclusive prefix over the 16 lanes
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xF, 0xF, false);
+    const int n = max_lanes<16>(upto);
+    if (__any(n > 16)) return best_by_rounds<16, V>(key, lane, K, id, id_key);
+    int at = upto - mine;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const bool wanted = key[v] >= bound;
+        space.found[wanted ? at : 16 + lane] = {key[v], v * 16 + lane};
+        at += wanted;
+    }
+    wave_fence();
+    const Candidate own = lane < n ? space.found[lane] : Candidate{kNoneKey, 0x7FFFFFFF};
+    int rank = 0;
+    for (int j = 0; j < n; ++j) {
+        const Candidate o = space.found[j];
+        rank += o.key > own.key || (o.key == own.key && o.expert < own.expert);
+    }
+    if (lane < n) space.best[rank] = own;
+    wave_fence();
+    if (lane < min(n, K)) {
+        id = space.best[lane].expert;
+        id_key = space.best[lane].key;
+    }
+    wave_fence(); // the next token's values come to the same LDS
+}
+
+// One token by a lane group: lane k < K returns its k-th expert and weight.
+template <int L, int V, typename T>
+__device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, TokenSpace<L, V> &space, int &id, float &weight)
+{
+    const T *row = (const T *)a.scores + n * a.ld;
+    float x[V];
+    int key[V];
+    const bool scored = a.bias || a.pair; // the choice needs the scores themselves
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = v * L + lane;
+        float f = e < a.E ? widen(row[e]) : -kInf;
+        f = f == f ? f : -kInf;
+        x[v] = f < kInf ? f : __FLT_MAX__;
+        key[v] = order_key(x[v]);
+    }
+    float top_x = 0.f, total = 1.f;
+    if (!a.sigmoid) {
+        int most = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) most = max(most, key[v]);
+        top_x = key_value(max_lanes<L>(most));
+        if (scored || !a.renormalize) {
+            float t = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) t += x[v] > -kInf ? exp_of(x[v] - top_x) : 0.f;
+            total = sum_lanes<L>(t);
+        }
+    }
+    if (scored) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane;
+            float s = a.sigmoid ? sigmoid(x[v]) : exp_of(x[v] - top_x) / total;
+            if (a.bias) s += e < a.E ? a.bias[e] : 0.f;
+            // A NaN bias makes its expert unfit, as a NaN score does.
+            s = x[v] > -kInf && s == s ? s : -kInf;
+            if (a.pair && e < a.E) space.judged[e + (e * a.group_magic >> 20)] = s;
+            if (a.bias) key[v] = order_key(s);
+        }
+    }
+    if (a.groups > 1) {
+        if (!a.pair) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = v * L + lane;
+                if (e < a.E) space.judged[e + (e * a.group_magic >> 20)] = key_value(key[v]);
+            }
+        }
+        wave_fence();
+        for (int g = lane; g < a.groups; g += L) {
+            float best = -kInf, next = -kInf;
+            for (int i = 0; i < a.group_size; ++i) {
+                const float s = space.judged[g * (a.group_size + 1) + i];
+                next = fmaxf(next, fminf(best, s));
+                best = fmaxf(best, s);
+            }
+            space.group_key[g] = order_key(!a.pair ? best : next > -kInf ? best + next : -kInf);
+        }
+        wave_fence();
+        int kept = 0;
+        for (int g = lane; g < a.groups; g += L) {
+            const int k = space.group_key[g];
+            int better = 0;
+            for (int h = 0; h < a.groups; ++h) {
+                const int o = space.group_key[h];
+                better += o > k || (o == k && h < g);
+            }
+            kept |= better < a.top_groups ? 1 << g : 0;
+        }
+        kept = or_lanes<L>(kept);
+        wave_fence();
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t e = v * L + lane;
+            if (!(kept >> ((e * a.group_magic >> 20) & 31) & 1)) key[v] = kNoneKey;
+        }
+    }
+    int id_key = kNoneKey;
+    id = -1;
+    if constexpr (L == 16 && V >= 4) {
+        if (a.K <= kFilterTop) best_by_filter<V>(key, lane, a.K, space, id, id_key);
+        else best_by_rounds<L, V>(key, lane, a.K, id, id_key);
+    } else {
+        best_by_rounds<L, V>(key, lane, a.K, id, id_key);
+    }
+    // The key is x's, or the biased score's: then x is read again.
+    float x_of = id < 0 ? -kInf : key_value(id_key);
+    if (a.bias && id >= 0) {
+        x_of = widen(row[id]);
+        x_of = x_of < kInf ? x_of : __FLT_MAX__;
+    }
+    float w = id < 0 ? 0.f : a.sigmoid ? sigmoid(x_of) : exp_of(x_of - top_x);
+    if (a.renormalize) {
+        if (a.sigmoid) { // e^-m / (1 + e^-x): no underflow where all x are low
+            const float m = fminf(key_value(max_lanes<L>(order_key(x_of))), 0.f);
+            w = id < 0 ? 0.f : 1.f / (expf(m) + expf(m - x_of));
+        }
+        const float t = sum_lanes<L>(w);
+        w = t > 0.f ? w / t : 0.f;
+    } else if (!a.sigmoid) {
+        w = id < 0 ? 0.f : w / total;
+    }
+    weight = w * a.scale;
+}
+
+// The pair's expert as one of this GPU's, or -1.
+__device__ __forceinline__ int held_expert(const RouteArgs &a, int id)
+{
+    return id >= a.lo && id - a.lo < a.held ? id - a.lo : -1;
+}
 
 template <int L, int V, typename T>
 __global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
@@ -78,12 +294,9 @@ __global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
     constexpr int kPerWave = kWave / L;
     constexpr int kPass = kWaves * kPerWave; // tokens a workgroup takes at a time
     __shared__ uint32_t count[kMostExperts];
-    // Judged scores of the tokens in work, a word of padding per group.
-    __shared__ float judged_of[kPass][L * V + kMostGroups];
-    __shared__ int group_key[kPass][kMostGroups];
+    __shared__ TokenSpace<L, V> space[kPass];
 
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % L;
-    const int mine = wave * kPerWave + threadIdx.x % kWave / L; // token of a pass
+    const int lane = threadIdx.x % L, mine = threadIdx.x / L; // token of a pass
     if (a.offsets) {
         for (int j = threadIdx.x; j < a.held; j += kThreads) count[j] = 0;
         __syncthreads();
@@ -91,125 +304,114 @@ __global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
     for (int p = 0; p < kTokens; p += kPass) {
         const int64_t n = (int64_t)blockIdx.x * kTokens + p + mine;
         if (n >= a.N) break; // ends for whole lane groups; no barrier in the loop
-        const T *row = (const T *)a.scores + n * a.ld;
-        float x[V];
-        int most = kNoneKey;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = v * L + lane;
-            float f = e < a.E ? widen(row[e]) : -kInf;
-            f = f == f ? f : -kInf;
-            x[v] = f < kInf ? f : __FLT_MAX__;
-            most = max(most, order_key(x[v]));
-        }
-        float top_x = 0.f, total = 1.f;
-        int key[V];
-        const bool scored = a.bias || a.pair; // the choice needs the scores themselves
-        if (!a.sigmoid) {
-            top_x = key_value(max_lanes<L>(most));
-            float t = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) t += x[v] > -kInf ? expf(x[v] - top_x) : 0.f;
-            total = sum_lanes<L>(t);
-        }
-        if (!scored) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = order_key(x[v]);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int e = v * L + lane;
-                float s = a.sigmoid ? sigmoid(x[v]) : expf(x[v] - top_x) / total;
-                if (a.bias) s += e < a.E ? a.bias[e] : 0.f;
-                // A NaN bias makes its expert unfit, as a NaN score does.
-                s = x[v] > -kInf && s == s ? s : -kInf;
-                if (a.pair && e < a.E) judged_of[mine][e + (e * a.group_magic >> 20)] = s;
-                key[v] = a.bias ? order_key(s) : order_key(x[v]);
-            }
-        }
-        if (a.groups > 1) {
-            if (!a.pair) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int e = v * L + lane;
-                    if (e < a.E) judged_of[mine][e + (e * a.group_magic >> 20)] = key_value(key[v]);
-                }
-            }
-            wave_fence();
-            for (int g = lane; g < a.groups; g += L) {
-                float best = -kInf, next = -kInf;
-                for (int i = 0; i < a.group_size; ++i) {
-                    const float s = judged_of[mine][g * (a.group_size + 1) + i];
-                    next = fmaxf(next, fminf(best, s));
-                    best = fmaxf(best, s);
-                }
-                group_key[mine][g] = order_key(!a.pair ? best : next > -kInf ? best + next : -kInf);
-            }
-            wave_fence();
-            int kept = 0;
-            for (int g = lane; g < a.groups; g += L) {
-                const int k = group_key[mine][g];
-                int better = 0;
-                for (int h = 0; h < a.groups; ++h) {
-                    const int o = group_key[mine][h];
-                    better += o > k || (o == k && h < g);
-                }
-                kept |= better < a.top_groups ? 1 << g : 0;
-            }
-            kept = or_lanes<L>(kept);
-            wave_fence(); // the next pass writes the same LDS
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t e = v * L + lane;
-                if (!(kept >> ((e * a.group_magic >> 20) & 31) & 1)) key[v] = kNoneKey;
-            }
-        }
-        // K rounds; lane k of the group keeps round k's result.
-        int id = -1;
-        float x_of = -kInf;
-        for (int k = 0; k < a.K; ++k) {
-            int m = key[0];
-#pragma unroll
-            for (int v = 1; v < V; ++v) m = max(m, key[v]);
-            m = max_lanes<L>(m);
-            if (m == kNoneKey) break; // the same for all lanes of a group
-            int e = 0x7FFFFFFF;
-#pragma unroll
-            for (int v = V - 1; v >= 0; --v) e = key[v] == m ? v * L + lane : e;
-            e = min_lanes<L>(e);
-            float xe = -kInf;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool it = e == v * L + lane;
-                xe = it ? x[v] : xe;
-                key[v] = it ? kNoneKey : key[v];
-            }
-            xe = key_value(max_lanes<L>(order_key(xe))); // only the owner's is above -infinity
-            if (lane == k) {
-                id = e;
-                x_of = xe;
-            }
-        }
-        float w = id < 0 ? 0.f : a.sigmoid ? sigmoid(x_of) : expf(x_of - top_x);
-        if (a.renormalize) {
-            if (a.sigmoid) { // e^-m / (1 + e^-x): no underflow where all x are low
-                const float m = fminf(key_value(max_lanes<L>(order_key(x_of))), 0.f);
-                w = id < 0 ? 0.f : 1.f / (expf(m) + expf(m - x_of));
-            }
-            const float t = sum_lanes<L>(w);
-            w = t > 0.f ? w / t : 0.f;
-        } else if (!a.sigmoid) {
-            w = id < 0 ? 0.f : w / total;
-        }
+        int id;
+        float w;
+        choose<L, V, T>(a, n, lane, space[mine], id, w);
         if (lane < a.K) {
             a.ids[n * a.K + lane] = id;
-            a.weights[n * a.K + lane] = w * a.scale;
-            if (a.offsets && id >= a.lo && id - a.lo < a.held) atomicAdd(&count[id - a.lo], 1u);
+            a.weights[n * a.K + lane] = w;
+            if (a.offsets && held_expert(a, id) >= 0) atomicAdd(&count[id - a.lo], 1u);
         }
     }
     if (!a.offsets) return;
     __syncthreads();
     for (int j = threadIdx.x; j < a.held; j += kThreads) a.counts[(int64_t)blockIdx.x * a.held + j] = count[j];
+}
+
+// The lanes of a wave that hold the same expert j (those with j < 0: none).
+__device__ __forceinline__ uint64_t same_expert(int j, int bits)
+{
+    uint64_t same = __ballot(j >= 0);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(j >> b & 1);
+        same &= j >> b & 1 ? set : ~set;
+    }
+    return same;
+}
+
+// Inclusive prefix over a wave.
+__device__ __forceinline__ uint32_t prefix_in_wave(uint32_t v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t o = __shfl_up(v, d);
+        v += (int)(threadIdx.x % kWave) >= d ? o : 0;
+    }
+    return v;
+}
+
+// The whole of it for few tokens, in one workgroup.
+template <int L, int V, typename T>
+__global__ __launch_bounds__(kFewWaves *kWave) void eb_route_few(RouteArgs a)
+{
+    constexpr int kAll = kFewWaves * kWave, kPass = kAll / L;
+    __shared__ union {
+        TokenSpace<L, V> token[kPass];
+        uint32_t next[kFewWaves][kMostExperts]; // counts, then the next slot, per wave and expert
+    } space;
+    __shared__ int16_t expert_of[kFewPairs];
+    __shared__ uint32_t wave_sum[kFewWaves];
+
+    const int wave = threadIdx.x / kWave, in_wave = threadIdx.x % kWave, lane = threadIdx.x % L;
+    for (int p = threadIdx.x / L; p < a.N; p += kPass) {
+        int id;
+        float w;
+        choose<L, V, T>(a, p, lane, space.token[threadIdx.x / L], id, w);
+        if (lane < a.K) {
+            a.ids[p * a.K + lane] = id;
+            a.weights[p * a.K + lane] = w;
+            expert_of[p * a.K + lane] = (int16_t)held_expert(a, id);
+        }
+    }
+    if (!a.offsets) return;
+    __syncthreads();
+    // A wave takes a run of the pairs.
+    const int pairs = (int)a.N * a.K, run = (pairs + kFewWaves - 1) / kFewWaves;
+    const int p0 = min(pairs, wave * run), p1 = min(pairs, p0 + run);
+    for (int j = in_wave; j < a.held; j += kWave) space.next[wave][j] = 0;
+    wave_fence();
+    for (int p = p0 + in_wave; p < p1; p += kWave)
+        if (expert_of[p] >= 0) atomicAdd(&space.next[wave][expert_of[p]], 1u);
+    __syncthreads();
+    // kMostExperts threads: an expert each.
+    static_assert(kAll >= kMostExperts, "a thread per expert");
+    const int j = threadIdx.x;
+    uint32_t sum = 0;
+    if (j < a.held)
+        for (int w = 0; w < kFewWaves; ++w) {
+            const uint32_t n = space.next[w][j];
+            space.next[w][j] = sum;
+            sum += n;
+        }
+    const uint32_t upto = prefix_in_wave(sum);
+    if (in_wave == kWave - 1) wave_sum[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - sum, total = 0;
+    for (int w = 0; w < kFewWaves; ++w) {
+        before += w < wave ? wave_sum[w] : 0;
+        total += wave_sum[w];
+    }
+    if (j < a.held) {
+        a.offsets[j] = (int32_t)before;
+        for (int w = 0; w < kFewWaves; ++w) space.next[w][j] += before;
+    }
+    if (j == 0) a.offsets[a.held] = (int32_t)total;
+    __syncthreads();
+    const int bits = 32 - __clz(a.held | 1);
+    for (int q = p0; q < p1; q += kWave) {
+        const int p = q + in_wave;
+        const int e = p < p1 ? expert_of[p] : -1;
+        const uint64_t same = same_expert(e, bits);
+        const int rank = __popcll(same & ((1ull << in_wave) - 1));
+        uint32_t at = 0;
+        if (e >= 0) at = space.next[wave][e] + rank;
+        wave_fence();
+        if (e >= 0 && rank == 0) space.next[wave][e] += __popcll(same);
+        wave_fence();
+        if (p < p1) a.slots[p] = e >= 0 ? (int32_t)at : -1;
+        if (e >= 0) a.tokens[at] = p / a.K;
+        if (p < p1 && p >= (int)total) a.tokens[p] = -1; // past the last slot
+    }
 }
 
 // counts[c][j] becomes the pairs of expert j in the chunks before c; the totals
@@ -256,8 +458,8 @@ __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
     for (int j = lane; j < a.held; j += kWave) next[wave][j] = 0;
     wave_fence();
     for (int64_t p = p0 + lane; p < p1; p += kWave) {
-        const int j = a.ids[p] - a.lo;
-        if (a.ids[p] >= 0 && j >= 0 && j < a.held) atomicAdd(&next[wave][j], 1u);
+        const int j = held_expert(a, a.ids[p]);
+        if (j >= 0) atomicAdd(&next[wave][j], 1u);
     }
     __syncthreads();
     // Slots of the experts before mine: an exclusive prefix over the totals,
@@ -267,12 +469,7 @@ __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
     for (int j0 = 0; j0 < a.held; j0 += kThreads) {
         const int j = j0 + threadIdx.x;
         const uint32_t mine = j < a.held ? total[j] : 0;
-        uint32_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-            const uint32_t o = __shfl_up(sum, d);
-            sum += lane >= d ? o : 0;
-        }
+        const uint32_t sum = prefix_in_wave(mine);
         if (lane == kWave - 1) wave_sum[wave] = sum;
         __syncthreads();
         uint32_t before = base + sum - mine;
@@ -293,17 +490,8 @@ __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
     const int bits = 32 - __clz(a.held | 1);
     for (int64_t q = p0; q < p1; q += kWave) {
         const int64_t p = q + lane;
-        int j = -1;
-        if (p < p1) {
-            const int id = a.ids[p];
-            j = id >= a.lo && id - a.lo < a.held ? id - a.lo : -1;
-        }
-        // The lanes with this lane's expert.
-        uint64_t same = __ballot(j >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot(j >> b & 1);
-            same &= j >> b & 1 ? set : ~set;
-        }
+        const int j = p < p1 ? held_expert(a, a.ids[p]) : -1;
+        const uint64_t same = same_expert(j, bits);
         const int rank = __popcll(same & ((1ull << lane) - 1));
         uint32_t at = 0;
         if (j >= 0) at = next[wave][j] + rank;
@@ -321,23 +509,39 @@ __global__ void eb_route_none(int32_t *offsets, int32_t n)
     for (int j = threadIdx.x; j < n; j += blockDim.x) offsets[j] = 0;
 }
 
+template <int L, int V, typename T>
+void *kernel_of(bool few)
+{
+    return few ? (void *)eb_route_few<L, V, T> : (void *)eb_route_choose<L, V, T>;
+}
+
 template <typename T>
-void *choose_kernel(int32_t E, int32_t K)
+void *choose_kernel(bool few, int32_t E, int32_t K)
 {
     if (K <= 16 && E <= 256) {
-        if (E <= 32) return (void *)eb_route_choose<16, 2, T>;
-        if (E <= 64) return (void *)eb_route_choose<16, 4, T>;
-        if (E <= 128) return (void *)eb_route_choose<16, 8, T>;
-        return (void *)eb_route_choose<16, 16, T>;
+        if (E <= 32) return kernel_of<16, 2, T>(few);
+        if (E <= 64) return kernel_of<16, 4, T>(few);
+        if (E <= 128) return kernel_of<16, 8, T>(few);
+        return kernel_of<16, 16, T>(few);
     }
-    if (E <= 256) return (void *)eb_route_choose<64, 4, T>;
-    if (E <= 512) return (void *)eb_route_choose<64, 8, T>;
-    return (void *)eb_route_choose<64, 16, T>;
+    if (E <= 256) return kernel_of<64, 4, T>(few);
+    if (E <= 512) return kernel_of<64, 8, T>(few);
+    return kernel_of<64, 16, T>(few);
+}
+
+// Whether one workgroup does all: it takes kPass = 64 tokens at a time (16 with 64 lanes each).
+bool few_tokens(int64_t N, int32_t E, int32_t K)
+{
+    const bool wide = K > 16 || E > 256;
+    return N <= (wide ? kFewTokens / 4 : kFewTokens) && N * K <= kFewPairs;
 }
 
 int64_t chunks_of(int64_t N) { return (N + kTokens - 1) / kTokens; }
 
-size_t workspace_of(int64_t N, int32_t held) { return (size_t)(chunks_of(N) + 1) * (size_t)held * 4; }
+size_t workspace_of(int64_t N, int32_t E, int32_t K, int32_t held)
+{
+    return few_tokens(N, E, K) ? 0 : (size_t)(chunks_of(N) + 1) * (size_t)held * 4;
+}
 
 int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *scores, int32_t dtype, int64_t ld,
                const float *bias, int32_t mode, int32_t groups, int32_t top_groups, float scale, int32_t shard_lo,
@@ -361,7 +565,8 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     if (N > 0 && (!scores || !ids || !weights)) return fail(EB_ERR_INVALID, "%s: NULL scores, ids or weights", who);
     if (N > 0 && offsets && (!tokens || !slots)) return fail(EB_ERR_INVALID, "%s: NULL tokens or slots", who);
     const int32_t held = shard_hi - shard_lo;
-    if (N > 0 && offsets && (!workspace || workspace_bytes < workspace_of(N, held) || (uintptr_t)workspace % 4))
+    const size_t needed = offsets ? workspace_of(N, E, K, held) : 0;
+    if (needed > 0 && (!workspace || workspace_bytes < needed || (uintptr_t)workspace % 4))
         return fail(EB_ERR_INVALID, "%s: workspace missing, too small or misaligned", who);
 
     const hipStream_t s = (hipStream_t)stream;
@@ -395,10 +600,12 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     a.slots = slots;
     a.counts = (uint32_t *)workspace;
     a.chunks = chunks_of(N);
-    void *kernel = dtype == EB_F32 ? choose_kernel<float>(E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(E, K) : choose_kernel<Bf16>(E, K);
+    const bool few = few_tokens(N, E, K);
+    void *kernel = dtype == EB_F32 ? choose_kernel<float>(few, E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(few, E, K) : choose_kernel<Bf16>(few, E, K);
     void *args[] = {&a};
-    hipError_t err = hipLaunchKernel(kernel, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
-    if (err == hipSuccess && offsets) {
+    hipError_t err = few ? hipLaunchKernel(kernel, dim3(1), dim3(kFewWaves * kWave), args, 0, s)
+                         : hipLaunchKernel(kernel, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
+    if (err == hipSuccess && offsets && !few) {
         if (held > 0) err = hipLaunchKernel((void *)eb_route_scan, dim3((unsigned)((held + kWave - 1) / kWave)), dim3(kScanWaves * kWave), args, 0, s);
         if (err == hipSuccess) err = hipLaunchKernel((void *)eb_route_place, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
     }
@@ -410,13 +617,13 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
 
 extern "C" {
 
-int eb_route_experts_workspace(int64_t N, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes)
+int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes)
 {
-    if (!bytes || N < 0 || K < 1 || shard_lo < 0 || shard_hi < shard_lo || shard_hi > kMostExperts ||
-        N > (int64_t)std::numeric_limits<int32_t>::max())
+    if (!bytes || N < 0 || K < 1 || K > E || shard_lo < 0 || shard_hi < shard_lo || shard_hi > E)
         return fail(EB_ERR_INVALID, "eb_route_experts_workspace: NULL bytes or a bad size");
-    const size_t n = workspace_of(N, shard_hi - shard_lo);
-    *bytes = n > 0 ? n : 1;
+    if (E > kMostExperts || N > (int64_t)std::numeric_limits<int32_t>::max() / K)
+        return fail(EB_ERR_UNSUPPORTED, "eb_route_experts_workspace: more than 1024 experts or 2^31 - 1 pairs");
+    *bytes = workspace_of(N, E, K, shard_hi - shard_lo);
     return EB_OK;
 }
 

@@ -13,6 +13,7 @@ vectors, joined per token by a weighted pooled lookup (``EmbeddingBagTables``).
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple
 
 from . import eb
@@ -33,7 +34,7 @@ def library() -> ctypes.CDLL:
     if _lib is None:
         lib = eb.library()
         p, i32, i64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-        lib.eb_route_experts_workspace.argtypes = [i64, i32, i32, i32, ctypes.POINTER(size)]
+        lib.eb_route_experts_workspace.argtypes = [i64, i32, i32, i32, i32, ctypes.POINTER(size)]
         lib.eb_route_experts_workspace.restype = ctypes.c_int
         lib.eb_route_experts.argtypes = [i64, i32, i32, p, i32, i64, p, i32, i32, i32, ctypes.c_float, i32, i32, p, p, p, p, p,
                                          p, size, p]
@@ -46,9 +47,9 @@ def library() -> ctypes.CDLL:
     return _lib
 
 
-def eb_route_experts_workspace(N: int, K: int, shard_lo: int, shard_hi: int) -> int:
+def eb_route_experts_workspace(N: int, E: int, K: int, shard_lo: int, shard_hi: int) -> int:
     n = ctypes.c_size_t()
-    _check(library().eb_route_experts_workspace(N, K, shard_lo, shard_hi, ctypes.byref(n)))
+    _check(library().eb_route_experts_workspace(N, E, K, shard_lo, shard_hi, ctypes.byref(n)))
     return n.value
 
 
@@ -94,19 +95,12 @@ def _code(dtype, fp8: bool = False) -> int:
     return code
 
 
-def _maker(x, stream):
-    """empty(shape, dtype) on x's device, from ``stream``'s memory where one is
-    given: what the caching allocator hands out again is then ordered with it."""
+def _on(stream):
+    """Allocations made under it are ``stream``'s, where one is given: what the
+    caching allocator hands out again is then ordered with it."""
     import torch
 
-    if stream is None:
-        return lambda shape, dtype: x.new_empty(shape, dtype=dtype)
-
-    def empty(shape, dtype):
-        with torch.cuda.stream(stream):
-            return x.new_empty(shape, dtype=dtype)
-
-    return empty
+    return torch.cuda.stream(stream)
 
 
 def _blocks(n: int) -> int:
@@ -139,32 +133,45 @@ def route(scores, top: int, mode: int = EB_SOFTMAX | EB_RENORMALIZE, bias=None, 
     or None.  ``grouped=False`` gives ids and weights only."""
     import torch
 
+    if stream is not None:
+        with _on(stream):
+            return _route(torch, scores, top, mode, bias, groups, top_groups, scale, shard_lo, shard_hi, grouped, stream)
+    return _route(torch, scores, top, mode, bias, groups, top_groups, scale, shard_lo, shard_hi, grouped, None)
+
+
+def _route(torch, scores, top, mode, bias, groups, top_groups, scale, lo, hi, grouped, stream):
     if scores.dim() != 2 or not scores.is_cuda:
         raise ValueError("scores must be a 2-D device tensor")
     N, E = scores.shape
-    dtype, ld, dev = _code(scores.dtype), _pitch(scores, "scores"), scores.device
-    if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != E):
-        raise ValueError("bias must be contiguous fp32 [E]")
-    _same_device(dev, bias)
-    hi = E if shard_hi is None else int(shard_hi)
-    empty = _maker(scores, stream)
-    ids = empty((N, top), torch.int32)
-    weights = empty((N, top), torch.float32)
+    dtype, ld, dev, bias_ptr = _code(scores.dtype), _pitch(scores, "scores"), scores.device, None
+    if bias is not None:
+        if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != E:
+            raise ValueError("bias must be contiguous fp32 [E]")
+        _same_device(dev, bias)
+        bias_ptr = bias.data_ptr()
+    hi = E if hi is None else int(hi)
+    lib = _lib or library()
+    nbytes = _route_workspace(N, E, top, lo, hi) if grouped else 0
+    ids = scores.new_empty((N, top), dtype=torch.int32)
+    weights = torch.empty_like(ids, dtype=torch.float32)
     offsets = tokens = slots = ws = None
-    nbytes = 0
     if grouped:
-        nbytes = eb_route_experts_workspace(N, top, shard_lo, hi)
-        offsets = empty((hi - shard_lo + 1,), torch.int32)
-        tokens = empty((N * top,), torch.int32)
-        slots = empty((N, top), torch.int32)
-        ws = empty((nbytes,), torch.uint8)
-    _check(library().eb_route_experts(
-        N, E, top, scores.data_ptr() or None, dtype, ld, bias.data_ptr() if bias is not None else None, mode, groups,
-        top_groups, scale, shard_lo, hi, ids.data_ptr() or None, weights.data_ptr() or None,
-        offsets.data_ptr() if grouped else None, (tokens.data_ptr() or None) if grouped else None,
-        (slots.data_ptr() or None) if grouped else None, ws.data_ptr() if grouped else None, nbytes,
-        _stream_ptr(stream, dev) or None))
+        offsets = ids.new_empty((hi - lo + 1,))
+        tokens = ids.new_empty((N * top,))
+        slots = torch.empty_like(ids)
+        ws = ids.new_empty((nbytes // 4,)) if nbytes else None
+    rc = lib.eb_route_experts(
+        N, E, top, scores.data_ptr(), dtype, ld, bias_ptr, mode, groups, top_groups, scale, lo, hi, ids.data_ptr(),
+        weights.data_ptr(), offsets.data_ptr() if grouped else None, tokens.data_ptr() if grouped else None,
+        slots.data_ptr() if grouped else None, ws.data_ptr() if nbytes else None, nbytes, _stream_ptr(stream, dev))
+    if rc:
+        _check(rc)
     return Route(ids, weights, offsets, tokens, slots)
+
+
+@functools.lru_cache(maxsize=256)
+def _route_workspace(N, E, top, lo, hi):
+    return eb_route_experts_workspace(N, E, top, lo, hi)
 
 
 def quantize_fp8(x, block_rows: int = 1, stream=None):
@@ -176,28 +183,40 @@ def quantize_fp8(x, block_rows: int = 1, stream=None):
     of one column of blocks side by side in memory."""
     import torch
 
-    if x.dim() not in (2, 3) or not x.is_cuda:
+    if stream is not None:
+        with _on(stream):
+            return _quantize(torch, x, block_rows, stream)
+    return _quantize(torch, x, block_rows, None)
+
+
+def _quantize(torch, x, block_rows, stream):
+    dim = x.dim()
+    if dim not in (2, 3) or not x.is_cuda:
         raise ValueError("x must be a 2-D or 3-D device tensor")
-    m, (rows, cols) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
-    flat = x if x.dim() == 2 else (x[0] if m else x.reshape(0, cols))
-    dtype, ldx = _code(x.dtype), _pitch(flat, "x")
-    if m > 1 and rows == 1:
-        ldx = x.stride(0)
-    elif m > 1 and x.stride(0) != rows * ldx:
-        raise ValueError("x's matrices must be stacked row after row")
-    empty = _maker(x, stream)
-    pitch = -(-cols // 16) * 16
-    q = empty((m, rows, pitch), torch.float8_e4m3fn)[:, :, :cols]
-    if block_rows == 1:
-        scales = empty((_blocks(cols), m * rows), torch.float32)
-        lds, shaped = m * rows, scales.t()
-        shaped = shaped.view(m, rows, -1) if x.dim() == 3 else shaped
+    if dim == 2:
+        (rows, cols), m, ldx = x.shape, 1, _pitch(x, "x")
     else:
-        scales = empty((m, _blocks(rows), _blocks(cols)), torch.float32)
-        lds, shaped = 0, scales if x.dim() == 3 else scales[0]
-    _check(library().eb_quantize_fp8(m, rows, cols, x.data_ptr() or None, dtype, ldx, block_rows, q.data_ptr() or None, pitch,
-                                     scales.data_ptr() or None, lds, _stream_ptr(stream, x.device) or None))
-    return (q if x.dim() == 3 else q[0]), shaped
+        m, rows, cols = x.shape
+        ldx = _pitch(x[0], "x") if m else cols
+        if m > 1 and rows == 1:
+            ldx = x.stride(0)
+        elif m > 1 and x.stride(0) != rows * ldx:
+            raise ValueError("x's matrices must be stacked row after row")
+    dtype, pitch, blocks = _code(x.dtype), (cols + 15) & -16, (cols + BLOCK - 1) // BLOCK
+    q = x.new_empty((rows, pitch) if dim == 2 else (m, rows, pitch), dtype=torch.float8_e4m3fn)
+    if block_rows == 1:
+        scales = x.new_empty((blocks, m * rows), dtype=torch.float32)
+        lds, shaped = m * rows, scales.t()
+        if dim == 3:
+            shaped = shaped.view(m, rows, blocks)
+    else:
+        scales = x.new_empty((m, _blocks(rows), blocks), dtype=torch.float32)
+        lds, shaped = 0, scales if dim == 3 else scales[0]
+    rc = (_lib or library()).eb_quantize_fp8(m, rows, cols, x.data_ptr(), dtype, ldx, block_rows, q.data_ptr(), pitch,
+                                             scales.data_ptr(), lds, _stream_ptr(stream, x.device))
+    if rc:
+        _check(rc)
+    return (q if pitch == cols else q[..., :cols]), shaped
 
 
 def product(x, x_scales, w, w_scales, offsets=None, tokens=None, bias=None, act: int = EB_ACT_NONE, out_dtype=None,
@@ -214,57 +233,80 @@ def product(x, x_scales, w, w_scales, offsets=None, tokens=None, bias=None, act:
     written.  ``out``: the floating-point output, with unit column stride."""
     import torch
 
+    if stream is not None:
+        with _on(stream):
+            return _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dtype, out, stream)
+    return _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dtype, out, None)
+
+
+def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dtype, out, stream):
+    f8, f32, i32 = torch.float8_e4m3fn, torch.float32, torch.int32
     if x.dim() != 2 or w.dim() not in (2, 3) or not x.is_cuda:
         raise ValueError("x must be a 2-D device tensor, w 2-D or 3-D")
-    if x.dtype != torch.float8_e4m3fn or w.dtype != torch.float8_e4m3fn:
+    if x.dtype != f8 or w.dtype != f8:
         raise ValueError("x and w must be float8_e4m3fn")
-    dev, (rows, K), (N, wk) = x.device, x.shape, w.shape[-2:]
-    E = w.shape[0] if w.dim() == 3 else 1
-    if wk != K or E == 0:
-        raise ValueError("w must be [N, K] or [E, N, K], E at least 1")
-    ldw = _pitch(w if w.dim() == 2 else w[0], "w")
-    if E > 1 and N == 1:
-        ldw = w.stride(0)
-    elif E > 1 and w.stride(0) != N * ldw:
-        raise ValueError("w's matrices must be stacked row after row")
-    ldx, kb = _pitch(x, "x"), _blocks(K)
+    dev, (rows, K) = x.device, x.shape
+    if w.dim() == 2:
+        (N, wk), E, ldw = w.shape, 1, _pitch(w, "w")
+    else:
+        E, N, wk = w.shape
+        if E == 0:
+            raise ValueError("w must hold an expert")
+        ldw = _pitch(w[0], "w")
+        if E > 1 and N == 1:
+            ldw = w.stride(0)
+        elif E > 1 and w.stride(0) != N * ldw:
+            raise ValueError("w's matrices must be stacked row after row")
+    if wk != K:
+        raise ValueError("w must be [N, K] or [E, N, K]")
+    ldx, kb = _pitch(x, "x"), (K + BLOCK - 1) // BLOCK
     gate = act == EB_ACT_SILU_GATE
     width = N // 2 if gate else N
-    if x_scales.dtype != torch.float32 or tuple(x_scales.shape) != (rows, kb):
+    blocks = (width + BLOCK - 1) // BLOCK
+    if x_scales.dtype != f32 or x_scales.shape != (rows, kb):
         raise ValueError("x_scales must be fp32 [rows, ceil(K/128)]")
-    if rows > 1 and x_scales.stride(0) != 1 or kb > 1 and x_scales.stride(1) < rows:
+    by_row, by_block = x_scales.stride()
+    if rows > 1 and by_row != 1 or kb > 1 and by_block < rows:
         x_scales = x_scales.t().contiguous().t()
-    ldxs = x_scales.stride(1) if kb > 1 else rows
-    if w_scales.dtype != torch.float32 or not w_scales.is_contiguous() or \
-            w_scales.numel() != E * (2 if gate else 1) * _blocks(width) * kb:
+        by_block = rows
+    ldxs = by_block if kb > 1 else rows
+    if w_scales.dtype != f32 or not w_scales.is_contiguous() or w_scales.numel() != (2 if gate else 1) * E * blocks * kb:
         raise ValueError("w_scales must be contiguous fp32, a scale per 128 x 128 of w")
-    if offsets is not None and (offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.numel() != E + 1):
-        raise ValueError("offsets must be contiguous int32 [E + 1]")
-    if tokens is not None and (tokens.dtype != torch.int32 or not tokens.is_contiguous()):
-        raise ValueError("tokens must be contiguous int32")
-    if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != E * N):
-        raise ValueError("bias must be contiguous fp32 [E, N]")
+    M, offsets_ptr, tokens_ptr, bias_ptr = rows, None, None, None
+    if offsets is not None:
+        if offsets.dtype != i32 or not offsets.is_contiguous() or offsets.numel() != E + 1:
+            raise ValueError("offsets must be contiguous int32 [E + 1]")
+        offsets_ptr = offsets.data_ptr()
+    if tokens is not None:
+        if tokens.dtype != i32 or not tokens.is_contiguous():
+            raise ValueError("tokens must be contiguous int32")
+        M, tokens_ptr = tokens.numel(), tokens.data_ptr()
+    if bias is not None:
+        if bias.dtype != f32 or not bias.is_contiguous() or bias.numel() != E * N:
+            raise ValueError("bias must be contiguous fp32 [E, N]")
+        bias_ptr = bias.data_ptr()
     _same_device(dev, x_scales, w, w_scales, offsets, tokens, bias, out)
-    M = rows if tokens is None else tokens.numel()
-    out_dtype = out.dtype if out is not None else torch.bfloat16 if out_dtype is None else out_dtype
-    code = _code(out_dtype, fp8=True)
-    empty, scales = _maker(x, stream), None
+    scales_ptr, scales = None, None
+    code = _code(out.dtype if out is not None else torch.bfloat16 if out_dtype is None else out_dtype, fp8=True)
     if code == EB_FP8:
         if out is not None:
             raise ValueError("out is for floating-point outputs")
-        ldo = -(-width // 16) * 16
-        out = empty((M, ldo), out_dtype)[:, :width]
-        scales = empty((_blocks(width), M), torch.float32)
+        ldo = (width + 15) & -16
+        out = x.new_empty((M, ldo))
+        scales = x.new_empty((blocks, M), dtype=f32)
+        scales_ptr = scales.data_ptr()
+    elif out is None:
+        ldo = width
+        out = x.new_empty((M, width), dtype=torch.bfloat16 if out_dtype is None else out_dtype)
     else:
-        if out is None:
-            out = empty((M, width), out_dtype)
-        elif tuple(out.shape) != (M, width):
+        if out.shape != (M, width):
             raise ValueError("out must be [slots, width]")
         ldo = _pitch(out, "out")
-    _check(library().eb_expert_product(
-        M, E, N, K, x.data_ptr() or None, ldx, rows, x_scales.data_ptr() or None, ldxs,
-        (tokens.data_ptr() or None) if tokens is not None else None, w.data_ptr() or None, ldw, w_scales.data_ptr() or None,
-        offsets.data_ptr() if offsets is not None else None, bias.data_ptr() if bias is not None else None, act, code,
-        out.data_ptr() or None, ldo, scales.data_ptr() or None if scales is not None else None, M,
-        _stream_ptr(stream, dev) or None))
-    return (out, scales.t()) if code == EB_FP8 else out
+    rc = (_lib or library()).eb_expert_product(
+        M, E, N, K, x.data_ptr(), ldx, rows, x_scales.data_ptr(), ldxs, tokens_ptr, w.data_ptr(), ldw, w_scales.data_ptr(),
+        offsets_ptr, bias_ptr, act, code, out.data_ptr(), ldo, scales_ptr, M, _stream_ptr(stream, dev))
+    if rc:
+        _check(rc)
+    if code == EB_FP8:
+        return (out if ldo == width else out[:, :width]), scales.t()
+    return out
