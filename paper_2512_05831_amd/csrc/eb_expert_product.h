@@ -307,6 +307,6 @@ struct KernelPlan {
 };
 
 KernelPlan stream_kernel(int32_t tokens, bool gate, bool fp8);
-KernelPlan tile_kernel(bool gate, int32_t out_type);
+KernelPlan tile_kernel(bool gate, int32_t out_type, bool large);
 
 } // namespace eb_product

@@ -85,7 +85,9 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     constexpr int64_t kMost32 = (int64_t)1 << 32;
     const bool reachable = N * ldw < kMost32 && (tokens ? x_rows : 256) * ldx < kMost32 && x_rows > 0;
     const bool tiles = reachable && mean > 64;
-    const KernelPlan plan = tiles ? tile_kernel(gate, out_type) : stream_kernel((int32_t)mean, gate, fp8);
+    KernelPlan plan = tiles ? tile_kernel(gate, out_type, true) : stream_kernel((int32_t)mean, gate, fp8);
+    // Large tiles where they give every compute unit a workgroup.
+    if (tiles && (M + plan.height - 1) / plan.height * ((width + plan.columns - 1) / plan.columns) < 256) plan = tile_kernel(gate, out_type, false);
     a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
     // At most one tile per expert is not full.
     const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);

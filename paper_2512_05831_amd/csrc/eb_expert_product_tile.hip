@@ -4,15 +4,26 @@
 
 namespace eb_product {
 
+namespace {
+
+template <bool kWide, bool kFp8>
+KernelPlan plan_of(bool gate, bool large)
+{
+    if (large) return gate ? tile_plan<TileShape<8, 4, 2, 4, kWide, true, kFp8>>() : tile_plan<TileShape<8, 4, 2, 4, kWide, false, kFp8>>();
+    if (!gate) return tile_plan<TileShape<4, 4, 2, 2, kWide, false, kFp8>>();
+    // 8-bit outputs need their 128 columns in the workgroup.
+    if constexpr (kFp8) return tile_plan<TileShape<4, 4, 1, 4, kWide, true, kFp8>>();
+    else return tile_plan<TileShape<4, 4, 2, 2, kWide, true, kFp8>>();
+}
+
+} // namespace
+
 // 16-bit outputs: the 8-bit matrix unit.  fp32 and 8-bit outputs (whose scales
 // are fp32): the 16-bit unit, exact.
-KernelPlan tile_kernel(bool gate, int32_t out_type)
+KernelPlan tile_kernel(bool gate, int32_t out_type, bool large)
 {
-    const bool fp8 = out_type == EB_FP8;
-    if (out_type == EB_F16 || out_type == EB_BF16)
-        return gate ? tile_plan<TileShape<8, 4, 2, 4, false, true, false>>() : tile_plan<TileShape<8, 4, 2, 4, false, false, false>>();
-    if (gate) return fp8 ? tile_plan<TileShape<4, 4, 2, 4, true, true, true>>() : tile_plan<TileShape<4, 4, 2, 4, true, true, false>>();
-    return fp8 ? tile_plan<TileShape<4, 4, 2, 4, true, false, true>>() : tile_plan<TileShape<4, 4, 2, 4, true, false, false>>();
+    if (out_type == EB_F16 || out_type == EB_BF16) return plan_of<false, false>(gate, large);
+    return out_type == EB_FP8 ? plan_of<true, true>(gate, large) : plan_of<true, false>(gate, large);
 }
 
 } // namespace eb_product

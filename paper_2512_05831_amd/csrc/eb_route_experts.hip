@@ -15,17 +15,20 @@
 //         lowest expert that has it, out with it" are 680 (16 values a lane).
 //         Those rounds are taken where more than 16 values reach the bound, and
 //         for other K and L.  Each workgroup counts its pairs per expert.
-// scan    exclusive prefix of the counts over the chunks of kTokens tokens.
+// scan    exclusive prefix of each expert's counts over the chunks of kTokens
+//         tokens.
 // place   each workgroup ranks its pairs within their experts (in pair order:
 //         the lanes of a wave that hold the same expert find each other by
 //         ballots over the expert's bits) and writes them.
-// Up to kFewTokens tokens and kFewPairs pairs one workgroup does all of it in
-// one launch, the pairs and counts in LDS.
+// A launch costs more than the work of a small batch, so up to kFewTokens
+// tokens one workgroup does all of it, and up to kFewPairs pairs one workgroup
+// scans and places after choose.
 
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
 
+#include <algorithm>
 #include <limits>
 
 #include "../../include/eb.h"
@@ -40,9 +43,11 @@ using eb_detail::fail;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
+constexpr int kChooseThreads = 512; // 32 tokens of 16 lanes
 constexpr int kTokens = 32;        // tokens of a chunk
 constexpr int kFewWaves = 16;      // of the workgroup that does all
-constexpr int kFewTokens = 256, kFewPairs = 2048;
+constexpr int kFewTokens = 64, kFewPairs = 4096, kFewExperts = 512;
+constexpr int kMostFewPairs = kFewTokens * 64;
 constexpr int kFilterTop = 8;      // most experts per token for the filter
 constexpr int kMostExperts = 1024;
 constexpr int kMostTop = 64;
@@ -65,7 +70,7 @@ struct RouteArgs {
     int32_t *ids;
     float *weights;
     int32_t *offsets, *tokens, *slots;
-    uint32_t *counts; // [chunks][held], then [held] totals
+    uint32_t *counts; // [held][chunks + 1], the total last, or NULL: none are taken
     int64_t chunks;
 };
 
@@ -88,9 +93,8 @@ __device__ __forceinline__ float exp_of(float v)
     return h > -126.f ? fmaf(e, l * 0.693147181f, e) : 0.f;
 }
 
-struct Candidate {
-    int key, expert;
-};
+// A key and its expert as one integer: of equal keys the lower expert is larger.
+__device__ __forceinline__ int64_t candidate(int key, int expert) { return (int64_t)key << 32 | (0x7FFFFFFF - expert); }
 
 // What a lane group has in LDS for one token.
 template <int L, int V>
@@ -101,8 +105,8 @@ struct TokenSpace {
             int group_key[kMostGroups];
         };
         struct {
-            Candidate found[16 + L]; // from 16 on: what is not wanted
-            Candidate best[16];
+            int64_t found[16 + L]; // from 16 on: what is not wanted
+            int64_t best[16];
         };
     };
 };
@@ -153,25 +157,27 @@ __device__ __forceinline__ void best_by_filter(int (&key)[V], int lane, int K, T
     upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xF, 0xF, false);
     const int n = max_lanes<16>(upto);
     if (__any(n > 16)) return best_by_rounds<16, V>(key, lane, K, id, id_key);
+    const int64_t none = candidate(kNoneKey, 0x7FFFFFFF);
+    space.found[lane] = none;
+    wave_fence();
     int at = upto - mine;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const bool wanted = key[v] >= bound;
-        space.found[wanted ? at : 16 + lane] = {key[v], v * 16 + lane};
+        space.found[wanted ? at : 16 + lane] = candidate(key[v], v * 16 + lane);
         at += wanted;
     }
     wave_fence();
-    const Candidate own = lane < n ? space.found[lane] : Candidate{kNoneKey, 0x7FFFFFFF};
+    const int64_t own = space.found[lane];
     int rank = 0;
-    for (int j = 0; j < n; ++j) {
-        const Candidate o = space.found[j];
-        rank += o.key > own.key || (o.key == own.key && o.expert < own.expert);
-    }
-    if (lane < n) space.best[rank] = own;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) rank += space.found[j] > own;
+    if (own != none) space.best[rank] = own;
     wave_fence();
     if (lane < min(n, K)) {
-        id = space.best[lane].expert;
-        id_key = space.best[lane].key;
+        const int64_t c = space.best[lane];
+        id = 0x7FFFFFFF - (int)c;
+        id_key = (int)(c >> 32);
     }
     wave_fence(); // the next token's values come to the same LDS
 }
@@ -184,10 +190,18 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
     float x[V];
     int key[V];
     const bool scored = a.bias || a.pair; // the choice needs the scores themselves
+    T raw[V];
+    float bias[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw[v] = row[min(v * L + lane, a.E - 1)];
+    if (a.bias) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bias[v] = a.bias[min(v * L + lane, a.E - 1)];
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = v * L + lane;
-        float f = e < a.E ? widen(row[e]) : -kInf;
+        float f = e < a.E ? widen(raw[v]) : -kInf;
         f = f == f ? f : -kInf;
         x[v] = f < kInf ? f : __FLT_MAX__;
         key[v] = order_key(x[v]);
@@ -210,7 +224,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
         for (int v = 0; v < V; ++v) {
             const int e = v * L + lane;
             float s = a.sigmoid ? sigmoid(x[v]) : exp_of(x[v] - top_x) / total;
-            if (a.bias) s += e < a.E ? a.bias[e] : 0.f;
+            if (a.bias) s += bias[v];
             // A NaN bias makes its expert unfit, as a NaN score does.
             s = x[v] > -kInf && s == s ? s : -kInf;
             if (a.pair && e < a.E) space.judged[e + (e * a.group_magic >> 20)] = s;
@@ -228,6 +242,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
         wave_fence();
         for (int g = lane; g < a.groups; g += L) {
             float best = -kInf, next = -kInf;
+#pragma unroll 8
             for (int i = 0; i < a.group_size; ++i) {
                 const float s = space.judged[g * (a.group_size + 1) + i];
                 next = fmaxf(next, fminf(best, s));
@@ -240,6 +255,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
         for (int g = lane; g < a.groups; g += L) {
             const int k = space.group_key[g];
             int better = 0;
+#pragma unroll 8
             for (int h = 0; h < a.groups; ++h) {
                 const int o = space.group_key[h];
                 better += o > k || (o == k && h < g);
@@ -289,16 +305,15 @@ __device__ __forceinline__ int held_expert(const RouteArgs &a, int id)
 }
 
 template <int L, int V, typename T>
-__global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
+__global__ __launch_bounds__(kChooseThreads, L *V <= 512 ? 4 : 2) void eb_route_choose(RouteArgs a)
 {
-    constexpr int kPerWave = kWave / L;
-    constexpr int kPass = kWaves * kPerWave; // tokens a workgroup takes at a time
+    constexpr int kPass = kChooseThreads / L; // tokens a workgroup takes at a time
     __shared__ uint32_t count[kMostExperts];
     __shared__ TokenSpace<L, V> space[kPass];
 
     const int lane = threadIdx.x % L, mine = threadIdx.x / L; // token of a pass
-    if (a.offsets) {
-        for (int j = threadIdx.x; j < a.held; j += kThreads) count[j] = 0;
+    if (a.counts) {
+        for (int j = threadIdx.x; j < a.held; j += kChooseThreads) count[j] = 0;
         __syncthreads();
     }
     for (int p = 0; p < kTokens; p += kPass) {
@@ -310,12 +325,12 @@ __global__ __launch_bounds__(kThreads) void eb_route_choose(RouteArgs a)
         if (lane < a.K) {
             a.ids[n * a.K + lane] = id;
             a.weights[n * a.K + lane] = w;
-            if (a.offsets && held_expert(a, id) >= 0) atomicAdd(&count[id - a.lo], 1u);
+            if (a.counts && held_expert(a, id) >= 0) atomicAdd(&count[id - a.lo], 1u);
         }
     }
-    if (!a.offsets) return;
+    if (!a.counts) return;
     __syncthreads();
-    for (int j = threadIdx.x; j < a.held; j += kThreads) a.counts[(int64_t)blockIdx.x * a.held + j] = count[j];
+    for (int j = threadIdx.x; j < a.held; j += kChooseThreads) a.counts[j * (a.chunks + 1) + blockIdx.x] = count[j];
 }
 
 // The lanes of a wave that hold the same expert j (those with j < 0: none).
@@ -340,19 +355,85 @@ __device__ __forceinline__ uint32_t prefix_in_wave(uint32_t v)
     return v;
 }
 
+// Scan and placing of few pairs by one workgroup of kFewWaves waves.
+// expert_of(p): the held expert of pair p, or -1.
+constexpr int kAllThreads = kFewWaves * kWave;
+
+struct PlaceSpace {
+    uint32_t next[kFewWaves][kMostExperts]; // counts, then the next slot, per wave and expert
+};
+
+template <typename ExpertOf>
+__device__ __forceinline__ void place_all(const RouteArgs &a, PlaceSpace &space, uint32_t (&wave_sum)[kFewWaves], ExpertOf expert_of)
+{
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    // A wave takes a run of the pairs.
+    const int pairs = (int)a.N * a.K, run = (pairs + kFewWaves - 1) / kFewWaves;
+    const int p0 = min(pairs, wave * run), p1 = min(pairs, p0 + run);
+    for (int j = lane; j < a.held; j += kWave) space.next[wave][j] = 0;
+    wave_fence();
+    for (int p = p0 + lane; p < p1; p += kWave) {
+        const int j = expert_of(p);
+        if (j >= 0) atomicAdd(&space.next[wave][j], 1u);
+    }
+    __syncthreads();
+    static_assert(kAllThreads >= kMostExperts, "a thread per expert");
+    const int j = threadIdx.x;
+    uint32_t sum = 0;
+    if (j < a.held) {
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) {
+            const uint32_t n = space.next[w][j];
+            space.next[w][j] = sum;
+            sum += n;
+        }
+    }
+    const uint32_t upto = prefix_in_wave(sum);
+    if (lane == kWave - 1) wave_sum[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+        before += w < wave ? wave_sum[w] : 0;
+        total += wave_sum[w];
+    }
+    if (j < a.held) {
+        a.offsets[j] = (int32_t)before;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) space.next[w][j] += before;
+    }
+    if (j == 0) a.offsets[a.held] = (int32_t)total;
+    __syncthreads();
+    const int bits = 32 - __clz(a.held | 1);
+    for (int q = p0; q < p1; q += kWave) {
+        const int p = q + lane;
+        const int e = p < p1 ? expert_of(p) : -1;
+        const uint64_t same = same_expert(e, bits);
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        uint32_t at = 0;
+        if (e >= 0) at = space.next[wave][e] + rank;
+        wave_fence();
+        if (e >= 0 && rank == 0) space.next[wave][e] += __popcll(same);
+        wave_fence();
+        if (p < p1) a.slots[p] = e >= 0 ? (int32_t)at : -1;
+        if (e >= 0) a.tokens[at] = p / a.K;
+        if (p < p1 && p >= (int)total) a.tokens[p] = -1; // past the last slot
+    }
+}
+
 // The whole of it for few tokens, in one workgroup.
 template <int L, int V, typename T>
-__global__ __launch_bounds__(kFewWaves *kWave) void eb_route_few(RouteArgs a)
+__global__ __launch_bounds__(kAllThreads) void eb_route_few(RouteArgs a)
 {
-    constexpr int kAll = kFewWaves * kWave, kPass = kAll / L;
+    constexpr int kPass = kAllThreads / L;
     __shared__ union {
         TokenSpace<L, V> token[kPass];
-        uint32_t next[kFewWaves][kMostExperts]; // counts, then the next slot, per wave and expert
+        PlaceSpace place;
     } space;
-    __shared__ int16_t expert_of[kFewPairs];
+    __shared__ int16_t expert_of[kMostFewPairs];
     __shared__ uint32_t wave_sum[kFewWaves];
 
-    const int wave = threadIdx.x / kWave, in_wave = threadIdx.x % kWave, lane = threadIdx.x % L;
+    const int lane = threadIdx.x % L;
     for (int p = threadIdx.x / L; p < a.N; p += kPass) {
         int id;
         float w;
@@ -365,84 +446,42 @@ __global__ __launch_bounds__(kFewWaves *kWave) void eb_route_few(RouteArgs a)
     }
     if (!a.offsets) return;
     __syncthreads();
-    // A wave takes a run of the pairs.
-    const int pairs = (int)a.N * a.K, run = (pairs + kFewWaves - 1) / kFewWaves;
-    const int p0 = min(pairs, wave * run), p1 = min(pairs, p0 + run);
-    for (int j = in_wave; j < a.held; j += kWave) space.next[wave][j] = 0;
-    wave_fence();
-    for (int p = p0 + in_wave; p < p1; p += kWave)
-        if (expert_of[p] >= 0) atomicAdd(&space.next[wave][expert_of[p]], 1u);
-    __syncthreads();
-    // kMostExperts threads: an expert each.
-    static_assert(kAll >= kMostExperts, "a thread per expert");
-    const int j = threadIdx.x;
-    uint32_t sum = 0;
-    if (j < a.held)
-        for (int w = 0; w < kFewWaves; ++w) {
-            const uint32_t n = space.next[w][j];
-            space.next[w][j] = sum;
-            sum += n;
-        }
-    const uint32_t upto = prefix_in_wave(sum);
-    if (in_wave == kWave - 1) wave_sum[wave] = upto;
-    __syncthreads();
-    uint32_t before = upto - sum, total = 0;
-    for (int w = 0; w < kFewWaves; ++w) {
-        before += w < wave ? wave_sum[w] : 0;
-        total += wave_sum[w];
-    }
-    if (j < a.held) {
-        a.offsets[j] = (int32_t)before;
-        for (int w = 0; w < kFewWaves; ++w) space.next[w][j] += before;
-    }
-    if (j == 0) a.offsets[a.held] = (int32_t)total;
-    __syncthreads();
-    const int bits = 32 - __clz(a.held | 1);
-    for (int q = p0; q < p1; q += kWave) {
-        const int p = q + in_wave;
-        const int e = p < p1 ? expert_of[p] : -1;
-        const uint64_t same = same_expert(e, bits);
-        const int rank = __popcll(same & ((1ull << in_wave) - 1));
-        uint32_t at = 0;
-        if (e >= 0) at = space.next[wave][e] + rank;
-        wave_fence();
-        if (e >= 0 && rank == 0) space.next[wave][e] += __popcll(same);
-        wave_fence();
-        if (p < p1) a.slots[p] = e >= 0 ? (int32_t)at : -1;
-        if (e >= 0) a.tokens[at] = p / a.K;
-        if (p < p1 && p >= (int)total) a.tokens[p] = -1; // past the last slot
-    }
+    place_all(a, space.place, wave_sum, [&](int p) { return (int)expert_of[p]; });
 }
 
-// counts[c][j] becomes the pairs of expert j in the chunks before c; the totals
-// follow the last chunk.  A workgroup takes 64 experts (a lane each), its waves
-// a run of chunks each.
-constexpr int kScanWaves = 16;
-
-__global__ __launch_bounds__(kScanWaves *kWave) void eb_route_scan(RouteArgs a)
+__global__ __launch_bounds__(kAllThreads) void eb_route_place_few(RouteArgs a)
 {
-    __shared__ uint32_t sum_of[kScanWaves][kWave];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int j = blockIdx.x * kWave + lane;
-    const int64_t run = (a.chunks + kScanWaves - 1) / kScanWaves;
-    const int64_t c0 = min(a.chunks, wave * run), c1 = min(a.chunks, c0 + run);
-    uint32_t sum = 0;
-    if (j < a.held)
-        for (int64_t c = c0; c < c1; ++c) sum += a.counts[c * a.held + j];
-    sum_of[wave][lane] = sum;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-    for (int w = 0; w < kScanWaves; ++w) {
-        before += w < wave ? sum_of[w][lane] : 0;
-        all += sum_of[w][lane];
-    }
+    __shared__ PlaceSpace space;
+    __shared__ uint32_t wave_sum[kFewWaves];
+    place_all(a, space, wave_sum, [&](int p) { return held_expert(a, a.ids[p]); });
+}
+
+// counts[j][c] becomes the pairs of expert j in the chunks before c, the total
+// last: a wave per expert.
+__global__ __launch_bounds__(kThreads) void eb_route_scan(RouteArgs a)
+{
+    const int lane = threadIdx.x % kWave;
+    const int j = blockIdx.x * kWaves + threadIdx.x / kWave;
     if (j >= a.held) return;
-    for (int64_t c = c0; c < c1; ++c) {
-        const uint32_t n = a.counts[c * a.held + j];
-        a.counts[c * a.held + j] = before;
-        before += n;
+    uint32_t *row = a.counts + j * (a.chunks + 1);
+    uint32_t before = 0;
+    constexpr int kEach = 8; // loads under way
+    for (int64_t c0 = 0; c0 < a.chunks; c0 += kEach * kWave) {
+        uint32_t n[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int64_t c = c0 + i * kWave + lane;
+            n[i] = c < a.chunks ? row[c] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int64_t c = c0 + i * kWave + lane;
+            const uint32_t upto = prefix_in_wave(n[i]);
+            if (c < a.chunks) row[c] = before + upto - n[i];
+            before += __shfl(upto, kWave - 1);
+        }
     }
-    if (wave == 0) a.counts[a.chunks * a.held + j] = all;
+    if (lane == 0) row[a.chunks] = before;
 }
 
 __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
@@ -464,11 +503,11 @@ __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
     __syncthreads();
     // Slots of the experts before mine: an exclusive prefix over the totals,
     // kThreads experts at a time.
-    const uint32_t *total = a.counts + a.chunks * a.held;
     uint32_t base = 0;
     for (int j0 = 0; j0 < a.held; j0 += kThreads) {
         const int j = j0 + threadIdx.x;
-        const uint32_t mine = j < a.held ? total[j] : 0;
+        const uint32_t *row = a.counts + j * (a.chunks + 1);
+        const uint32_t mine = j < a.held ? row[a.chunks] : 0;
         const uint32_t sum = prefix_in_wave(mine);
         if (lane == kWave - 1) wave_sum[wave] = sum;
         __syncthreads();
@@ -477,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void eb_route_place(RouteArgs a)
         for (int w = 0; w < kWaves; ++w) base += wave_sum[w];
         if (j < a.held) {
             if (blockIdx.x == 0) a.offsets[j] = (int32_t)before;
-            uint32_t at = before + a.counts[(int64_t)blockIdx.x * a.held + j];
+            uint32_t at = before + row[blockIdx.x];
             for (int w = 0; w < kWaves; ++w) {
                 const uint32_t n = next[w][j];
                 next[w][j] = at;
@@ -509,38 +548,37 @@ __global__ void eb_route_none(int32_t *offsets, int32_t n)
     for (int j = threadIdx.x; j < n; j += blockDim.x) offsets[j] = 0;
 }
 
-template <int L, int V, typename T>
-void *kernel_of(bool few)
+// Few tokens: a wave each, for its latency; up to kFewExperts, whose values 16
+// waves' registers hold.
+template <typename T>
+void *few_kernel(int32_t E)
 {
-    return few ? (void *)eb_route_few<L, V, T> : (void *)eb_route_choose<L, V, T>;
+    if (E <= 64) return (void *)eb_route_few<64, 1, T>;
+    if (E <= 128) return (void *)eb_route_few<64, 2, T>;
+    if (E <= 256) return (void *)eb_route_few<64, 4, T>;
+    return (void *)eb_route_few<64, 8, T>;
 }
 
 template <typename T>
 void *choose_kernel(bool few, int32_t E, int32_t K)
 {
+    if (few) return few_kernel<T>(E);
     if (K <= 16 && E <= 256) {
-        if (E <= 32) return kernel_of<16, 2, T>(few);
-        if (E <= 64) return kernel_of<16, 4, T>(few);
-        if (E <= 128) return kernel_of<16, 8, T>(few);
-        return kernel_of<16, 16, T>(few);
+        if (E <= 32) return (void *)eb_route_choose<16, 2, T>;
+        if (E <= 64) return (void *)eb_route_choose<16, 4, T>;
+        if (E <= 128) return (void *)eb_route_choose<16, 8, T>;
+        return (void *)eb_route_choose<16, 16, T>;
     }
-    if (E <= 256) return kernel_of<64, 4, T>(few);
-    if (E <= 512) return kernel_of<64, 8, T>(few);
-    return kernel_of<64, 16, T>(few);
-}
-
-// Whether one workgroup does all: it takes kPass = 64 tokens at a time (16 with 64 lanes each).
-bool few_tokens(int64_t N, int32_t E, int32_t K)
-{
-    const bool wide = K > 16 || E > 256;
-    return N <= (wide ? kFewTokens / 4 : kFewTokens) && N * K <= kFewPairs;
+    if (E <= 256) return (void *)eb_route_choose<64, 4, T>;
+    if (E <= 512) return (void *)eb_route_choose<64, 8, T>;
+    return (void *)eb_route_choose<64, 16, T>;
 }
 
 int64_t chunks_of(int64_t N) { return (N + kTokens - 1) / kTokens; }
 
-size_t workspace_of(int64_t N, int32_t E, int32_t K, int32_t held)
+size_t workspace_of(int64_t N, int32_t K, int32_t held)
 {
-    return few_tokens(N, E, K) ? 0 : (size_t)(chunks_of(N) + 1) * (size_t)held * 4;
+    return N * K <= kFewPairs ? 0 : (size_t)(chunks_of(N) + 1) * (size_t)std::max(held, 1) * 4;
 }
 
 int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *scores, int32_t dtype, int64_t ld,
@@ -565,7 +603,7 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     if (N > 0 && (!scores || !ids || !weights)) return fail(EB_ERR_INVALID, "%s: NULL scores, ids or weights", who);
     if (N > 0 && offsets && (!tokens || !slots)) return fail(EB_ERR_INVALID, "%s: NULL tokens or slots", who);
     const int32_t held = shard_hi - shard_lo;
-    const size_t needed = offsets ? workspace_of(N, E, K, held) : 0;
+    const size_t needed = offsets ? workspace_of(N, K, held) : 0;
     if (needed > 0 && (!workspace || workspace_bytes < needed || (uintptr_t)workspace % 4))
         return fail(EB_ERR_INVALID, "%s: workspace missing, too small or misaligned", who);
 
@@ -598,16 +636,22 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     a.offsets = offsets;
     a.tokens = tokens;
     a.slots = slots;
-    a.counts = (uint32_t *)workspace;
+    a.counts = needed > 0 ? (uint32_t *)workspace : nullptr;
     a.chunks = chunks_of(N);
-    const bool few = few_tokens(N, E, K);
+    const bool few = N <= kFewTokens && E <= kFewExperts;
     void *kernel = dtype == EB_F32 ? choose_kernel<float>(few, E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(few, E, K) : choose_kernel<Bf16>(few, E, K);
     void *args[] = {&a};
-    hipError_t err = few ? hipLaunchKernel(kernel, dim3(1), dim3(kFewWaves * kWave), args, 0, s)
-                         : hipLaunchKernel(kernel, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
+    auto launch = [&](void *f, int64_t grid, int threads) {
+        return hipLaunchKernel(f, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, s);
+    };
+    hipError_t err = few ? launch(kernel, 1, kAllThreads) : launch(kernel, a.chunks, kChooseThreads);
     if (err == hipSuccess && offsets && !few) {
-        if (held > 0) err = hipLaunchKernel((void *)eb_route_scan, dim3((unsigned)((held + kWave - 1) / kWave)), dim3(kScanWaves * kWave), args, 0, s);
-        if (err == hipSuccess) err = hipLaunchKernel((void *)eb_route_place, dim3((unsigned)a.chunks), dim3(kThreads), args, 0, s);
+        if (!a.counts) {
+            err = launch((void *)eb_route_place_few, 1, kAllThreads);
+        } else {
+            if (held > 0) err = launch((void *)eb_route_scan, (held + kWaves - 1) / kWaves, kThreads);
+            if (err == hipSuccess) err = launch((void *)eb_route_place, a.chunks, kThreads);
+        }
     }
     if (err != hipSuccess) return fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
     return EB_OK;
@@ -623,7 +667,7 @@ int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo
         return fail(EB_ERR_INVALID, "eb_route_experts_workspace: NULL bytes or a bad size");
     if (E > kMostExperts || N > (int64_t)std::numeric_limits<int32_t>::max() / K)
         return fail(EB_ERR_UNSUPPORTED, "eb_route_experts_workspace: more than 1024 experts or 2^31 - 1 pairs");
-    *bytes = workspace_of(N, E, K, shard_hi - shard_lo);
+    *bytes = workspace_of(N, K, shard_hi - shard_lo);
     return EB_OK;
 }
 

@@ -109,11 +109,13 @@ def _blocks(n: int) -> int:
 
 def _pitch(t, what: str) -> int:
     """Elements between the rows of a 2-D tensor of unit column stride."""
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    (rows, cols), (ld, unit) = t.shape, t.stride()
+    if unit != 1 and cols > 1:
         raise ValueError(f"{what} must have unit column stride")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    if ld < t.shape[1]:
-        raise ValueError(f"{what} must have rows that do not overlap")
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{what} must have rows that do not overlap")
+        return cols
     return ld
 
 
