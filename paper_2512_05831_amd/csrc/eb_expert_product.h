@@ -183,14 +183,12 @@ __device__ __forceinline__ f32x4 bias4(const float *bias, int32_t row, int32_t e
     return b;
 }
 
-// g / (1 + exp(-g)).  exp(-g) = 2^h (1 + l ln 2) with h + l = -g log2(e) in
-// twice fp32's precision; the hardware's 2^h and reciprocal are within an ulp.
+// g / (1 + exp(-g)).  The hardware's 2^x and reciprocal are within an ulp, and
+// the exponent's rounding adds |g| ulps to exp(-g): a few ulps where it counts
+// beside the 1, and far less than an ulp of g of what is left for large -g.
 __device__ __forceinline__ float silu(float g)
 {
-    const float h = g * -1.44269502f, l = fmaf(g, -1.44269502f, -h) + g * -1.92596303e-8f;
-    float e = __builtin_amdgcn_exp2f(h);
-    e = fabsf(h) < 126.f ? fmaf(e, l * 0.693147181f, e) : e; // past it e or 1 does not count
-    return g * __builtin_amdgcn_rcpf(1.f + e);
+    return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269502f));
 }
 
 // The sums of kRows x kTokens tiles (weight rows of one wave) to outputs: bias,
@@ -252,18 +250,17 @@ __device__ __forceinline__ void store_floats(const ProductArgs &a, int32_t colum
 
 // The largest magnitude of this wave's outputs for each of its tokens into
 // `most` (LDS, one word per token of the workgroup's tile and output block,
-// zero before).
+// zero before).  Columns past the width repeat the last one.
 template <int kOut, int kRows, int kTokens>
-__device__ __forceinline__ void most_of_outputs(const ProductArgs &a, int32_t column, const f32x4 (&s)[kRows][kTokens], int *most)
+__device__ __forceinline__ void most_of_outputs(const f32x4 (&s)[kRows][kTokens], int *most)
 {
-    const int part = threadIdx.x % kWave / 16 * 4;
 #pragma unroll
     for (int t = 0; t < kTokens; ++t) {
         int m = 0;
 #pragma unroll
         for (int r = 0; r < kOut; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m = max(m, column + r * 16 + part + i < a.width ? magnitude(s[r][t][i]) : 0);
+            for (int i = 0; i < 4; ++i) m = max(m, magnitude(s[r][t][i]));
         auto p = __builtin_amdgcn_permlane16_swap((unsigned)m, (unsigned)m, false, false);
         m = max((int)p[0], (int)p[1]);
         auto q = __builtin_amdgcn_permlane32_swap((unsigned)m, (unsigned)m, false, false);
@@ -306,7 +303,10 @@ struct KernelPlan {
     int32_t band;    // the grid holds a multiple of so many slot tiles
 };
 
-KernelPlan stream_kernel(int32_t tokens, bool gate, bool fp8);
-KernelPlan tile_kernel(bool gate, int32_t out_type, bool large);
+// Slots and weight rows of a workgroup: 256 x 256, 128 x 256, 32 x 256.
+enum class TileSize { kLarge, kMedium, kSmall };
+
+KernelPlan stream_kernel(bool gate, bool fp8);
+KernelPlan tile_kernel(bool gate, int32_t out_type, TileSize size);
 
 } // namespace eb_product

@@ -20,6 +20,41 @@ constexpr int64_t kMostSize = (int64_t)1 << 30;
 
 int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1 : 2; }
 
+// The kernel for a call, from its mean of slots per expert (the counts are on
+// the device) and the workgroups that each tile gives.  Measured with 1, 8 and
+// 64 experts of 1024 x 2048 and 3328 x 1024 and 4 to 1024 slots each, us a call:
+//   stream against small tiles: as long as small tiles are fewer than a quarter
+//   of the compute units (one expert, 12 slots: 4.4 and 7.3; 8 experts, 12
+//   slots, 64 small tiles: 8.9 and 8.0); never with a gate and 8-bit outputs,
+//   whose workgroups hold 256 rows of all K too (12.1 and 10.2).
+//   Larger tiles read their operands less often, smaller ones fill the GPU and
+//   waste less of an expert's last tile.  8-bit unit: medium from 80 slots and
+//   128 tiles (64 experts, 96 slots: 40.9, small 48.3), large from 384 slots and
+//   128 tiles (8 experts, 512 slots: 21.6, medium 24.3).  16-bit unit, whose
+//   operands matter less: medium from 192 slots and 512 tiles (64 experts, 512
+//   slots: 184, small 220, large 210), large from 768 slots and 256 tiles (64
+//   experts, 1024 slots: 331, medium 343).
+KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t width, int64_t ldx, int64_t ldw, bool gathered,
+                         int64_t x_rows, bool gate, int32_t out_type)
+{
+    const bool fp8 = out_type == EB_FP8, wide = fp8 || out_type == EB_F32;
+    // The tile kernel addresses x (a slot tile's rows, or all where they are
+    // gathered) and an expert's weights with 32 bits.
+    constexpr int64_t kMost32 = (int64_t)1 << 32;
+    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 256) * ldx >= kMost32) return stream_kernel(gate, fp8);
+    const int64_t mean = (M + E - 1) / E;
+    auto tiles = [&](const KernelPlan &p) {
+        return std::min<int64_t>(E, M) * ((mean + p.height - 1) / p.height) * ((width + p.columns - 1) / p.columns);
+    };
+    const KernelPlan large = tile_kernel(gate, out_type, TileSize::kLarge);
+    if (mean >= (wide ? 768 : 384) && tiles(large) >= (wide ? 256 : 128)) return large;
+    const KernelPlan medium = tile_kernel(gate, out_type, TileSize::kMedium);
+    if (mean >= (wide ? 192 : 80) && tiles(medium) >= (wide ? 512 : 128)) return medium;
+    const KernelPlan small = tile_kernel(gate, out_type, TileSize::kSmall);
+    if (mean <= 96 && tiles(small) < 64 && !(gate && fp8)) return stream_kernel(gate, fp8);
+    return small;
+}
+
 int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
                  const float *x_scales, int64_t ldxs, const int32_t *tokens, const void *w, int64_t ldw,
                  const float *w_scales, const int32_t *offsets, const float *bias, int32_t act, int32_t out_type, void *out,
@@ -79,15 +114,7 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     const int es = element_bytes(out_type);
     a.vector_out = ldo * es % 16 == 0 && (uintptr_t)out % 16 == 0;
 
-    const int64_t mean = (M + E - 1) / E;
-    // The tile kernel addresses x (a slot tile's rows, or all where they are
-    // gathered) and an expert's weights with 32 bits.
-    constexpr int64_t kMost32 = (int64_t)1 << 32;
-    const bool reachable = N * ldw < kMost32 && (tokens ? x_rows : 256) * ldx < kMost32 && x_rows > 0;
-    const bool tiles = reachable && mean > 64;
-    KernelPlan plan = tiles ? tile_kernel(gate, out_type, true) : stream_kernel((int32_t)mean, gate, fp8);
-    // Large tiles where they give every compute unit a workgroup.
-    if (tiles && (M + plan.height - 1) / plan.height * ((width + plan.columns - 1) / plan.columns) < 256) plan = tile_kernel(gate, out_type, false);
+    const KernelPlan plan = choose_kernel(M, E, N, width, ldx, ldw, tokens != nullptr, x_rows, gate, out_type);
     a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
     // At most one tile per expert is not full.
     const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);

@@ -1,9 +1,11 @@
-// eb_expert_product for few slots per expert: bound by reading the weights.
+// eb_expert_product for few slots of few experts: bound by latency and by the
+// weights' way to the few compute units that have them.
 //
 // A workgroup of eight waves takes up to 16 * kTokens slots of an expert and a
 // run of its weight rows: kAcross waves side by side, each with kRows tiles of
 // 16 rows, kWaves / kAcross waves along K with every such block of 128 each,
-// joined in LDS in a fixed order.  The products are taken in the 16-bit unit,
+// joined in LDS in a fixed order.  Where the outputs are not quantised that is
+// 16 rows and all waves along K: many workgroups with short ways.  The products are taken in the 16-bit unit,
 // exact: its rate does not matter here.  Both operands come straight from global
 // memory into the registers of the matrix instructions; each weight is read
 // once per kTokens tiles, and a wave's 16 rows of 128 bytes are whole lines.
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(kWaves *kWave) void eb_product_stream(ProductArgs a
     if constexpr (kFp8) {
         if (threadIdx.x < kHeight) most[threadIdx.x] = 0;
         __syncthreads();
-        if (along == 0) most_of_outputs<kOut>(a, column, sum, most);
+        if (along == 0) most_of_outputs<kOut>(sum, most);
         __syncthreads();
         if (along == 0) store_fp8<kOut>(a, column, slot, sum, most, across == 0);
     } else {
@@ -133,20 +135,12 @@ KernelPlan plan()
             kWaves * kWave, 1};
 }
 
-template <int kTokens>
-KernelPlan plan_of(bool gate, bool fp8)
-{
-    if (gate) return fp8 ? plan<kTokens, 2, 8, true, true>() : plan<kTokens, 2, 1, true, false>();
-    return fp8 ? plan<kTokens, 2, 4, false, true>() : plan<kTokens, 1, 1, false, false>();
-}
-
 } // namespace
 
-KernelPlan stream_kernel(int32_t tokens, bool gate, bool fp8)
+KernelPlan stream_kernel(bool gate, bool fp8)
 {
-    if (tokens <= 16) return plan_of<1>(gate, fp8);
-    if (tokens <= 32) return plan_of<2>(gate, fp8);
-    return plan_of<4>(gate, fp8);
+    if (gate) return fp8 ? plan<1, 2, 8, true, true>() : plan<1, 2, 1, true, false>();
+    return fp8 ? plan<1, 2, 4, false, true>() : plan<1, 1, 1, false, false>();
 }
 
 } // namespace eb_product

@@ -66,7 +66,7 @@ struct alignas(16) Chunk {
 template <typename S>
 struct Stage {
     Chunk x[S::kHeight][8], w[S::kLines][8];
-    float x_scale[S::kHeight];
+    float x_scale[S::kHeight > kWave ? S::kHeight : kWave]; // copied by whole waves
 };
 
 // Workgroups are dealt to the 8 XCDs in turn.  Each takes runs of 32 tiles (its
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         }
         w_at[i] = (uint32_t)n * (uint32_t)a.ldw + chunk;
     }
-    // Scales: wave w < kHeight / 64 copies those of slots w * 64 + lane.
-    const bool copies_scales = wave < S::kHeight / kWave;
+    // Scales: wave w copies those of slots w * 64 + lane (past the tile: any).
+    const bool copies_scales = wave < (S::kHeight + kWave - 1) / kWave;
     uint32_t scale_at = 0;
     if (copies_scales) {
         const int32_t m = min(tile.first + wave * kWave + lane, tile.end - 1);
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         int *mine = &most[in_row / kBlock * S::kHeight + across_t * T * 16];
         for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) most[i] = 0;
         __syncthreads();
-        most_of_outputs<S::kOut16>(a, column, sum, mine);
+        most_of_outputs<S::kOut16>(sum, mine);
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < T; ++t) {

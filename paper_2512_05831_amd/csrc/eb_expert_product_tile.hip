@@ -6,24 +6,23 @@ namespace eb_product {
 
 namespace {
 
-template <bool kWide, bool kFp8>
-KernelPlan plan_of(bool gate, bool large)
+template <bool kWide, bool kGate, bool kFp8>
+KernelPlan plan_of(TileSize size)
 {
-    if (large) return gate ? tile_plan<TileShape<8, 4, 2, 4, kWide, true, kFp8>>() : tile_plan<TileShape<8, 4, 2, 4, kWide, false, kFp8>>();
-    if (!gate) return tile_plan<TileShape<4, 4, 2, 2, kWide, false, kFp8>>();
-    // 8-bit outputs need their 128 columns in the workgroup.
-    if constexpr (kFp8) return tile_plan<TileShape<4, 4, 1, 4, kWide, true, kFp8>>();
-    else return tile_plan<TileShape<4, 4, 2, 2, kWide, true, kFp8>>();
+    if (size == TileSize::kLarge) return tile_plan<TileShape<8, 4, 2, 4, kWide, kGate, kFp8>>();
+    if (size == TileSize::kMedium) return tile_plan<TileShape<4, 4, 2, 4, kWide, kGate, kFp8>>();
+    return tile_plan<TileShape<2, 4, 1, 4, kWide, kGate, kFp8>>();
 }
 
 } // namespace
 
 // 16-bit outputs: the 8-bit matrix unit.  fp32 and 8-bit outputs (whose scales
 // are fp32): the 16-bit unit, exact.
-KernelPlan tile_kernel(bool gate, int32_t out_type, bool large)
+KernelPlan tile_kernel(bool gate, int32_t out_type, TileSize size)
 {
-    if (out_type == EB_F16 || out_type == EB_BF16) return plan_of<false, false>(gate, large);
-    return out_type == EB_FP8 ? plan_of<true, true>(gate, large) : plan_of<true, false>(gate, large);
+    if (out_type == EB_F16 || out_type == EB_BF16) return gate ? plan_of<false, true, false>(size) : plan_of<false, false, false>(size);
+    if (out_type == EB_FP8) return gate ? plan_of<true, true, true>(size) : plan_of<true, false, true>(size);
+    return gate ? plan_of<true, true, false>(size) : plan_of<true, false, false>(size);
 }
 
 } // namespace eb_product

@@ -140,6 +140,20 @@ def test_outputs(out, act, M, N, K, bias, device):
         close(got, case, out)
 
 
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_SILU_GATE])
+@pytest.mark.parametrize("M,N,K,counts", [(6000, 2900, 300, None), (8200, 2050, 520, None), (8200, 4100, 129, None),
+                                          (8003, 2304, 640, [1000, 3, 2000, 0, 5000]), (3000, 4096, 400, [500] * 6), (1700, 2560, 256, [100, 103] * 8)])
+def test_every_size_of_tile(out, act, M, N, K, counts, device):
+    """Calls that large and medium tiles take, with tiles that are cut on either side."""
+    case = Case(M, N, K, device, E=1 if counts is None else len(counts), act=act, bias=True, counts=counts, gather=None if counts is None else 777)
+    got = case.run(out_dtype=out)
+    if out == torch.float8_e4m3fn:
+        close_fp8(*got, case)
+    else:
+        close(got, case, out)
+
+
 COUNTS = {"even": [20] * 9, "ragged": [0, 1, 130, 17, 0, 0, 64, 5, 300], "one": [0, 0, 0, 0, 500, 0, 0, 0, 0], "empty": [0] * 9,
           "long": [700, 3, 257, 0, 1400, 129, 128, 127, 1]}
 
