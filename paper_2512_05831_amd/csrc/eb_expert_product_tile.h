@@ -210,6 +210,13 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         };
 #pragma unroll
         for (int t = 0; t < T; ++t) {
+            // The wave that is behind goes first: a SIMD's two then reach the barrier together.
+            switch (t * 4 / T) {
+            case 0: __builtin_amdgcn_s_setprio(3); break;
+            case 1: __builtin_amdgcn_s_setprio(2); break;
+            case 2: __builtin_amdgcn_s_setprio(1); break;
+            default: __builtin_amdgcn_s_setprio(0);
+            }
             const Operand x = fit(next);
             f[t % 2] = next_scale * sw;
             f2[t % 2] = S::kGate ? next_scale * sw2 : f[t % 2];
