@@ -90,6 +90,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     __shared__ Stage<S> stage0, stage1;
     char *const out_tile = (char *)&stage0; // after the last block
     __shared__ int most[S::kFp8 ? S::kOutBlocks * S::kHeight : 1];
+    __shared__ int32_t slot_of[S::kHeight]; // of the tile's tokens; -1: not written
 
     const uint32_t at = tile_in_order(blockIdx.x, gridDim.x);
     // kBand slot tiles by all columns: a run of 32 covers 4 x 8 tiles.
@@ -102,23 +103,11 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     const int across_t = wave % S::kAcrossT, across_r = wave / S::kAcrossT;
 
     // Copies: the i-th of a wave fills rows (i * kWaves + wave) * 8 + lane / 8.
-    const int64_t x_first = a.tokens ? 0 : tile.first; // the buffer's first row
-    const int64_t x_end = a.tokens ? a.x_rows : tile.end;
-    const int64_t row_bytes = ((int64_t)a.K + 15) / 16 * 16; // of the last row; past it a buffer reads as zeros
-    const Buffer x_buffer = buffer_of(a.x + x_first * a.ldx, (uint32_t)((x_end - x_first - 1) * a.ldx + row_bytes));
-    const Buffer w_buffer = buffer_of(a.w + (int64_t)tile.expert * a.N * a.ldw, (uint32_t)((a.N - 1) * a.ldw + row_bytes));
+    // The weights' first: the tokens' wait for their rows' numbers.
+    const int32_t row_bytes = (a.K + 15) / 16 * 16; // of a buffer's last row; past it reads give zeros
     const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
-    uint32_t x_at[S::kCopiesX], w_at[S::kCopiesW];
-#pragma unroll
-    for (int i = 0; i < S::kCopiesX; ++i) {
-        const int32_t m = min(tile.first + (i * S::kWaves + wave) * 8 + lane / 8, tile.end - 1);
-        int32_t row = m - (int32_t)x_first;
-        if (a.tokens) {
-            row = a.tokens[m];
-            row = row >= 0 && row < a.x_rows ? row : 0;
-        }
-        x_at[i] = (uint32_t)row * (uint32_t)a.ldx + chunk;
-    }
+    const Buffer w_buffer = buffer_of(a.w + (int64_t)tile.expert * a.N * a.ldw, (uint32_t)((a.N - 1) * a.ldw + row_bytes));
+    uint32_t w_at[S::kCopiesW];
 #pragma unroll
     for (int i = 0; i < S::kCopiesW; ++i) {
         const int line = (i * S::kWaves + wave) * 8 + lane / 8;
@@ -132,28 +121,44 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         }
         w_at[i] = (uint32_t)n * (uint32_t)a.ldw + chunk;
     }
+    auto fill_weights = [&](Stage<S> &s, int32_t kb) {
+#pragma unroll
+        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i], (uint32_t)kb * kBlock);
+    };
+    fill_weights(stage0, 0);
+
+    const int64_t x_first = a.tokens ? 0 : tile.first; // the buffer's first row
+    const int64_t x_end = a.tokens ? a.x_rows : tile.end;
+    const Buffer x_buffer = buffer_of(a.x + x_first * a.ldx, (uint32_t)((x_end - x_first - 1) * a.ldx + row_bytes));
+    auto row_of = [&](int token) { // in the buffer; a slot that is not written takes any
+        const int32_t m = min(tile.first + token, tile.end - 1);
+        if (!a.tokens) return m - tile.first;
+        const int32_t row = a.tokens[m];
+        return row >= 0 && row < a.x_rows ? row : 0;
+    };
+    uint32_t x_at[S::kCopiesX];
+#pragma unroll
+    for (int i = 0; i < S::kCopiesX; ++i) x_at[i] = (uint32_t)row_of((i * S::kWaves + wave) * 8 + lane / 8) * (uint32_t)a.ldx + chunk;
     // Scales: wave w copies those of slots w * 64 + lane (past the tile: any).
     const bool copies_scales = wave < (S::kHeight + kWave - 1) / kWave;
-    uint32_t scale_at = 0;
-    if (copies_scales) {
-        const int32_t m = min(tile.first + wave * kWave + lane, tile.end - 1);
-        int32_t row = m - (int32_t)x_first;
-        if (a.tokens) {
-            row = a.tokens[m];
-            row = row >= 0 && row < a.x_rows ? row : 0;
-        }
-        scale_at = (uint32_t)row * 4;
-    }
-
-    auto fill = [&](Stage<S> &s, int32_t kb) {
-        const uint32_t k0 = (uint32_t)kb * kBlock;
+    const uint32_t scale_at = (uint32_t)row_of(threadIdx.x % S::kHeight) * 4;
+    auto fill_tokens = [&](Stage<S> &s, int32_t kb) {
 #pragma unroll
-        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i], k0);
-#pragma unroll
-        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i], k0);
+        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i], (uint32_t)kb * kBlock);
         if (copies_scales)
             copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.x_scale[wave * kWave], scale_at, 0);
     };
+    fill_tokens(stage0, 0);
+    auto fill = [&](Stage<S> &s, int32_t kb) {
+        fill_tokens(s, kb);
+        fill_weights(s, kb);
+    };
+    for (int i = threadIdx.x; i < S::kHeight; i += S::kThreads) {
+        const int32_t m = tile.first + i;
+        int32_t slot = m < tile.end ? m : -1;
+        if (a.tokens && slot >= 0 && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) slot = -1;
+        slot_of[i] = slot;
+    }
     // K's last block: what was copied from past a row's end becomes zeros.
     auto cut = [&](Stage<S> &s, int left) {
         for (int i = threadIdx.x; i < S::kHeight + S::kLines; i += S::kThreads) {
@@ -252,7 +257,6 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         __syncthreads();
     };
     const int tail = a.K % kBlock;
-    fill(stage0, 0);
     int32_t kb = 0;
     for (; kb + 1 < a.k_blocks; kb += 2) {
         arrive();
@@ -274,11 +278,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.
         int32_t slot[T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            const int32_t m = tile.first + (across_t * T + t) * 16 + lane % 16;
-            slot[t] = m < tile.end ? m : -1;
-            if (a.tokens && slot[t] >= 0 && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) slot[t] = -1;
-        }
+        for (int t = 0; t < T; ++t) slot[t] = slot_of[(across_t * T + t) * 16 + lane % 16];
         store_floats<S::kOut16>(a, column, slot, sum);
         return;
     }
@@ -295,12 +295,8 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
             // Of each kAcrossT-th of the tile's tokens a pass takes T / kPasses tiles of 16.
             constexpr int kPart = T / kPasses * 16;
             const int j = i / kChunks, c = i % kChunks;
-            const int32_t m = tile.first + j / kPart * T * 16 + pass * kPart + j % kPart;
-            if (c * 16 >= left || m >= tile.end) continue;
-            if (a.tokens) {
-                const int32_t row = a.tokens[m];
-                if (row < 0 || row >= a.x_rows) continue;
-            }
+            const int32_t m = slot_of[j / kPart * T * 16 + pass * kPart + j % kPart];
+            if (c * 16 >= left || m < 0) continue;
             const char *from = chunk_of(j, c);
             char *to = (char *)a.out + ((int64_t)m * a.ldo + column0) * kSize + c * 16;
             if (a.vector_out && c * 16 + 16 <= left) {
@@ -330,9 +326,8 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         __syncthreads();
         to_slots(0);
         for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) {
-            const int32_t m = tile.first + i % S::kHeight, b = column0 / kBlock + i / S::kHeight;
-            if (m >= tile.end || b >= a.row_blocks) continue;
-            if (a.tokens && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) continue;
+            const int32_t m = slot_of[i % S::kHeight], b = column0 / kBlock + i / S::kHeight;
+            if (m < 0 || b >= a.row_blocks) continue;
             a.out_scales[(int64_t)b * a.ldos + m] = block_scale(most[i]);
         }
     } else {
