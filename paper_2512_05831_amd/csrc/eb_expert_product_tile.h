@@ -25,16 +25,18 @@ __device__ __forceinline__ Buffer buffer_of(const void *p, uint32_t bytes)
     return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000);
 }
 
-// kBytes per lane from a buffer to LDS, lane after lane from `to`.
+// kBytes per lane from a buffer to LDS, lane after lane from `to`.  The whole
+// offset is the lane's: a scalar one would be left out of the bounds check, which
+// gives zeros for what K's last block has past the last row.
 template <int kBytes>
-__device__ __forceinline__ void copy_to_lds(Buffer from, void *to, uint32_t lane_offset, uint32_t offset)
+__device__ __forceinline__ void copy_to_lds(Buffer from, void *to, uint32_t offset)
 {
     static_assert(kBytes == 16 || kBytes == 4, "");
     const auto lds = (__attribute__((address_space(3))) void *)to;
     if constexpr (kBytes == 16)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, lane_offset, offset, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, offset, 0, 0, 0);
     else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, lane_offset, offset, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, offset, 0, 0, 0);
 }
 
 template <int kTokens16_, int kRows16_, int kAcrossT_, int kAcrossR_, bool kWide_, bool kGate_, bool kFp8_>
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     }
     auto fill_weights = [&](Stage<S> &s, int32_t kb) {
 #pragma unroll
-        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i], (uint32_t)kb * kBlock);
+        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i] + (uint32_t)kb * kBlock);
     };
     fill_weights(stage0, 0);
 
@@ -144,9 +146,9 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     const uint32_t scale_at = (uint32_t)row_of(threadIdx.x % S::kHeight) * 4;
     auto fill_tokens = [&](Stage<S> &s, int32_t kb) {
 #pragma unroll
-        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i], (uint32_t)kb * kBlock);
+        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i] + (uint32_t)kb * kBlock);
         if (copies_scales)
-            copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.x_scale[wave * kWave], scale_at, 0);
+            copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.x_scale[wave * kWave], scale_at);
     };
     fill_tokens(stage0, 0);
     auto fill = [&](Stage<S> &s, int32_t kb) {
