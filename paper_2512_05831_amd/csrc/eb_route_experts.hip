@@ -13,8 +13,9 @@
 //         where K is 8) go to LDS, a lane takes one each and counts the better
 //         ones: about 220 instructions, where K rounds of "largest value left,
 //         lowest expert that has it, out with it" are 680 (16 values a lane).
-//         Those rounds are taken where more than 16 values reach the bound, and
-//         for other K and L.  Each workgroup counts its pairs per expert.
+//         (Two each where 17 to 32 reach the bound: one token in 25, but then its
+//         whole wave.)  Those rounds are taken where more do, and for other K
+//         and L.  Each workgroup counts its pairs per expert.
 // scan    exclusive prefix of each expert's counts over the chunks of kTokens
 //         tokens.
 // place   each workgroup ranks its pairs within their experts (in pair order:
@@ -105,8 +106,8 @@ struct TokenSpace {
             int group_key[kMostGroups];
         };
         struct {
-            int64_t found[16 + L]; // from 16 on: what is not wanted
-            int64_t best[16];
+            int64_t found[32 + L]; // from 32 on: what is not wanted
+            int64_t best[kFilterTop];
         };
     };
 };
@@ -156,23 +157,32 @@ __device__ __forceinline__ void best_by_filter(int (&key)[V], int lane, int K, T
     upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xF, 0xF, false);
     upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xF, 0xF, false);
     const int n = max_lanes<16>(upto);
-    if (__any(n > 16)) return best_by_rounds<16, V>(key, lane, K, id, id_key);
+    if (__any(n > 32)) return best_by_rounds<16, V>(key, lane, K, id, id_key);
+    const bool second = __any(n > 16); // a lane then takes two
     const int64_t none = candidate(kNoneKey, 0x7FFFFFFF);
     space.found[lane] = none;
+    space.found[16 + lane] = none;
     wave_fence();
     int at = upto - mine;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const bool wanted = key[v] >= bound;
-        space.found[wanted ? at : 16 + lane] = candidate(key[v], v * 16 + lane);
+        space.found[wanted ? at : 32 + lane] = candidate(key[v], v * 16 + lane);
         at += wanted;
     }
     wave_fence();
-    const int64_t own = space.found[lane];
-    int rank = 0;
+    auto settle = [&](int64_t own) {
+        int rank = 0;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) rank += space.found[j] > own;
-    if (own != none) space.best[rank] = own;
+        for (int j = 0; j < 16; ++j) rank += space.found[j] > own;
+        if (second) {
+#pragma unroll
+            for (int j = 16; j < 32; ++j) rank += space.found[j] > own;
+        }
+        if (own != none && rank < kFilterTop) space.best[rank] = own;
+    };
+    settle(space.found[lane]);
+    if (second) settle(space.found[16 + lane]);
     wave_fence();
     if (lane < min(n, K)) {
         const int64_t c = space.best[lane];
@@ -220,15 +230,32 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
         }
     }
     if (scored) {
+        // A branch around each loop, not in it: the values' chains then overlap.
+        float s[V];
+        if (a.sigmoid) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = v * L + lane;
-            float s = a.sigmoid ? sigmoid(x[v]) : exp_of(x[v] - top_x) / total;
-            if (a.bias) s += bias[v];
-            // A NaN bias makes its expert unfit, as a NaN score does.
-            s = x[v] > -kInf && s == s ? s : -kInf;
-            if (a.pair && e < a.E) space.judged[e + (e * a.group_magic >> 20)] = s;
-            if (a.bias) key[v] = order_key(s);
+            for (int v = 0; v < V; ++v) s[v] = sigmoid(x[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) s[v] = exp_of(x[v] - top_x) / total;
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) s[v] += bias[v];
+        }
+        // A NaN bias makes its expert unfit, as a NaN score does.
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = x[v] > -kInf && s[v] == s[v] ? s[v] : -kInf;
+        if (a.pair) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = v * L + lane;
+                space.judged[min((int)(e + (e * a.group_magic >> 20)), L * V + kMostGroups - 1)] = s[v];
+            }
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = order_key(s[v]);
         }
     }
     if (a.groups > 1) {
@@ -236,7 +263,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int e = v * L + lane;
-                if (e < a.E) space.judged[e + (e * a.group_magic >> 20)] = key_value(key[v]);
+                space.judged[min((int)(e + (e * a.group_magic >> 20)), L * V + kMostGroups - 1)] = key_value(key[v]);
             }
         }
         wave_fence();
