@@ -17,7 +17,7 @@ import functools
 from typing import NamedTuple
 
 from . import eb
-from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, EbError, _check, _same_device, _stream_ptr
+from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, _check, _same_device, _stream_ptr
 
 EB_FP8 = 3
 EB_SOFTMAX, EB_SIGMOID = 0, 1
@@ -312,3 +312,55 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
     if code == EB_FP8:
         return (out if ldo == width else out[:, :width]), scales.t()
     return out
+
+
+class ExpertLayer:
+    """A mixture of experts for inference: each token's ``top`` experts' two
+    layers, joined with the router's weights.
+
+    ``w_up``: [E, N, K] and ``w_down``: [E, D, N] (or, gated, [E, D, N / 2]) device
+    tensors of fp32, fp16 or bf16, held here in 8 bits with a scale per
+    128 x 128; ``router``: [experts, K] fp32, whose rows give the scores of all
+    experts.  Row-wise over several GPUs, a GPU holds the experts
+    [shard_lo, shard_lo + E) of them, as a row shard of a table holds rows: its
+    results are partial sums, to be added over the GPUs (``sum_partials``)."""
+
+    def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = EB_SOFTMAX | EB_RENORMALIZE,
+                 bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0, shard_lo: int = 0):
+        if w_up.dim() != 3 or w_down.dim() != 3 or router.dim() != 2:
+            raise ValueError("w_up and w_down must be 3-D, router 2-D")
+        E, N, K = w_up.shape
+        gate = act == EB_ACT_SILU_GATE
+        if gate and N % 2 or tuple(w_down.shape[::2]) != (E, N // 2 if gate else N) or router.shape[1] != K:
+            raise ValueError("w_up [E, N, K], w_down [E, D, N or N / 2] and router [experts, K] do not fit")
+        self.E, self.K, self.D, self.top, self.act, self.mode = E, K, int(w_down.shape[1]), top, act, mode
+        self.router, self.bias, self.groups, self.top_groups, self.scale = router, bias, groups, top_groups, scale
+        self.shard_lo = shard_lo
+        # Under a gate each half of the rows is blocked on its own.
+        parts = 2 if gate else 1
+        q, s = quantize_fp8(w_up.contiguous().view(E * parts, N // parts, K), block_rows=BLOCK)
+        self.w_up, self.up_scales = q.as_strided((E, N, K), (N * q.stride(1), q.stride(1), 1)), s.view(E, -1, s.shape[2])
+        self.w_down, self.down_scales = quantize_fp8(w_down.contiguous(), block_rows=BLOCK)
+        self._bags = None
+
+    def forward(self, x, scores=None, out=None):
+        """``x``: device [B, K] of fp32, fp16 or bf16, for example a batch's
+        pooled lookups; ``scores``: [B, experts], or None for the router's.
+        Returns fp32 [B, D]."""
+        import torch
+
+        B = int(x.shape[0])
+        if scores is None:
+            scores = x.float() @ self.router.t()
+        r = route(scores, self.top, self.mode, self.bias, self.groups, self.top_groups, self.scale, self.shard_lo,
+                  self.shard_lo + self.E)
+        q, s = quantize_fp8(x)
+        h, hs = product(q, s, self.w_up, self.up_scales, r.offsets, r.tokens, act=self.act, out_dtype=torch.float8_e4m3fn)
+        y = product(h, hs, self.w_down, self.down_scales, r.offsets, out_dtype=torch.bfloat16)
+        if self._bags is None or self._bags.numel() != B + 1 or self._bags.device != x.device:
+            self._bags = torch.arange(0, B * self.top + 1, self.top, dtype=torch.int32, device=x.device)
+        # A token is a bag of its pairs' slots; a pair without one (-1) is skipped.
+        slots = eb.EmbeddingBagTables([y])
+        out = slots.forward_ex(r.slots.view(-1), self._bags, B, EB_SUM, out=out, weights=r.weights.view(-1))
+        slots.close()
+        return out
