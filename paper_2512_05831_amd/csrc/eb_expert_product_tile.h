@@ -204,7 +204,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
         // Products on their way to the sums: those of the kDelay tiles of 16 x 16
         // (in the order of tokens, then rows) before the one in work.
-        constexpr int kDelay = S::kWide ? 2 : R;
+        constexpr int kDelay = S::kWide ? 1 : R;
         f32x4 product[kDelay];
         float f[2], f2[2]; // factors of even and odd token tiles
         auto add = [&](int i) {

@@ -17,7 +17,7 @@ import functools
 from typing import NamedTuple
 
 from . import eb
-from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, _check, _same_device, _stream_ptr
+from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, _check, _stream_ptr
 
 EB_FP8 = 3
 EB_SOFTMAX, EB_SIGMOID = 0, 1
@@ -101,6 +101,14 @@ def _on(stream):
     import torch
 
     return torch.cuda.stream(stream)
+
+
+def _same_device(dev, *tensors) -> None:
+    """Every tensor given (None skipped) lives on the GPU ``dev``."""
+    index = dev.index
+    for x in tensors:
+        if x is not None and x.get_device() != index:
+            raise ValueError(f"tensor on {x.device}, expected {dev}")
 
 
 def _blocks(n: int) -> int:
