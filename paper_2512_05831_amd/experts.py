@@ -349,7 +349,6 @@ class ExpertLayer:
         q, s = quantize_fp8(w_up.contiguous().view(E * parts, N // parts, K), block_rows=BLOCK)
         self.w_up, self.up_scales = q.as_strided((E, N, K), (N * q.stride(1), q.stride(1), 1)), s.view(E, -1, s.shape[2])
         self.w_down, self.down_scales = quantize_fp8(w_down.contiguous(), block_rows=BLOCK)
-        self._bags = None
 
     def forward(self, x, scores=None, out=None):
         """``x``: device [B, K] of fp32, fp16 or bf16, for example a batch's
@@ -365,10 +364,9 @@ class ExpertLayer:
         q, s = quantize_fp8(x)
         h, hs = product(q, s, self.w_up, self.up_scales, r.offsets, r.tokens, act=self.act, out_dtype=torch.float8_e4m3fn)
         y = product(h, hs, self.w_down, self.down_scales, r.offsets, out_dtype=torch.bfloat16)
-        if self._bags is None or self._bags.numel() != B + 1 or self._bags.device != x.device:
-            self._bags = torch.arange(0, B * self.top + 1, self.top, dtype=torch.int32, device=x.device)
+        bags = torch.arange(0, B * self.top + 1, self.top, dtype=torch.int32, device=x.device)
         # A token is a bag of its pairs' slots; a pair without one (-1) is skipped.
         slots = eb.EmbeddingBagTables([y])
-        out = slots.forward_ex(r.slots.view(-1), self._bags, B, EB_SUM, out=out, weights=r.weights.view(-1))
+        out = slots.forward_ex(r.slots.view(-1), bags, B, EB_SUM, out=out, weights=r.weights.view(-1))
         slots.close()
         return out

@@ -113,3 +113,23 @@ def test_refusals(device):
     for bad in ((w_up[:, :5], w_down, router), (w_up, w_down[:1], router), (w_up, w_down, router[:, :7]), (w_up[0], w_down, router)):
         with pytest.raises(ValueError):
             ex.ExpertLayer(*bad, 1)
+
+
+def test_one_layer_on_two_streams(device):
+    """A stream that has not waited for another's call does not need that call's results."""
+    layer = layer_of(8, 256, 128, 64, 2, ex.EB_ACT_RELU, device)
+    x = torch.randn(50, 256, device=device)
+    scores = torch.randn(50, 8, device=device)
+    want = layer_of(8, 256, 128, 64, 2, ex.EB_ACT_RELU, device).forward(x, scores)
+    torch.cuda.synchronize()
+    late, early = torch.cuda.Stream(), torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device=device)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(late):
+        for _ in range(20):  # holds this stream's call back
+            big = big @ big * 1e-3
+        first = layer.forward(x, scores)
+    with torch.cuda.stream(early):
+        second = layer.forward(x, scores)
+    torch.cuda.synchronize()
+    assert torch.equal(first, want) and torch.equal(second, want)
