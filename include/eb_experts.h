@@ -62,7 +62,7 @@ int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo
  *                outputs x.  An expert whose x is -infinity or NaN cannot be
  *                chosen; +infinity counts as the largest finite float.
  *   bias         device fp32 [E] added to the scores for the choice only, or
- *                NULL.
+ *                NULL.  NaN and -infinity keep their expert from being chosen.
  *   mode         EB_SOFTMAX (s = softmax of a token's x) or EB_SIGMOID
  *                (s = 1 / (1 + exp(-x))), optionally | EB_RENORMALIZE
  *                | EB_GROUP_PAIR.
@@ -94,8 +94,8 @@ int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo
  *
  * Scores, sums and weights are fp32 whatever the type of x.  Equal calls give
  * equal bits.  Errors: EB_ERR_INVALID for an argument outside the above,
- * EB_ERR_UNSUPPORTED for E, K, groups or N * K beyond the limits, EB_ERR_HIP
- * when a launch fails.  N == 0 writes zero offsets.
+ * EB_ERR_UNSUPPORTED for E, K, groups or N * K beyond the limits or 2^28 tokens
+ * and more, EB_ERR_HIP when a launch fails.  N == 0 writes zero offsets.
  */
 int eb_route_experts(int64_t N, int32_t E, int32_t K, const void *scores, int32_t dtype, int64_t ld,
                      const float *bias, int32_t mode, int32_t groups, int32_t top_groups, float scale,
@@ -125,7 +125,8 @@ int eb_route_experts(int64_t N, int32_t E, int32_t K, const void *scores, int32_
  * to nearest even, both divisions in fp32: the value held is q * scale.  A
  * block with an infinity or a NaN has the scale NaN and only NaNs.  Errors:
  * EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED for
- * more than 2^31 blocks, EB_ERR_HIP when a launch fails.
+ * sizes one launch does not hold (2^24 strips of 16 rows by 512 columns, or of
+ * 128 x 128), EB_ERR_HIP when a launch fails.
  */
 int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx,
                     int32_t block_rows, void *q, int64_t ldq, float *scales, int64_t lds, void *stream);
@@ -180,7 +181,8 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  * them cut off: about 1.5e-5 of the size of a sum of normal values, far below
  * the outputs' rounding.  Equal calls give equal bits.
  * Errors: EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED
- * for sizes one launch does not hold, EB_ERR_HIP when a launch fails.
+ * for sizes one launch does not hold (2^23 tiles), EB_ERR_HIP when a launch
+ * fails.
  */
 int eb_expert_product(int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
                       const float *x_scales, int64_t ldxs, const int32_t *tokens, const void *w, int64_t ldw,

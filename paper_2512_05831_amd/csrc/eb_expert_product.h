@@ -90,7 +90,7 @@ __device__ __forceinline__ SlotTile slot_tile(const ProductArgs &a, int32_t inde
             const int32_t first = lo + (index - (upto - n)) * kHeight;
             const int32_t from = __shfl(first, at), to = __shfl(hi, at);
             return {__builtin_amdgcn_readfirstlane(e0 + at), __builtin_amdgcn_readfirstlane(from),
-                    __builtin_amdgcn_readfirstlane(min(to, from + kHeight))};
+                    __builtin_amdgcn_readfirstlane(from + min(to - from, kHeight))};
         }
         index -= __shfl(upto, kWave - 1);
     }

@@ -119,8 +119,9 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     // At most one tile per expert is not full.
     const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);
     const int64_t slot_tiles = (most_tiles + plan.band - 1) / plan.band * plan.band;
-    if (slot_tiles > std::numeric_limits<int32_t>::max() / a.column_tiles)
-        return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", who);
+    // A launch's threads are counted in 32 bits.
+    if (slot_tiles > std::numeric_limits<uint32_t>::max() / plan.threads / a.column_tiles)
+        return fail(EB_ERR_UNSUPPORTED, "%s: more tiles than one launch holds", who);
     void *args[] = {&a};
     const hipError_t err = hipLaunchKernel((void *)plan.kernel, dim3((unsigned)(slot_tiles * a.column_tiles)), dim3((unsigned)plan.threads),
                                            args, 0, (hipStream_t)stream);

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     const int64_t x_end = a.tokens ? a.x_rows : tile.end;
     const Buffer x_buffer = buffer_of(a.x + x_first * a.ldx, (uint32_t)((x_end - x_first - 1) * a.ldx + row_bytes));
     auto row_of = [&](int token) { // in the buffer; a slot that is not written takes any
-        const int32_t m = min(tile.first + token, tile.end - 1);
+        const int32_t m = tile.first + min(token, tile.end - tile.first - 1);
         if (!a.tokens) return m - tile.first;
         const int32_t row = a.tokens[m];
         return row >= 0 && row < a.x_rows ? row : 0;
@@ -156,9 +156,8 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         fill_weights(s, kb);
     };
     for (int i = threadIdx.x; i < S::kHeight; i += S::kThreads) {
-        const int32_t m = tile.first + i;
-        int32_t slot = m < tile.end ? m : -1;
-        if (a.tokens && slot >= 0 && (a.tokens[m] < 0 || a.tokens[m] >= a.x_rows)) slot = -1;
+        int32_t slot = i < tile.end - tile.first ? tile.first + i : -1;
+        if (a.tokens && slot >= 0 && (a.tokens[slot] < 0 || a.tokens[slot] >= a.x_rows)) slot = -1;
         slot_of[i] = slot;
     }
     // K's last block: what was copied from past a row's end becomes zeros.

@@ -195,7 +195,8 @@ int quantize_impl(const char *who, int32_t matrices, int64_t rows, int64_t cols,
         a.row_blocks = (rows + kBlock - 1) / kBlock;
         grid = a.col_blocks > kMost / a.row_blocks / matrices ? kMost + 1 : matrices * a.row_blocks * a.col_blocks;
     }
-    if (grid > kMost) return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks", who);
+    if (grid > std::numeric_limits<uint32_t>::max() / kThreads) // a launch's threads are counted in 32 bits
+        return fail(EB_ERR_UNSUPPORTED, "%s: more blocks than one launch holds", who);
     void *kernel = dtype == EB_F32 ? kernel_of<float>(block_rows != 1, aligned)
                    : dtype == EB_F16 ? kernel_of<_Float16>(block_rows != 1, aligned)
                                      : kernel_of<Bf16>(block_rows != 1, aligned);

@@ -313,6 +313,10 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
     }
     float w = id < 0 ? 0.f : a.sigmoid ? sigmoid(x_of) : exp_of(x_of - top_x);
     if (a.renormalize) {
+        if (!a.sigmoid && scored) { // against the largest of the chosen: they may lie far below top_x
+            const float m = key_value(max_lanes<L>(order_key(x_of)));
+            w = id < 0 ? 0.f : exp_of(x_of - m);
+        }
         if (a.sigmoid) { // e^-m / (1 + e^-x): no underflow where all x are low
             const float m = fminf(key_value(max_lanes<L>(order_key(x_of))), 0.f);
             w = id < 0 ? 0.f : 1.f / (expf(m) + expf(m - x_of));
@@ -671,6 +675,8 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     auto launch = [&](void *f, int64_t grid, int threads) {
         return hipLaunchKernel(f, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, s);
     };
+    if (a.chunks > std::numeric_limits<uint32_t>::max() / kChooseThreads)
+        return fail(EB_ERR_UNSUPPORTED, "%s: more tokens than one launch holds", who);
     hipError_t err = few ? launch(kernel, 1, kAllThreads) : launch(kernel, a.chunks, kChooseThreads);
     if (err == hipSuccess && offsets && !few) {
         if (!a.counts) {

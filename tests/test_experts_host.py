@@ -98,3 +98,11 @@ def test_product_rejects(kw, code):
 
 def test_product_without_work():
     product(M=0, x_rows=0, ldxs=0, x_ptr=None, out_ptr=None)
+
+
+def test_more_than_one_launch_holds():
+    """A launch has fewer than 2^32 threads."""
+    assert code_of(route, N=1 << 28, E=1, K=1, ld=1, shard_hi=1, workspace_bytes=1 << 40) == U
+    assert code_of(quantize, rows=1 << 28, cols=1, ldx=1, ldq=16, lds=1 << 28) == U
+    assert code_of(quantize, matrices=1 << 24, rows=1, cols=1, ldx=1, ldq=16, block_rows=128) == U
+    assert code_of(product, M=1 << 28, E=1, N=1 << 20, ldo=1 << 20, x_rows=1 << 28, ldxs=1 << 28) == U

@@ -235,3 +235,19 @@ def test_refusals(device):
         ex.route(x.t(), 2)
     with pytest.raises(ValueError):
         ex.route(x, 2, bias=torch.zeros(31, device=device))
+
+
+def test_softmax_of_chosen_far_below_the_largest(device):
+    """The bias keeps the largest score out; the others' shares of each other stay."""
+    g = torch.Generator().manual_seed(8)
+    for N in (5, 700):
+        x = torch.randn(N, 40, generator=g)
+        x[:, 11] = 200.0
+        bias = torch.linspace(0, 1, 40)
+        bias[11] = -9.0
+        r = check(x, 6, device, ex.EB_SOFTMAX | ex.EB_RENORMALIZE, bias)
+        assert (r.ids != 11).all() and (r.weights > 0).all()
+        pair = torch.randn(N, 40, generator=g)
+        pair[:, 13], pair[:, 12:16:2], pair[:, 15] = 150.0, -INF, -INF  # its group has no second
+        r = check(pair, 5, device, ex.EB_SOFTMAX | ex.EB_RENORMALIZE | ex.EB_GROUP_PAIR, groups=10, top_groups=4, least_clear=0.0)
+        assert (r.ids != 13).all() and (r.weights > 0).all()
