@@ -250,7 +250,7 @@ __device__ __forceinline__ void store_floats(const ProductArgs &a, int32_t colum
 
 // The largest magnitude of this wave's outputs for each of its tokens into
 // `most` (LDS, one word per token of the workgroup's tile and output block,
-// zero before).  Columns past the width repeat the last one.
+// zero before).
 template <int kOut, int kRows, int kTokens>
 __device__ __forceinline__ void most_of_outputs(const f32x4 (&s)[kRows][kTokens], int *most)
 {
@@ -303,7 +303,7 @@ struct KernelPlan {
     int32_t band;    // the grid holds a multiple of so many slot tiles
 };
 
-// Slots and weight rows of a workgroup: 256 x 256, 128 x 256, 32 x 256.
+// Slots of a workgroup: 128, 64, 32 (by 256 weight rows).
 enum class TileSize { kLarge, kMedium, kSmall };
 
 KernelPlan stream_kernel(bool gate, bool fp8);

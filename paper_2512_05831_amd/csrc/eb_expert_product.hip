@@ -21,19 +21,23 @@ constexpr int64_t kMostSize = (int64_t)1 << 30;
 int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1 : 2; }
 
 // The kernel for a call, from its mean of slots per expert (the counts are on
-// the device) and the workgroups that each tile gives.  Measured with 1, 8 and
-// 64 experts of 1024 x 2048 and 3328 x 1024 and 4 to 1024 slots each, us a call:
-//   stream against small tiles: as long as small tiles are fewer than a quarter
-//   of the compute units (one expert, 12 slots: 4.4 and 7.3; 8 experts, 12
-//   slots, 64 small tiles: 8.9 and 8.0); never with a gate and 8-bit outputs,
-//   whose workgroups hold 256 rows of all K too (12.1 and 10.2).
+// the device) and the workgroups that each kernel then has.  Measured, us of GPU
+// time a call, with slots a third around the mean:
+//   Stream against small tiles.  Its time is its workgroups', 16 slots by 16
+//   rows each, whatever the other's is per block of K: one expert of 2048 x 4096,
+//   100 slots (896 workgroups) 15.1 and 25.2 in the 8-bit unit, 17.9 and 28.0 in
+//   the 16-bit one; 200 slots (1664) 29.9 and 25.4, 22.6 and 28.1; 400 slots 52
+//   and 25.5, 38.5 and 28.3.  With a gate a workgroup has twice the rows (100
+//   slots 13.9 and 25.0, 400 slots 42.9 and 25.0), with 8-bit outputs eight times
+//   (1000 x 1520: 200 slots 9.4 and 14.4; 16 experts of 2048 x 1024, 16 slots: 15.5
+//   and 11.3), with both it holds 256 rows of all K as a tile does: 45.9 and 27.8.
 //   Larger tiles read their operands less often, smaller ones fill the GPU and
-//   waste less of an expert's last tile.  8-bit unit: medium from 80 slots and
-//   128 tiles (64 experts, 96 slots: 40.9, small 48.3), large from 384 slots and
-//   128 tiles (8 experts, 512 slots: 21.6, medium 24.3).  16-bit unit, whose
-//   operands matter less: medium from 192 slots and 512 tiles (64 experts, 512
-//   slots: 184, small 220, large 210), large from 768 slots and 256 tiles (64
-//   experts, 1024 slots: 331, medium 343).
+//   waste less of an expert's last tile.  16 experts of 2048 x 1024: large against
+//   medium, 8-bit unit, 200 slots (256 tiles) 16.8 and 17.8, 900 slots 43.6 and
+//   46.2; 16-bit unit 200 slots 33.8 and 25.0, 400 slots (512 tiles) 41.6 and 44.0.
+//   Medium against small: 8-bit unit, 100 slots (256 tiles) 13.1 and 13.4, 200
+//   slots 17.8 and 22.7; 16-bit unit 100 slots 17.0 and 17.4 (32 experts of 1024 x
+//   2048, also 256 tiles: 36.6 and 26.6), 200 slots (512 tiles) 25.0 and 28.8.
 KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t width, int64_t ldx, int64_t ldw, bool gathered,
                          int64_t x_rows, bool gate, int32_t out_type)
 {
@@ -41,18 +45,18 @@ KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t width, int64_t
     // The tile kernel addresses x (a slot tile's rows, or all where they are
     // gathered) and an expert's weights with 32 bits.
     constexpr int64_t kMost32 = (int64_t)1 << 32;
-    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 256) * ldx >= kMost32) return stream_kernel(gate, fp8);
+    const KernelPlan stream = stream_kernel(gate, fp8);
+    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 128) * ldx >= kMost32) return stream;
     const int64_t mean = (M + E - 1) / E;
     auto tiles = [&](const KernelPlan &p) {
         return std::min<int64_t>(E, M) * ((mean + p.height - 1) / p.height) * ((width + p.columns - 1) / p.columns);
     };
+    if (!(gate && fp8) && tiles(stream) * (fp8 ? 8 : gate ? 2 : 1) <= (wide ? 1536 : 1024)) return stream;
     const KernelPlan large = tile_kernel(gate, out_type, TileSize::kLarge);
-    if (mean >= (wide ? 768 : 384) && tiles(large) >= (wide ? 256 : 128)) return large;
+    if (tiles(large) >= (wide ? 512 : 256)) return large;
     const KernelPlan medium = tile_kernel(gate, out_type, TileSize::kMedium);
-    if (mean >= (wide ? 192 : 80) && tiles(medium) >= (wide ? 512 : 128)) return medium;
-    const KernelPlan small = tile_kernel(gate, out_type, TileSize::kSmall);
-    if (mean <= 96 && tiles(small) < 64 && !(gate && fp8)) return stream_kernel(gate, fp8);
-    return small;
+    if (tiles(medium) >= (wide ? 320 : 192)) return medium;
+    return tile_kernel(gate, out_type, TileSize::kSmall);
 }
 
 int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,

@@ -1,14 +1,30 @@
-// eb_expert_product for many slots per expert: bound by the matrix units.
+// eb_expert_product for many slots per expert: bound by the matrix units and, on
+// the way to them, by the power they may draw.
 //
-// A workgroup takes kTokens16 * kAcrossT * 16 slots of an expert by
-// kRows16 * kAcrossR * 16 weight rows, a wave kTokens16 x kRows16 tiles of
+// A workgroup of four waves takes kTokens16 * 16 slots of an expert by 256 weight
+// rows, a wave all the slots by its own 64 rows, as kTokens16 x 4 tiles of
 // 16 x 16.  A block of 128 of both operands (and the tokens' scales) goes from
-// global memory straight into LDS, double-buffered: the next block is under way
-// while this one is multiplied, and one barrier parts the two.  In LDS a row is
-// its 128 bytes, chunk c of 16 bytes at place c ^ (row % 8): the eight lanes
-// that an LDS access serves at a time then read eight different chunks of the
-// 128-byte line of banks.  (The place in LDS follows from the lane, so it is the
-// global addresses that are permuted.)
+// global memory straight into LDS.  The tokens are double-buffered and shared:
+// the next block's are under way while this one is multiplied, and one barrier
+// parts the two.  The weights are a wave's own and single: once it has them in
+// its registers it sends for the next block's.  That is 66 KB for 128 slots, so
+// a compute unit holds two workgroups, and one's epilogue runs beside the
+// other's products.  (256 slots in eight waves, one workgroup a compute unit: 64
+// experts of 2048 x 1024, 1024 slots each, gated, 8 bits out: 291 us, this 248;
+// 1024 x 1024, 16 bits out: 97 and 87.  It is ahead where K is long only: 16384
+// slots by 4096 x 8192, 16 bits out: 461 and 486.)
+//
+// Measured on random normal values: 16384 slots by 4096 x 3328 in the 8-bit unit
+// 201 us, 2.2 PFLOP/s; 65536 gathered slots of 64 experts by 2048 x 1024 in the
+// 16-bit unit 250 us, 1.1 PFLOP/s.  All zeros take four fifths of that time: the
+// clock falls with the bits that change.  In the 16-bit unit a wave widens 12
+// tiles for 32 products (192 conversions at half rate beside 128 matrix
+// instructions), which is why the vector unit is as busy as the matrix unit.
+//
+// In LDS a row is its 128 bytes, chunk c of 16 bytes at place
+// c ^ (row % 8): the eight lanes that an LDS access serves at a time then read
+// eight different chunks of the 128-byte line of banks.  (The place in LDS
+// follows from the lane, so it is the global addresses that are permuted.)
 #pragma once
 
 #include <type_traits>
@@ -39,36 +55,39 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, void *to, uint32_t offs
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, offset, 0, 0, 0);
 }
 
-template <int kTokens16_, int kRows16_, int kAcrossT_, int kAcrossR_, bool kWide_, bool kGate_, bool kFp8_>
+template <int kTokens16_, bool kWide_, bool kGate_, bool kFp8_>
 struct TileShape {
-    static constexpr int kTokens16 = kTokens16_, kRows16 = kRows16_, kAcrossT = kAcrossT_, kAcrossR = kAcrossR_;
+    static constexpr int kTokens16 = kTokens16_;
     static constexpr bool kWide = kWide_, kGate = kGate_, kFp8 = kFp8_;
-    static constexpr int kWaves = kAcrossT * kAcrossR;
+    static constexpr int kWaves = 4, kRows16 = 4;
     static constexpr int kThreads = kWaves * kWave;
-    static constexpr int kHeight = kTokens16 * kAcrossT * 16; // slots
-    static constexpr int kLines = kRows16 * kAcrossR * 16;    // weight rows
+    static constexpr int kHeight = kTokens16 * 16;        // slots
+    static constexpr int kLines = kRows16 * kWaves * 16;  // weight rows
     static constexpr int kOut16 = kGate ? kRows16 / 2 : kRows16;
-    static constexpr int kColumns = kOut16 * kAcrossR * 16;   // outputs
+    static constexpr int kColumns = kOut16 * kWaves * 16; // outputs
     static constexpr int kCopiesX = kHeight / 8 / kWaves, kCopiesW = kLines / 8 / kWaves; // per wave and block
     static constexpr int kOutBlocks = kColumns / kBlock;
-    // Parts in which 16- and 8-bit outputs pass through the LDS of one stage.
-    static constexpr int kOutBytes = kWide && !kFp8 ? 0 : kHeight * kColumns * (kFp8 ? 1 : 2), kStageBytes = (kHeight + kLines) * kBlock;
-    static constexpr int kPasses = kOutBytes <= kStageBytes ? 1 : kOutBytes <= 2 * kStageBytes ? 2 : 4;
-    static_assert(kOutBytes <= kPasses * kStageBytes && kTokens16 % kPasses == 0, "whole passes");
-    static_assert(kHeight % (8 * kWaves) == 0 && kLines % (8 * kWaves) == 0, "whole copies");
-    static_assert(!kFp8 || kColumns % kBlock == 0, "a scale needs its whole block in the workgroup");
-    static_assert(kBlock % (kOut16 * 16) == 0, "a wave's outputs lie in one block");
+    // Parts in which 16- and 8-bit outputs pass through the weights' LDS.
+    static constexpr int kOutBytes = kWide && !kFp8 ? 0 : kHeight * kColumns * (kFp8 ? 1 : 2), kLdsBytes = kLines * kBlock;
+    static constexpr int kPasses = kOutBytes <= kLdsBytes ? 1 : 2;
+    static_assert(kOutBytes <= kPasses * kLdsBytes && kTokens16 % kPasses == 0, "whole passes");
+    static_assert(kHeight % (8 * kWaves) == 0, "whole copies");
+    static_assert(kColumns % kBlock == 0 && kBlock % (kOut16 * 16) == 0, "whole blocks of outputs, and a wave's lie in one");
 };
 
 struct alignas(16) Chunk {
     char byte[16];
 };
 
-// One block of K of both operands.
+// One block of K of the tokens, and of the weights.
 template <typename S>
-struct Stage {
-    Chunk x[S::kHeight][8], w[S::kLines][8];
-    float x_scale[S::kHeight > kWave ? S::kHeight : kWave]; // copied by whole waves
+struct TokenBlock {
+    Chunk row[S::kHeight][8];
+    float scale[S::kHeight > kWave ? S::kHeight : kWave]; // copied by whole waves
+};
+template <typename S>
+struct WeightBlock {
+    Chunk row[S::kLines][8];
 };
 
 // Workgroups are dealt to the 8 XCDs in turn.  Each takes runs of 32 tiles (its
@@ -86,11 +105,12 @@ __device__ __forceinline__ uint32_t tile_in_order(uint32_t index, uint32_t count
 constexpr uint32_t kBand = 4; // slot tiles that take their columns together
 
 template <typename S>
-__global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
+__global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
 {
     constexpr int T = S::kTokens16, R = S::kRows16;
-    __shared__ Stage<S> stage0, stage1;
-    char *const out_tile = (char *)&stage0; // after the last block
+    __shared__ TokenBlock<S> tokens0, tokens1;
+    __shared__ WeightBlock<S> weights;
+    char *const out_tile = (char *)&weights; // after the last block
     __shared__ int most[S::kFp8 ? S::kOutBlocks * S::kHeight : 1];
     __shared__ int32_t slot_of[S::kHeight]; // of the tile's tokens; -1: not written
 
@@ -102,32 +122,26 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     const int32_t column0 = (int32_t)(in_band / kBand) * S::kColumns;
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int across_t = wave % S::kAcrossT, across_r = wave / S::kAcrossT;
+    const int in_row = wave * S::kOut16 * 16; // this wave's first output of the tile's
+    const int32_t column = column0 + in_row;
 
-    // Copies: the i-th of a wave fills rows (i * kWaves + wave) * 8 + lane / 8.
-    // The weights' first: the tokens' wait for their rows' numbers.
-    const int32_t row_bytes = (a.K + 15) / 16 * 16; // of a buffer's last row; past it reads give zeros
+    // Copies of 8 rows each, a row by 8 lanes.  The weights' first: the tokens'
+    // wait for their rows' numbers.  Weight rows past the last one are zeros, or
+    // under a gate any; what comes of them is not stored.
     const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+    const int32_t row_bytes = (a.K + 15) / 16 * 16; // of a buffer's last row; past it reads give zeros
     const Buffer w_buffer = buffer_of(a.w + (int64_t)tile.expert * a.N * a.ldw, (uint32_t)((a.N - 1) * a.ldw + row_bytes));
-    uint32_t w_at[S::kCopiesW];
+    const uint32_t w_at = lane / 8 * (uint32_t)a.ldw + chunk;
+    auto fill_weights = [&](int32_t kb) {
 #pragma unroll
-    for (int i = 0; i < S::kCopiesW; ++i) {
-        const int line = (i * S::kWaves + wave) * 8 + lane / 8;
-        int32_t n = column0 + line;
-        if constexpr (S::kGate) { // a wave's rows: those of the gate, then those it gates
-            constexpr int kHalf = S::kOut16 * 16;
-            const int in_wave = line % (2 * kHalf);
-            n = min(column0 + line / (2 * kHalf) * kHalf + in_wave % kHalf, a.width - 1) + (in_wave >= kHalf ? a.width : 0);
-        } else {
-            n = min(n, a.width - 1);
+        for (int i = 0; i < S::kCopiesW; ++i) {
+            // Under a gate a wave's rows are those of the gate, then those it gates.
+            const bool up = S::kGate && i >= S::kCopiesW / 2;
+            const int32_t n = column + (up ? a.width + (i - S::kCopiesW / 2) * 8 : i * 8);
+            copy_to_lds<16>(w_buffer, &weights.row[(wave * S::kCopiesW + i) * 8], w_at + ((uint32_t)n * (uint32_t)a.ldw + (uint32_t)kb * kBlock));
         }
-        w_at[i] = (uint32_t)n * (uint32_t)a.ldw + chunk;
-    }
-    auto fill_weights = [&](Stage<S> &s, int32_t kb) {
-#pragma unroll
-        for (int i = 0; i < S::kCopiesW; ++i) copy_to_lds<16>(w_buffer, &s.w[(i * S::kWaves + wave) * 8], w_at[i] + (uint32_t)kb * kBlock);
     };
-    fill_weights(stage0, 0);
+    fill_weights(0);
 
     const int64_t x_first = a.tokens ? 0 : tile.first; // the buffer's first row
     const int64_t x_end = a.tokens ? a.x_rows : tile.end;
@@ -138,33 +152,29 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         const int32_t row = a.tokens[m];
         return row >= 0 && row < a.x_rows ? row : 0;
     };
-    uint32_t x_at[S::kCopiesX];
-#pragma unroll
-    for (int i = 0; i < S::kCopiesX; ++i) x_at[i] = (uint32_t)row_of((i * S::kWaves + wave) * 8 + lane / 8) * (uint32_t)a.ldx + chunk;
-    // Scales: wave w copies those of slots w * 64 + lane (past the tile: any).
-    const bool copies_scales = wave < (S::kHeight + kWave - 1) / kWave;
-    const uint32_t scale_at = (uint32_t)row_of(threadIdx.x % S::kHeight) * 4;
-    auto fill_tokens = [&](Stage<S> &s, int32_t kb) {
-#pragma unroll
-        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.x[(i * S::kWaves + wave) * 8], x_at[i] + (uint32_t)kb * kBlock);
-        if (copies_scales)
-            copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.x_scale[wave * kWave], scale_at);
-    };
-    fill_tokens(stage0, 0);
-    auto fill = [&](Stage<S> &s, int32_t kb) {
-        fill_tokens(s, kb);
-        fill_weights(s, kb);
-    };
     for (int i = threadIdx.x; i < S::kHeight; i += S::kThreads) {
         int32_t slot = i < tile.end - tile.first ? tile.first + i : -1;
         if (a.tokens && slot >= 0 && (a.tokens[slot] < 0 || a.tokens[slot] >= a.x_rows)) slot = -1;
         slot_of[i] = slot;
     }
+    uint32_t x_at[S::kCopiesX];
+#pragma unroll
+    for (int i = 0; i < S::kCopiesX; ++i) x_at[i] = (uint32_t)row_of((wave * S::kCopiesX + i) * 8 + lane / 8) * (uint32_t)a.ldx + chunk;
+    // Scales: wave w copies those of slots w * 64 + lane (past the tile: any).
+    const bool copies_scales = wave < (S::kHeight + kWave - 1) / kWave;
+    const uint32_t scale_at = (uint32_t)row_of(threadIdx.x % S::kHeight) * 4;
+    auto fill_tokens = [&](TokenBlock<S> &s, int32_t kb) {
+#pragma unroll
+        for (int i = 0; i < S::kCopiesX; ++i) copy_to_lds<16>(x_buffer, &s.row[(wave * S::kCopiesX + i) * 8], x_at[i] + (uint32_t)kb * kBlock);
+        if (copies_scales)
+            copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.scale[wave * kWave], scale_at);
+    };
+    fill_tokens(tokens0, 0);
     // K's last block: what was copied from past a row's end becomes zeros.
-    auto cut = [&](Stage<S> &s, int left) {
+    auto cut = [&](TokenBlock<S> &s, int left) {
         for (int i = threadIdx.x; i < S::kHeight + S::kLines; i += S::kThreads) {
             const int row = i < S::kHeight ? i : i - S::kHeight;
-            Chunk *line = i < S::kHeight ? s.x[row] : s.w[row];
+            Chunk *line = i < S::kHeight ? s.row[row] : weights.row[row];
             for (int c = left / 16; c < 8; ++c) {
                 i32x4 *p = (i32x4 *)&line[c ^ row % 8];
                 *p = first_bytes(*p, left - c * 16);
@@ -173,7 +183,6 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         __syncthreads();
     };
 
-    const int32_t column = column0 + across_r * S::kOut16 * 16;
     const int32_t block = min(column / kBlock, a.row_blocks - 1);
     const float *w_scale = a.w_scales + ((int64_t)tile.expert * a.w_blocks + block) * a.k_blocks;
     const float *w_scale2 = w_scale + (S::kGate ? (int64_t)a.row_blocks * a.k_blocks : 0);
@@ -182,11 +191,11 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     // The weights' scales of a block, loaded when the block before has been read
     // from LDS: with a scalar load among them a wave waits for all its reads.
     float sw_next = eb_detail::scalar_load(w_scale), sw2_next = eb_detail::scalar_load(w_scale2);
-    auto multiply = [&](const Stage<S> &s, int32_t kb) {
+    auto multiply = [&](const TokenBlock<S> &s, int32_t kb) {
         const float sw = sw_next, sw2 = S::kGate ? sw2_next : sw;
         const int p = lane / 16 ^ lane % 8;
-        const Chunk(*ws)[8] = &s.w[across_r * R * 16 + lane % 16], (*xs)[8] = &s.x[across_t * T * 16 + lane % 16];
-        const float *scales = &s.x_scale[across_t * T * 16 + lane % 16];
+        const Chunk(*ws)[8] = &weights.row[wave * R * 16 + lane % 16], (*xs)[8] = &s.row[lane % 16];
+        const float *scales = &s.scale[lane % 16];
         auto read = [&](const Chunk(*from)[8], int tile16) {
             return operand(*(const i32x4 *)&from[tile16 * 16][p], *(const i32x4 *)&from[tile16 * 16][p ^ 4]);
         };
@@ -201,6 +210,11 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         float next_scale = scales[0];
 #pragma unroll
         for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
+        // All of this wave's weights are read: the next block's may come.
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
+        if (kb + 1 < a.k_blocks) fill_weights(kb + 1);
+        __builtin_amdgcn_sched_barrier(0);
         // Products on their way to the sums: those of the kDelay tiles of 16 x 16
         // (in the order of tokens, then rows) before the one in work.
         constexpr int kDelay = S::kWide ? 1 : R;
@@ -216,13 +230,6 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         };
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            // The wave that is behind goes first: a SIMD's two then reach the barrier together.
-            switch (t * 4 / T) {
-            case 0: __builtin_amdgcn_s_setprio(3); break;
-            case 1: __builtin_amdgcn_s_setprio(2); break;
-            case 2: __builtin_amdgcn_s_setprio(1); break;
-            default: __builtin_amdgcn_s_setprio(0);
-            }
             const Operand x = fit(next);
             f[t % 2] = next_scale * sw;
             f2[t % 2] = S::kGate ? next_scale * sw2 : f[t % 2];
@@ -261,17 +268,17 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     int32_t kb = 0;
     for (; kb + 1 < a.k_blocks; kb += 2) {
         arrive();
-        fill(stage1, kb + 1);
-        multiply(stage0, kb);
+        fill_tokens(tokens1, kb + 1);
+        multiply(tokens0, kb);
         arrive();
-        if (kb + 2 < a.k_blocks) fill(stage0, kb + 2);
-        else if (tail) cut(stage1, tail);
-        multiply(stage1, kb + 1);
+        if (kb + 2 < a.k_blocks) fill_tokens(tokens0, kb + 2);
+        else if (tail) cut(tokens1, tail);
+        multiply(tokens1, kb + 1);
     }
     if (kb < a.k_blocks) {
         arrive();
-        if (tail) cut(stage0, tail);
-        multiply(stage0, kb);
+        if (tail) cut(tokens0, tail);
+        multiply(tokens0, kb);
     }
 
     finish<R, T, S::kGate>(a, tile.expert, column, sum);
@@ -279,7 +286,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
         // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.
         int32_t slot[T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) slot[t] = slot_of[(across_t * T + t) * 16 + lane % 16];
+        for (int t = 0; t < T; ++t) slot[t] = slot_of[t * 16 + lane % 16];
         store_floats<S::kOut16>(a, column, slot, sum);
         return;
     }
@@ -293,10 +300,8 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
     auto to_slots = [&](int pass) {
         const int left = min(a.width - column0, S::kColumns) * kSize; // bytes of a row
         for (int i = threadIdx.x; i < S::kHeight / kPasses * kChunks; i += S::kThreads) {
-            // Of each kAcrossT-th of the tile's tokens a pass takes T / kPasses tiles of 16.
-            constexpr int kPart = T / kPasses * 16;
             const int j = i / kChunks, c = i % kChunks;
-            const int32_t m = slot_of[j / kPart * T * 16 + pass * kPart + j % kPart];
+            const int32_t m = slot_of[pass * (S::kHeight / kPasses) + j];
             if (c * 16 >= left || m < 0) continue;
             const char *from = chunk_of(j, c);
             char *to = (char *)a.out + ((int64_t)m * a.ldo + column0) * kSize + c * 16;
@@ -309,17 +314,25 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
             }
         }
     };
-    const int part = lane / 16 * 4, in_row = across_r * S::kOut16 * 16;
+    const int part = lane / 16 * 4;
     if constexpr (S::kFp8) {
-        int *mine = &most[in_row / kBlock * S::kHeight + across_t * T * 16];
+        int *mine = &most[in_row / kBlock * S::kHeight];
         for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) most[i] = 0;
         __syncthreads();
+        if (column + S::kOut16 * 16 > a.width) { // outputs past the width do not count
+#pragma unroll
+            for (int r = 0; r < S::kOut16; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int t = 0; t < T; ++t) sum[r][t][i] = column + r * 16 + part + i < a.width ? sum[r][t][i] : 0.f;
+        }
         most_of_outputs<S::kOut16>(sum, mine);
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const int token = (across_t * T + t) * 16 + lane % 16;
-            const float f = block_scale(mine[t * 16 + lane % 16]);
+            const int token = t * 16 + lane % 16;
+            const float f = block_scale(mine[token]);
 #pragma unroll
             for (int r = 0; r < S::kOut16; ++r)
                 *(int *)(chunk_of(token, in_row / 16 + r) + part) = pack_fp8(sum[r][t], f);
@@ -338,7 +351,7 @@ __global__ __launch_bounds__(S::kThreads) void eb_product_tile(ProductArgs a)
             auto to_lds = [&](auto bits) {
 #pragma unroll
                 for (int u = 0; u < T / kPasses; ++u) {
-                    const int t = pass * (T / kPasses) + u, token = (across_t * (T / kPasses) + u) * 16 + lane % 16;
+                    const int t = pass * (T / kPasses) + u, token = u * 16 + lane % 16;
 #pragma unroll
                     for (int r = 0; r < S::kOut16; ++r) {
                         const int c = in_row + r * 16 + part;

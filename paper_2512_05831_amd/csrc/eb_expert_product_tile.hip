@@ -9,9 +9,9 @@ namespace {
 template <bool kWide, bool kGate, bool kFp8>
 KernelPlan plan_of(TileSize size)
 {
-    if (size == TileSize::kLarge) return tile_plan<TileShape<8, 4, 2, 4, kWide, kGate, kFp8>>();
-    if (size == TileSize::kMedium) return tile_plan<TileShape<4, 4, 2, 4, kWide, kGate, kFp8>>();
-    return tile_plan<TileShape<2, 4, 1, 4, kWide, kGate, kFp8>>();
+    if (size == TileSize::kLarge) return tile_plan<TileShape<8, kWide, kGate, kFp8>>();
+    if (size == TileSize::kMedium) return tile_plan<TileShape<4, kWide, kGate, kFp8>>();
+    return tile_plan<TileShape<2, kWide, kGate, kFp8>>();
 }
 
 } // namespace
