@@ -303,8 +303,8 @@ struct KernelPlan {
     int32_t band;    // the grid holds a multiple of so many slot tiles
 };
 
-// Slots of a workgroup: 128, 64, 32 (by 256 weight rows).
-enum class TileSize { kLarge, kMedium, kSmall };
+// Slots of a workgroup: 256, 128, 64, 32 (by 256 weight rows).
+enum class TileSize { kHuge, kLarge, kMedium, kSmall };
 
 KernelPlan stream_kernel(bool gate, bool fp8);
 KernelPlan tile_kernel(bool gate, int32_t out_type, TileSize size);

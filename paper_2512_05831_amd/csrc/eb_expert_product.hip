@@ -32,7 +32,10 @@ int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1
 //   (1000 x 1520: 200 slots 9.4 and 14.4; 16 experts of 2048 x 1024, 16 slots: 15.5
 //   and 11.3), with both it holds 256 rows of all K as a tile does: 45.9 and 27.8.
 //   Larger tiles read their operands less often, smaller ones fill the GPU and
-//   waste less of an expert's last tile.  16 experts of 2048 x 1024: large against
+//   waste less of an expert's last tile.  Huge against large, 16384 slots of one
+//   expert of 4096 x 3328: 195 and 213 in the 8-bit unit, 346 and 363 in the 16-bit
+//   one; 64 experts of 2048 x 3328, 512 slots each: 287 and 272, gated with 8-bit
+//   outputs 470 and 417; 2048 slots each: equal within 1 %.  16 experts of 2048 x 1024: large against
 //   medium, 8-bit unit, 200 slots (256 tiles) 16.8 and 17.8, 900 slots 43.6 and
 //   46.2; 16-bit unit 200 slots 33.8 and 25.0, 400 slots (512 tiles) 41.6 and 44.0.
 //   Medium against small: 8-bit unit, 100 slots (256 tiles) 13.1 and 13.4, 200
@@ -46,12 +49,14 @@ KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t width, int64_t
     // gathered) and an expert's weights with 32 bits.
     constexpr int64_t kMost32 = (int64_t)1 << 32;
     const KernelPlan stream = stream_kernel(gate, fp8);
-    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 128) * ldx >= kMost32) return stream;
+    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 256) * ldx >= kMost32) return stream;
     const int64_t mean = (M + E - 1) / E;
     auto tiles = [&](const KernelPlan &p) {
         return std::min<int64_t>(E, M) * ((mean + p.height - 1) / p.height) * ((width + p.columns - 1) / p.columns);
     };
     if (!(gate && fp8) && tiles(stream) * (fp8 ? 8 : gate ? 2 : 1) <= (wide ? 1536 : 1024)) return stream;
+    const KernelPlan huge = tile_kernel(gate, out_type, TileSize::kHuge);
+    if (mean >= 4096 && tiles(huge) >= 512) return huge;
     const KernelPlan large = tile_kernel(gate, out_type, TileSize::kLarge);
     if (tiles(large) >= (wide ? 512 : 256)) return large;
     const KernelPlan medium = tile_kernel(gate, out_type, TileSize::kMedium);

@@ -1,30 +1,29 @@
 // eb_expert_product for many slots per expert: bound by the matrix units and, on
 // the way to them, by the power they may draw.
 //
-// A workgroup of four waves takes kTokens16 * 16 slots of an expert by 256 weight
-// rows, a wave all the slots by its own 64 rows, as kTokens16 x 4 tiles of
-// 16 x 16.  A block of 128 of both operands (and the tokens' scales) goes from
-// global memory straight into LDS.  The tokens are double-buffered and shared:
-// the next block's are under way while this one is multiplied, and one barrier
-// parts the two.  The weights are a wave's own and single: once it has them in
-// its registers it sends for the next block's.  That is 66 KB for 128 slots, so
-// a compute unit holds two workgroups, and one's epilogue runs beside the
-// other's products.  (256 slots in eight waves, one workgroup a compute unit: 64
-// experts of 2048 x 1024, 1024 slots each, gated, 8 bits out: 291 us, this 248;
-// 1024 x 1024, 16 bits out: 97 and 87.  It is ahead where K is long only: 16384
-// slots by 4096 x 8192, 16 bits out: 461 and 486.)
+// A workgroup takes kTokens16 * kAcrossT * 16 slots of an expert by 256 weight
+// rows, a wave kTokens16 x 4 tiles of 16 x 16, four waves side by side along the
+// rows.  A block of 128 of both operands (and the tokens' scales) goes from global
+// memory straight into LDS, the next block's while this one is multiplied, and
+// one barrier parts the two.
+//   Four waves (kAcrossT 1): the tokens are double-buffered; the weights are a
+// wave's own and single: once it has them in its registers it sends for the next
+// block's.  That is 66 KB for 128 slots, so a compute unit holds two workgroups,
+// and one's epilogue runs beside the other's products.
+//   Eight waves (kAcrossT 2, 256 slots): two stages of both operands, 134 KB, one
+// workgroup a compute unit, two thirds of the copies for the same products.
+//   In LDS a row is its 128 bytes, chunk c of 16 bytes at place c ^ (row % 8): the
+// eight lanes that an LDS access serves at a time then read eight different
+// chunks of the 128-byte line of banks.  (The place in LDS follows from the lane,
+// so it is the global addresses that are permuted.)
 //
-// Measured on random normal values: 16384 slots by 4096 x 3328 in the 8-bit unit
-// 201 us, 2.2 PFLOP/s; 65536 gathered slots of 64 experts by 2048 x 1024 in the
-// 16-bit unit 250 us, 1.1 PFLOP/s.  All zeros take four fifths of that time: the
-// clock falls with the bits that change.  In the 16-bit unit a wave widens 12
-// tiles for 32 products (192 conversions at half rate beside 128 matrix
-// instructions), which is why the vector unit is as busy as the matrix unit.
-//
-// In LDS a row is its 128 bytes, chunk c of 16 bytes at place
-// c ^ (row % 8): the eight lanes that an LDS access serves at a time then read
-// eight different chunks of the 128-byte line of banks.  (The place in LDS
-// follows from the lane, so it is the global addresses that are permuted.)
+// Measured on random normal values in long runs: 16384 slots by 4096 x 3328 in the
+// 8-bit unit 195 us, 2.3 PFLOP/s (four waves 212); 65536 gathered slots of 64
+// experts by 2048 x 1024, gated, in the 16-bit unit 264 us, 1.04 PFLOP/s (eight
+// waves 286).  Zeros take four fifths of that time: the clock falls with the bits
+// that change, which is also why fewer copies count.  In the 16-bit unit a wave
+// widens 12 tiles for 32 products (192 conversions at half rate beside 128 matrix
+// instructions): the vector unit is as busy as the matrix unit.
 #pragma once
 
 #include <type_traits>
@@ -55,23 +54,26 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, void *to, uint32_t offs
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, offset, 0, 0, 0);
 }
 
-template <int kTokens16_, bool kWide_, bool kGate_, bool kFp8_>
+template <int kTokens16_, int kAcrossT_, bool kWide_, bool kGate_, bool kFp8_>
 struct TileShape {
-    static constexpr int kTokens16 = kTokens16_;
+    static constexpr int kTokens16 = kTokens16_, kAcrossT = kAcrossT_;
     static constexpr bool kWide = kWide_, kGate = kGate_, kFp8 = kFp8_;
-    static constexpr int kWaves = 4, kRows16 = 4;
+    static constexpr bool kOwn = kAcrossT == 1; // a wave's weight rows are its own
+    static constexpr int kAcrossR = 4, kRows16 = 4;
+    static constexpr int kWaves = kAcrossT * kAcrossR;
     static constexpr int kThreads = kWaves * kWave;
-    static constexpr int kHeight = kTokens16 * 16;        // slots
-    static constexpr int kLines = kRows16 * kWaves * 16;  // weight rows
+    static constexpr int kHeight = kTokens16 * kAcrossT * 16; // slots
+    static constexpr int kLines = kRows16 * kAcrossR * 16;    // weight rows
     static constexpr int kOut16 = kGate ? kRows16 / 2 : kRows16;
-    static constexpr int kColumns = kOut16 * kWaves * 16; // outputs
+    static constexpr int kColumns = kOut16 * kAcrossR * 16;   // outputs
     static constexpr int kCopiesX = kHeight / 8 / kWaves, kCopiesW = kLines / 8 / kWaves; // per wave and block
     static constexpr int kOutBlocks = kColumns / kBlock;
-    // Parts in which 16- and 8-bit outputs pass through the weights' LDS.
-    static constexpr int kOutBytes = kWide && !kFp8 ? 0 : kHeight * kColumns * (kFp8 ? 1 : 2), kLdsBytes = kLines * kBlock;
+    // Parts in which 16- and 8-bit outputs pass through LDS: that of the weights, or of a stage.
+    static constexpr int kOutBytes = kWide && !kFp8 ? 0 : kHeight * kColumns * (kFp8 ? 1 : 2);
+    static constexpr int kLdsBytes = (kLines + (kOwn ? 0 : kHeight)) * kBlock;
     static constexpr int kPasses = kOutBytes <= kLdsBytes ? 1 : 2;
     static_assert(kOutBytes <= kPasses * kLdsBytes && kTokens16 % kPasses == 0, "whole passes");
-    static_assert(kHeight % (8 * kWaves) == 0, "whole copies");
+    static_assert(kHeight % (8 * kWaves) == 0 && kLines % (8 * kWaves) == 0, "whole copies");
     static_assert(kColumns % kBlock == 0 && kBlock % (kOut16 * 16) == 0, "whole blocks of outputs, and a wave's lie in one");
 };
 
@@ -88,6 +90,11 @@ struct TokenBlock {
 template <typename S>
 struct WeightBlock {
     Chunk row[S::kLines][8];
+};
+template <typename S>
+struct Stage {
+    TokenBlock<S> tokens;
+    WeightBlock<S> weights;
 };
 
 // Workgroups are dealt to the 8 XCDs in turn.  Each takes runs of 32 tiles (its
@@ -108,9 +115,21 @@ template <typename S>
 __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
 {
     constexpr int T = S::kTokens16, R = S::kRows16;
-    __shared__ TokenBlock<S> tokens0, tokens1;
-    __shared__ WeightBlock<S> weights;
-    char *const out_tile = (char *)&weights; // after the last block
+    // What is copied to while another part is read is a variable of its own: the
+    // compiler then sees that those reads need not wait for the copies.
+    __shared__ std::conditional_t<S::kOwn, TokenBlock<S>, Stage<S>> part0, part1;
+    __shared__ std::conditional_t<S::kOwn, WeightBlock<S>, Chunk> own;
+    auto tokens_of = [](auto &part) -> TokenBlock<S> & {
+        if constexpr (S::kOwn) return part;
+        else return part.tokens;
+    };
+    auto weights_of = [&](auto &part) -> WeightBlock<S> & {
+        if constexpr (S::kOwn) return own;
+        else return part.weights;
+    };
+    TokenBlock<S> &tokens0 = tokens_of(part0), &tokens1 = tokens_of(part1);
+    WeightBlock<S> &weights0 = weights_of(part0), &weights1 = weights_of(part1);
+    char *const out_tile = S::kOwn ? (char *)&own : (char *)&part0; // after the last block
     __shared__ int most[S::kFp8 ? S::kOutBlocks * S::kHeight : 1];
     __shared__ int32_t slot_of[S::kHeight]; // of the tile's tokens; -1: not written
 
@@ -122,7 +141,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     const int32_t column0 = (int32_t)(in_band / kBand) * S::kColumns;
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int in_row = wave * S::kOut16 * 16; // this wave's first output of the tile's
+    const int across_r = wave % S::kAcrossR, across_t = wave / S::kAcrossR;
+    const int in_row = across_r * S::kOut16 * 16; // this wave's first output of the tile's
     const int32_t column = column0 + in_row;
 
     // Copies of 8 rows each, a row by 8 lanes.  The weights' first: the tokens'
@@ -132,16 +152,19 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     const int32_t row_bytes = (a.K + 15) / 16 * 16; // of a buffer's last row; past it reads give zeros
     const Buffer w_buffer = buffer_of(a.w + (int64_t)tile.expert * a.N * a.ldw, (uint32_t)((a.N - 1) * a.ldw + row_bytes));
     const uint32_t w_at = lane / 8 * (uint32_t)a.ldw + chunk;
-    auto fill_weights = [&](int32_t kb) {
+    auto fill_weights = [&](WeightBlock<S> &weights, int32_t kb) {
 #pragma unroll
         for (int i = 0; i < S::kCopiesW; ++i) {
-            // Under a gate a wave's rows are those of the gate, then those it gates.
-            const bool up = S::kGate && i >= S::kCopiesW / 2;
-            const int32_t n = column + (up ? a.width + (i - S::kCopiesW / 2) * 8 : i * 8);
-            copy_to_lds<16>(w_buffer, &weights.row[(wave * S::kCopiesW + i) * 8], w_at + ((uint32_t)n * (uint32_t)a.ldw + (uint32_t)kb * kBlock));
+            const int line = (wave * S::kCopiesW + i) * 8;
+            // Under a gate the rows that a wave multiplies are those of the gate, then those it gates.
+            constexpr int kLinesOf = R * 16;
+            const int of = line / kLinesOf * S::kOut16 * 16, at = line % kLinesOf;
+            const bool up = S::kGate && at >= kLinesOf / 2;
+            const int32_t n = column0 + of + (up ? a.width + at - kLinesOf / 2 : at);
+            copy_to_lds<16>(w_buffer, &weights.row[line], w_at + ((uint32_t)n * (uint32_t)a.ldw + (uint32_t)kb * kBlock));
         }
     };
-    fill_weights(0);
+    fill_weights(weights0, 0);
 
     const int64_t x_first = a.tokens ? 0 : tile.first; // the buffer's first row
     const int64_t x_end = a.tokens ? a.x_rows : tile.end;
@@ -170,8 +193,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
             copy_to_lds<4>(buffer_of(a.x_scales + kb * a.ldxs + x_first, (uint32_t)(x_end - x_first) * 4), &s.scale[wave * kWave], scale_at);
     };
     fill_tokens(tokens0, 0);
+    auto fill = [&](TokenBlock<S> &s, WeightBlock<S> &weights, int32_t kb) {
+        fill_tokens(s, kb);
+        if constexpr (!S::kOwn) fill_weights(weights, kb);
+    };
     // K's last block: what was copied from past a row's end becomes zeros.
-    auto cut = [&](TokenBlock<S> &s, int left) {
+    auto cut = [&](TokenBlock<S> &s, WeightBlock<S> &weights, int left) {
         for (int i = threadIdx.x; i < S::kHeight + S::kLines; i += S::kThreads) {
             const int row = i < S::kHeight ? i : i - S::kHeight;
             Chunk *line = i < S::kHeight ? s.row[row] : weights.row[row];
@@ -191,11 +218,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     // The weights' scales of a block, loaded when the block before has been read
     // from LDS: with a scalar load among them a wave waits for all its reads.
     float sw_next = eb_detail::scalar_load(w_scale), sw2_next = eb_detail::scalar_load(w_scale2);
-    auto multiply = [&](const TokenBlock<S> &s, int32_t kb) {
+    auto multiply = [&](const TokenBlock<S> &s, WeightBlock<S> &weights, int32_t kb) {
         const float sw = sw_next, sw2 = S::kGate ? sw2_next : sw;
         const int p = lane / 16 ^ lane % 8;
-        const Chunk(*ws)[8] = &weights.row[wave * R * 16 + lane % 16], (*xs)[8] = &s.row[lane % 16];
-        const float *scales = &s.scale[lane % 16];
+        const Chunk(*ws)[8] = &weights.row[across_r * R * 16 + lane % 16], (*xs)[8] = &s.row[across_t * T * 16 + lane % 16];
+        const float *scales = &s.scale[across_t * T * 16 + lane % 16];
         auto read = [&](const Chunk(*from)[8], int tile16) {
             return operand(*(const i32x4 *)&from[tile16 * 16][p], *(const i32x4 *)&from[tile16 * 16][p ^ 4]);
         };
@@ -210,11 +237,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
         float next_scale = scales[0];
 #pragma unroll
         for (int r = 0; r < R; ++r) w[r] = fit(read(ws, r));
-        // All of this wave's weights are read: the next block's may come.
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
-        if (kb + 1 < a.k_blocks) fill_weights(kb + 1);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (S::kOwn) { // all of this wave's weights are read: the next block's may come
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
+            if (kb + 1 < a.k_blocks) fill_weights(weights, kb + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         // Products on their way to the sums: those of the kDelay tiles of 16 x 16
         // (in the order of tokens, then rows) before the one in work.
         constexpr int kDelay = S::kWide ? 1 : R;
@@ -230,6 +258,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
         };
 #pragma unroll
         for (int t = 0; t < T; ++t) {
+            if constexpr (!S::kOwn) {
+                // The wave that is behind goes first: a SIMD's two then reach the barrier together.
+                switch (t * 4 / T) {
+                case 0: __builtin_amdgcn_s_setprio(3); break;
+                case 1: __builtin_amdgcn_s_setprio(2); break;
+                case 2: __builtin_amdgcn_s_setprio(1); break;
+                default: __builtin_amdgcn_s_setprio(0);
+                }
+            }
             const Operand x = fit(next);
             f[t % 2] = next_scale * sw;
             f2[t % 2] = S::kGate ? next_scale * sw2 : f[t % 2];
@@ -268,17 +305,17 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     int32_t kb = 0;
     for (; kb + 1 < a.k_blocks; kb += 2) {
         arrive();
-        fill_tokens(tokens1, kb + 1);
-        multiply(tokens0, kb);
+        fill(tokens1, weights1, kb + 1);
+        multiply(tokens0, weights0, kb);
         arrive();
-        if (kb + 2 < a.k_blocks) fill_tokens(tokens0, kb + 2);
-        else if (tail) cut(tokens1, tail);
-        multiply(tokens1, kb + 1);
+        if (kb + 2 < a.k_blocks) fill(tokens0, weights0, kb + 2);
+        else if (tail) cut(tokens1, weights1, tail);
+        multiply(tokens1, weights1, kb + 1);
     }
     if (kb < a.k_blocks) {
         arrive();
-        if (tail) cut(tokens0, tail);
-        multiply(tokens0, kb);
+        if (tail) cut(tokens0, weights0, tail);
+        multiply(tokens0, weights0, kb);
     }
 
     finish<R, T, S::kGate>(a, tile.expert, column, sum);
@@ -286,7 +323,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
         // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.
         int32_t slot[T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) slot[t] = slot_of[t * 16 + lane % 16];
+        for (int t = 0; t < T; ++t) slot[t] = slot_of[(across_t * T + t) * 16 + lane % 16];
         store_floats<S::kOut16>(a, column, slot, sum);
         return;
     }
@@ -300,8 +337,10 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     auto to_slots = [&](int pass) {
         const int left = min(a.width - column0, S::kColumns) * kSize; // bytes of a row
         for (int i = threadIdx.x; i < S::kHeight / kPasses * kChunks; i += S::kThreads) {
+            // Of each kAcrossT-th of the tile's tokens a pass takes T / kPasses tiles of 16.
+            constexpr int kPart = T / kPasses * 16;
             const int j = i / kChunks, c = i % kChunks;
-            const int32_t m = slot_of[pass * (S::kHeight / kPasses) + j];
+            const int32_t m = slot_of[j / kPart * T * 16 + pass * kPart + j % kPart];
             if (c * 16 >= left || m < 0) continue;
             const char *from = chunk_of(j, c);
             char *to = (char *)a.out + ((int64_t)m * a.ldo + column0) * kSize + c * 16;
@@ -316,7 +355,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
     };
     const int part = lane / 16 * 4;
     if constexpr (S::kFp8) {
-        int *mine = &most[in_row / kBlock * S::kHeight];
+        int *mine = &most[in_row / kBlock * S::kHeight + across_t * T * 16];
         for (int i = threadIdx.x; i < S::kOutBlocks * S::kHeight; i += S::kThreads) most[i] = 0;
         __syncthreads();
         if (column + S::kOut16 * 16 > a.width) { // outputs past the width do not count
@@ -331,8 +370,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const int token = t * 16 + lane % 16;
-            const float f = block_scale(mine[token]);
+            const int token = (across_t * T + t) * 16 + lane % 16;
+            const float f = block_scale(mine[t * 16 + lane % 16]);
 #pragma unroll
             for (int r = 0; r < S::kOut16; ++r)
                 *(int *)(chunk_of(token, in_row / 16 + r) + part) = pack_fp8(sum[r][t], f);
@@ -351,7 +390,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
             auto to_lds = [&](auto bits) {
 #pragma unroll
                 for (int u = 0; u < T / kPasses; ++u) {
-                    const int t = pass * (T / kPasses) + u, token = u * 16 + lane % 16;
+                    const int t = pass * (T / kPasses) + u, token = (across_t * (T / kPasses) + u) * 16 + lane % 16;
 #pragma unroll
                     for (int r = 0; r < S::kOut16; ++r) {
                         const int c = in_row + r * 16 + part;

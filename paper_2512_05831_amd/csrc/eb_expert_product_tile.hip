@@ -9,9 +9,10 @@ namespace {
 template <bool kWide, bool kGate, bool kFp8>
 KernelPlan plan_of(TileSize size)
 {
-    if (size == TileSize::kLarge) return tile_plan<TileShape<8, kWide, kGate, kFp8>>();
-    if (size == TileSize::kMedium) return tile_plan<TileShape<4, kWide, kGate, kFp8>>();
-    return tile_plan<TileShape<2, kWide, kGate, kFp8>>();
+    if (size == TileSize::kHuge) return tile_plan<TileShape<8, 2, kWide, kGate, kFp8>>();
+    if (size == TileSize::kLarge) return tile_plan<TileShape<8, 1, kWide, kGate, kFp8>>();
+    if (size == TileSize::kMedium) return tile_plan<TileShape<4, 1, kWide, kGate, kFp8>>();
+    return tile_plan<TileShape<2, 1, kWide, kGate, kFp8>>();
 }
 
 } // namespace

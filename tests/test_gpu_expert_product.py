@@ -293,3 +293,17 @@ def test_refusals(device):
         three = Case(8, 63, 128, device)
         ex.product(three.x, three.xs, three.w, torch.zeros(2, 1, device=device), act=ex.EB_ACT_SILU_GATE)
     assert e.value.code == eb.EB_ERR_INVALID
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_SILU_GATE])
+@pytest.mark.parametrize("M,N,K,counts", [(8200, 4200, 640, None), (8193, 4100, 424, None), (4097, 8300, 128, None),
+                                          (12400, 3050, 300, [4000, 8299, 101])])
+def test_tiles_of_256_slots(out, act, M, N, K, counts, device):
+    """Calls with many slots per expert, whose last tiles are cut on either side."""
+    case = Case(M, N, K, device, E=1 if counts is None else len(counts), act=act, bias=K != 640, counts=counts, gather=None if counts is None else 1000)
+    got = case.run(out_dtype=out)
+    if out == torch.float8_e4m3fn:
+        close_fp8(*got, case)
+    else:
+        close(got, case, out)
