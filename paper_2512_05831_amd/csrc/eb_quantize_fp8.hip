@@ -3,12 +3,14 @@
 //
 //   scale = max(max|x| / 448, 2^-126),  q = e4m3(x / scale)
 //
-// One read of x, one write of q and the scales: bound by memory.
+// One read of x, one write of q and the scales: bound by memory.  16384 x 3328
+// fp32 values in 40 us where the last level of cache holds some, 6.8 TB/s (a copy of
+// 4 GiB on the same card: 4.7); 2048 x 1024 in 4.2.
 //
 // 1 x 128 blocks: 16 lanes hold a block, 8 values each, so a lane writes 8
 // bytes of q.  A workgroup takes 16 rows and up to kSteps blocks along them:
 // the 16 scales of a block column are neighbours in memory and are written
-// together.
+// together.  One, two, four and eight blocks: 41.2, 40.7, 43.0 and 49.2 us.
 // 128 x 128 blocks: a workgroup holds a block in registers, 64 values a lane.
 
 #include <hip/hip_runtime.h>
@@ -31,7 +33,7 @@ constexpr int kThreads = 256;
 constexpr int kLanes = 16;               // lanes of a 1 x 128 block
 constexpr int kEach = kBlock / kLanes;   // values of a lane
 constexpr int kRows = kThreads / kLanes; // rows of a workgroup
-constexpr int kSteps = 4;                // block columns of a workgroup
+constexpr int kSteps = 2;                // block columns of a workgroup
 
 struct QuantizeArgs {
     const void *x;

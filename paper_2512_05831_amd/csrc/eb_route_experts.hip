@@ -8,22 +8,30 @@
 // choose  L = 16 lanes (64 for many experts) hold a token's E values in
 //         registers, V each, as integers that order like the floats (an
 //         integer maximum takes its other operand straight from another lane).
-//         With 16 lanes and K <= 8: the K-th largest of the lanes' maxima
+//         With 16 lanes and 2 < K <= 8: the K-th largest of the lanes' maxima
 //         bounds the K best values from below, those above it (eleven or so
 //         where K is 8) go to LDS, a lane takes one each and counts the better
 //         ones: about 220 instructions, where K rounds of "largest value left,
 //         lowest expert that has it, out with it" are 680 (16 values a lane).
 //         (Two each where 17 to 32 reach the bound: one token in 25, but then its
 //         whole wave.)  Those rounds are taken where more do, and for other K
-//         and L.  Each workgroup counts its pairs per expert.
+//         and L.  16384 tokens in all: 8 of 256 experts 17.8 us, by rounds 20.9; 6
+//         of 64 13.0 and 13.9; 2 of 128 14.0 and 13.6.  Each workgroup counts its
+//         pairs per expert.
 // scan    exclusive prefix of each expert's counts over the chunks of kTokens
 //         tokens.
 // place   each workgroup ranks its pairs within their experts (in pair order:
 //         the lanes of a wave that hold the same expert find each other by
 //         ballots over the expert's bits) and writes them.
-// A launch costs more than the work of a small batch, so up to kFewTokens
-// tokens one workgroup does all of it, and up to kFewPairs pairs one workgroup
-// scans and places after choose.
+// Choose is bound by vector instructions: 16384 tokens of 256 experts with sigmoid,
+// bias and pairs of groups 16 us (0.85 issued a cycle) for 16.8 MB that a copy would
+// read in 4; scan and place are 4.5 and 5 us of latency there.
+// A launch costs more than the work of a small batch (2.4 us of the caller's time):
+// up to 16 tokens, or 128 of at most 64 experts, one workgroup does all of it (us
+// a call among others: 64 tokens, 6 of 64 experts 11.4, two launches 13.7; on the GPU
+// 6.8 and 7.2; but 64 tokens, 8 of 256 22.5 and 13.8).  Up to kFewPairs pairs one workgroup
+// scans and places after choose (4080 pairs 13.6, three launches 17.5, on the GPU
+// 11.1 each; 7800 pairs 16.1 and 17.7, on the GPU 16.3 and 11.3).
 
 #include <hip/hip_runtime.h>
 
@@ -47,8 +55,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kChooseThreads = 512; // 32 tokens of 16 lanes
 constexpr int kTokens = 32;        // tokens of a chunk
 constexpr int kFewWaves = 16;      // of the workgroup that does all
-constexpr int kFewTokens = 64, kFewPairs = 4096, kFewExperts = 512;
-constexpr int kMostFewPairs = kFewTokens * 64;
+constexpr int kFewTokens = 128, kFewPairs = 4096, kFewExperts = 512;
+constexpr int kMostFewPairs = kFewWaves * 64;
 constexpr int kFilterTop = 8;      // most experts per token for the filter
 constexpr int kMostExperts = 1024;
 constexpr int kMostTop = 64;
@@ -71,6 +79,7 @@ struct RouteArgs {
     int32_t *ids;
     float *weights;
     int32_t *offsets, *tokens, *slots;
+    int32_t each;     // tokens of a workgroup of choose
     uint32_t *counts; // [held][chunks + 1], the total last, or NULL: none are taken
     int64_t chunks;
 };
@@ -300,7 +309,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
     int id_key = kNoneKey;
     id = -1;
     if constexpr (L == 16 && V >= 4) {
-        if (a.K <= kFilterTop) best_by_filter<V>(key, lane, a.K, space, id, id_key);
+        if (a.K > 2 && a.K <= kFilterTop) best_by_filter<V>(key, lane, a.K, space, id, id_key);
         else best_by_rounds<L, V>(key, lane, a.K, id, id_key);
     } else {
         best_by_rounds<L, V>(key, lane, a.K, id, id_key);
@@ -347,8 +356,9 @@ __global__ __launch_bounds__(kChooseThreads, L *V <= 512 ? 4 : 2) void eb_route_
         for (int j = threadIdx.x; j < a.held; j += kChooseThreads) count[j] = 0;
         __syncthreads();
     }
-    for (int p = 0; p < kTokens; p += kPass) {
-        const int64_t n = (int64_t)blockIdx.x * kTokens + p + mine;
+    const int each = kPass >= kTokens ? kTokens : a.each;
+    for (int p = 0; p < each; p += kPass) {
+        const int64_t n = (int64_t)blockIdx.x * each + p + mine;
         if (n >= a.N) break; // ends for whole lane groups; no barrier in the loop
         int id;
         float w;
@@ -579,22 +589,30 @@ __global__ void eb_route_none(int32_t *offsets, int32_t n)
     for (int j = threadIdx.x; j < n; j += blockDim.x) offsets[j] = 0;
 }
 
-// Few tokens: a wave each, for its latency; up to kFewExperts, whose values 16
-// waves' registers hold.
-template <typename T>
-void *few_kernel(int32_t E)
+// Whether one workgroup does it all: a token per wave, or four where 16 lanes hold
+// the experts in four registers each (for more the 16 waves have too few).
+bool is_few(int64_t N, int32_t E, int32_t K)
 {
+    return N <= kFewWaves ? E <= kFewExperts : N <= kFewTokens && N * K <= kMostFewPairs && E <= 64 && K <= 16;
+}
+
+template <typename T>
+void *few_kernel(int64_t N, int32_t E, int32_t K)
+{
+    if (N > 4 && E <= 64 && K <= 16) return (void *)eb_route_few<16, 4, T>;
     if (E <= 64) return (void *)eb_route_few<64, 1, T>;
     if (E <= 128) return (void *)eb_route_few<64, 2, T>;
     if (E <= 256) return (void *)eb_route_few<64, 4, T>;
     return (void *)eb_route_few<64, 8, T>;
 }
 
+int choose_lanes(int32_t E, int32_t K) { return K <= 16 && E <= 256 ? 16 : 64; }
+
 template <typename T>
-void *choose_kernel(bool few, int32_t E, int32_t K)
+void *choose_kernel(bool few, int64_t N, int32_t E, int32_t K)
 {
-    if (few) return few_kernel<T>(E);
-    if (K <= 16 && E <= 256) {
+    if (few) return few_kernel<T>(N, E, K);
+    if (choose_lanes(E, K) == 16) {
         if (E <= 32) return (void *)eb_route_choose<16, 2, T>;
         if (E <= 64) return (void *)eb_route_choose<16, 4, T>;
         if (E <= 128) return (void *)eb_route_choose<16, 8, T>;
@@ -669,15 +687,18 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     a.slots = slots;
     a.counts = needed > 0 ? (uint32_t *)workspace : nullptr;
     a.chunks = chunks_of(N);
-    const bool few = N <= kFewTokens && E <= kFewExperts;
-    void *kernel = dtype == EB_F32 ? choose_kernel<float>(few, E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(few, E, K) : choose_kernel<Bf16>(few, E, K);
+    const bool few = is_few(N, E, K);
+    void *kernel = dtype == EB_F32 ? choose_kernel<float>(few, N, E, K) : dtype == EB_F16 ? choose_kernel<_Float16>(few, N, E, K) : choose_kernel<Bf16>(few, N, E, K);
     void *args[] = {&a};
     auto launch = [&](void *f, int64_t grid, int threads) {
         return hipLaunchKernel(f, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, s);
     };
-    if (a.chunks > std::numeric_limits<uint32_t>::max() / kChooseThreads)
+    // Chunks; few pairs, which are not counted by chunk, by what a workgroup takes at once.
+    a.each = N * K <= kFewPairs ? kChooseThreads / choose_lanes(E, K) : kTokens;
+    const int64_t grid = (N + a.each - 1) / a.each;
+    if (grid > std::numeric_limits<uint32_t>::max() / kChooseThreads)
         return fail(EB_ERR_UNSUPPORTED, "%s: more tokens than one launch holds", who);
-    hipError_t err = few ? launch(kernel, 1, kAllThreads) : launch(kernel, a.chunks, kChooseThreads);
+    hipError_t err = few ? launch(kernel, 1, kAllThreads) : launch(kernel, grid, kChooseThreads);
     if (err == hipSuccess && offsets && !few) {
         if (!a.counts) {
             err = launch((void *)eb_route_place_few, 1, kAllThreads);
