@@ -121,9 +121,10 @@ int eb_route_experts(int64_t N, int32_t E, int32_t K, const void *scores, int32_
  *                block_rows 128: [matrices][ceil(rows/128)][ceil(cols/128)],
  *                lds unused.
  *
- * scale = max(largest |x| of the block / 448, 2^-126), q = x / scale rounded
- * to nearest even, both divisions in fp32: the value held is q * scale.  A
- * block with an infinity or a NaN has the scale NaN and only NaNs.  Errors:
+ * scale = max(largest |x| of the block / 448, 2^-126), rounded to fp32; q =
+ * x / the scale before its rounding, the exact quotient rounded once, to nearest
+ * even.  The value held is q * scale.  A block with an infinity or a NaN has the
+ * scale NaN and only NaNs.  Errors:
  * EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED for
  * sizes one launch does not hold (2^24 strips of 16 rows by 512 columns, or of
  * 128 x 128), EB_ERR_HIP when a launch fails.
@@ -165,8 +166,8 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  *   out_type     EB_F32, EB_F16, EB_BF16 or EB_FP8.
  *   out          device, rows ldo elements (>= the output's width) apart,
  *                element-aligned.  EB_FP8: e4m3, 16-byte aligned, ldo a
- *                multiple of 16, quantised as by eb_quantize_fp8 with
- *                block_rows 1 from the fp32 values.
+ *                multiple of 16, scaled as by eb_quantize_fp8 with block_rows 1
+ *                from the fp32 values, the quotients within 2 ulp of fp32.
  *   out_scales   device fp32 [ceil(width/128)][ldos], ldos >= M, for EB_FP8;
  *                else unused.
  *

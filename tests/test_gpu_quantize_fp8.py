@@ -1,9 +1,11 @@
 """GPU parity of eb_quantize_fp8 with its definition.
 
-scale and quotient are single fp32 divisions and the cast rounds to nearest
-even, so the same steps on the CPU give the same bits; and against 64 bits,
-|q * scale - x| <= |x| 2^-4 (1 + 2^-20) + scale * 2^-10 (half a step of e4m3,
-normal and subnormal, and the two divisions' rounding).
+The scale is a single fp32 division, so the CPU's gives the same bits.  The
+exact quotient x * 448 / most is rounded to nearest even: x * 448 and the
+middles of e4m3 numbers times most are compared in 64 bits, which hold both, so
+that gives the same bits too.  And |q * scale - x| <= |x| 2^-4 (1 + 2^-20) +
+scale * 2^-10 (half a step of e4m3, normal and subnormal, and the rounding of
+the scale).
 """
 import pytest
 import torch
@@ -15,7 +17,7 @@ INF = float("inf")
 
 
 def plain(x, block_rows):
-    """q and scales of [m, rows, cols], in fp32 on the CPU."""
+    """q and scales of [m, rows, cols], on the CPU."""
     m, rows, cols = x.shape
     rb, cb = -(-rows // block_rows), -(-cols // 128)
     full = torch.zeros(m, rb * block_rows, cb * 128)
@@ -23,8 +25,14 @@ def plain(x, block_rows):
     b = full.view(m, rb, block_rows, cb, 128)
     most = b.abs().amax((2, 4))
     s = torch.where(torch.isfinite(most), (most / 448).clamp(min=2.0 ** -126), float("nan"))
-    q = (b / s[:, :, None, :, None]).view(m, rb * block_rows, cb * 128)[:, :rows, :cols]
-    return q.to(torch.float8_e4m3fn), s
+    at = most.double().clamp(min=448 * 2.0 ** -126)[:, :, None, :, None]
+    x448 = b.double().abs() * 448
+    step = torch.exp2(torch.floor(torch.log2((x448 / at).clamp(min=2.0 ** -6))) - 3)
+    k = torch.floor(x448 / at / step)
+    middle = (k + 0.5) * step * at
+    k += (x448 > middle) | ((x448 == middle) & (k % 2 == 1))
+    q = torch.where(s.isnan()[:, :, None, :, None], float("nan"), torch.copysign(k * step, b.double()))
+    return q.view(m, rb * block_rows, cb * 128)[:, :rows, :cols].to(torch.float8_e4m3fn), s
 
 
 def bits(q):
@@ -128,3 +136,23 @@ def test_refusals(device):
     for bad in (x.double(), x.cpu(), x.t(), x[0], torch.zeros(6, 4, 32, device=device)[::2]):
         with pytest.raises(ValueError):
             ex.quantize_fp8(bad)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quotients_at_and_by_the_middle(dtype, block_rows, device):
+    """Values at the exact middles of e4m3 numbers times most / 448, and their neighbours, at every size."""
+    values = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    middle = (values[1:] + values[:-1]) / 2
+    tiny, huge = torch.finfo(dtype).tiny, torch.finfo(dtype).max
+    rows = []
+    for most in (448.0, 1.0, 7.0, 3.5, 0.4375, 1.75 * 2.0 ** 9, 5.0, 1.1, huge, huge / 2, tiny * 448, tiny * 460, tiny * 512):
+        x = (middle * (most / 448)).to(dtype)
+        for y in (x, torch.nextafter(x, torch.zeros_like(x)), torch.nextafter(x, torch.full_like(x, INF))):
+            row = torch.zeros(128, dtype=dtype)
+            row[:126] = torch.where(y.float().abs() > most, torch.zeros_like(y), y)
+            row[1:126:2] *= -1
+            row[127] = most
+            rows.append(row)
+    x = torch.stack(rows)
+    check(x, 1, device) if block_rows == 1 else [check(r.expand(3, 128).contiguous(), 128, device) for r in rows]
