@@ -219,10 +219,11 @@ def _quantize(torch, x, block_rows, stream):
     dtype, pitch, blocks = _code(x.dtype), (cols + 15) & -16, (cols + BLOCK - 1) // BLOCK
     q = x.new_empty((rows, pitch) if dim == 2 else (m, rows, pitch), dtype=torch.float8_e4m3fn)
     if block_rows == 1:
-        scales = x.new_empty((blocks, m * rows), dtype=torch.float32)
-        lds, shaped = m * rows, scales.t()
-        if dim == 3:
-            shaped = shaped.view(m, rows, blocks)
+        lds = m * rows
+        if dim == 2:
+            scales = shaped = x.new_empty_strided((rows, blocks), (1, lds), dtype=torch.float32)
+        else:
+            scales = shaped = x.new_empty_strided((m, rows, blocks), (rows, 1, lds), dtype=torch.float32)
     else:
         scales = x.new_empty((m, _blocks(rows), blocks), dtype=torch.float32)
         lds, shaped = 0, scales if dim == 3 else scales[0]
@@ -307,7 +308,7 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
             raise ValueError("out is for floating-point outputs")
         ldo = (width + 15) & -16
         out = x.new_empty((M, ldo))
-        scales = x.new_empty((blocks, M), dtype=f32)
+        scales = x.new_empty_strided((M, blocks), (1, M), dtype=f32)
         scales_ptr = scales.data_ptr()
     elif out is None:
         ldo = width
@@ -322,7 +323,7 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
     if rc:
         _check(rc)
     if code == EB_FP8:
-        return (out if ldo == width else out[:, :width]), scales.t()
+        return (out if ldo == width else out[:, :width]), scales
     return out
 
 
