@@ -29,9 +29,10 @@
 // A launch costs more than the work of a small batch (2.4 us of the caller's time):
 // up to 16 tokens, or 128 of at most 64 experts, one workgroup does all of it (us
 // a call among others: 64 tokens, 6 of 64 experts 11.4, two launches 13.7; on the GPU
-// 6.8 and 7.2; but 64 tokens, 8 of 256 22.5 and 13.8).  Up to kFewPairs pairs one workgroup
-// scans and places after choose (4080 pairs 13.6, three launches 17.5, on the GPU
-// 11.1 each; 7800 pairs 16.1 and 17.7, on the GPU 16.3 and 11.3).
+// 6.8 and 7.2; but 64 tokens, 8 of 256 22.5 and 13.8).  Up to kFewPairs pairs there is
+// no scan: each workgroup that places kPart pairs counts all of them (8000 pairs of
+// 64 experts 13.7, three launches 17.6, on the GPU 10.8 and 11.3; 16000 pairs 13.9 and
+// 17.6, on the GPU 13.5 and 11.5).
 
 #include <hip/hip_runtime.h>
 
@@ -55,7 +56,7 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kChooseThreads = 512; // 32 tokens of 16 lanes
 constexpr int kTokens = 32;        // tokens of a chunk
 constexpr int kFewWaves = 16;      // of the workgroup that does all
-constexpr int kFewTokens = 128, kFewPairs = 4096, kFewExperts = 512;
+constexpr int kFewTokens = 128, kFewPairs = 16384, kFewExperts = 512;
 constexpr int kMostFewPairs = kFewWaves * 64;
 constexpr int kFilterTop = 8;      // most experts per token for the filter
 constexpr int kMostExperts = 1024;
@@ -396,56 +397,88 @@ __device__ __forceinline__ uint32_t prefix_in_wave(uint32_t v)
     return v;
 }
 
-// Scan and placing of few pairs by one workgroup of kFewWaves waves.
-// expert_of(p): the held expert of pair p, or -1.
+// Scan and placing of the pairs [begin, end) by a workgroup of kFewWaves waves,
+// which counts all the others too.  expert_of(p): the held expert of pair p, or -1.
 constexpr int kAllThreads = kFewWaves * kWave;
 
 struct PlaceSpace {
     uint32_t next[kFewWaves][kMostExperts]; // counts, then the next slot, per wave and expert
+    uint32_t before[kMostExperts], after[kMostExperts]; // pairs of other workgroups
 };
 
 template <typename ExpertOf>
-__device__ __forceinline__ void place_all(const RouteArgs &a, PlaceSpace &space, uint32_t (&wave_sum)[kFewWaves], ExpertOf expert_of)
+__device__ __forceinline__ void place_all(const RouteArgs &a, PlaceSpace &space, uint32_t (&wave_sum)[kFewWaves], int begin, int end,
+                                          ExpertOf expert_of)
 {
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     // A wave takes a run of the pairs.
-    const int pairs = (int)a.N * a.K, run = (pairs + kFewWaves - 1) / kFewWaves;
-    const int p0 = min(pairs, wave * run), p1 = min(pairs, p0 + run);
+    const int pairs = (int)a.N * a.K, run = (end - begin + kFewWaves - 1) / kFewWaves;
+    const int p0 = min(end, begin + wave * run), p1 = min(end, p0 + run);
+    const int bits = 32 - __clz(a.held | 1);
     for (int j = lane; j < a.held; j += kWave) space.next[wave][j] = 0;
+    for (int j = threadIdx.x; j < a.held; j += kAllThreads) space.before[j] = space.after[j] = 0;
     wave_fence();
     for (int p = p0 + lane; p < p1; p += kWave) {
         const int j = expert_of(p);
         if (j >= 0) atomicAdd(&space.next[wave][j], 1u);
     }
     __syncthreads();
+    auto count = [&](int from, int to, uint32_t *counts) {
+        constexpr int kEach = 8; // loads under way
+        for (int q = from; q < to; q += kEach * kAllThreads) {
+            int e[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int p = q + i * kAllThreads + (int)threadIdx.x;
+                e[i] = p < to ? expert_of(p) : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (q + i * kAllThreads >= to) break;
+                const int lead = __builtin_amdgcn_readfirstlane(e[i]);
+                if (__all(e[i] == lead)) {
+                    if (lead >= 0 && lane == 0) atomicAdd(&counts[lead], (uint32_t)kWave);
+                } else if (a.held > 8) {
+                    if (e[i] >= 0) atomicAdd(&counts[e[i]], 1u);
+                } else { // many lanes at one address: one for all of them
+                    const uint64_t same = same_expert(e[i], bits);
+                    if (e[i] >= 0 && (same & ((1ull << lane) - 1)) == 0) atomicAdd(&counts[e[i]], (uint32_t)__popcll(same));
+                }
+            }
+        }
+    };
+    count(0, begin, space.before);
+    count(end, pairs, space.after);
+    __syncthreads();
     static_assert(kAllThreads >= kMostExperts, "a thread per expert");
     const int j = threadIdx.x;
-    uint32_t sum = 0;
+    uint32_t mine = 0, sum = 0, earlier = 0;
     if (j < a.held) {
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) {
             const uint32_t n = space.next[w][j];
-            space.next[w][j] = sum;
-            sum += n;
+            space.next[w][j] = mine;
+            mine += n;
         }
+        earlier = space.before[j];
+        sum = earlier + mine + space.after[j];
     }
     const uint32_t upto = prefix_in_wave(sum);
     if (lane == kWave - 1) wave_sum[wave] = upto;
     __syncthreads();
-    uint32_t before = upto - sum, total = 0;
+    uint32_t first = upto - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) {
-        before += w < wave ? wave_sum[w] : 0;
+        first += w < wave ? wave_sum[w] : 0;
         total += wave_sum[w];
     }
     if (j < a.held) {
-        a.offsets[j] = (int32_t)before;
+        if (begin == 0) a.offsets[j] = (int32_t)first;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) space.next[w][j] += before;
+        for (int w = 0; w < kFewWaves; ++w) space.next[w][j] += first + earlier;
     }
-    if (j == 0) a.offsets[a.held] = (int32_t)total;
+    if (begin == 0 && j == 0) a.offsets[a.held] = (int32_t)total;
     __syncthreads();
-    const int bits = 32 - __clz(a.held | 1);
     for (int q = p0; q < p1; q += kWave) {
         const int p = q + lane;
         const int e = p < p1 ? expert_of(p) : -1;
@@ -487,14 +520,17 @@ __global__ __launch_bounds__(kAllThreads) void eb_route_few(RouteArgs a)
     }
     if (!a.offsets) return;
     __syncthreads();
-    place_all(a, space.place, wave_sum, [&](int p) { return (int)expert_of[p]; });
+    place_all(a, space.place, wave_sum, 0, (int)a.N * a.K, [&](int p) { return (int)expert_of[p]; });
 }
+
+constexpr int kPart = 1024; // pairs that a workgroup of it places
 
 __global__ __launch_bounds__(kAllThreads) void eb_route_place_few(RouteArgs a)
 {
     __shared__ PlaceSpace space;
     __shared__ uint32_t wave_sum[kFewWaves];
-    place_all(a, space, wave_sum, [&](int p) { return held_expert(a, a.ids[p]); });
+    const int begin = (int)blockIdx.x * kPart;
+    place_all(a, space, wave_sum, begin, min((int)a.N * a.K, begin + kPart), [&](int p) { return held_expert(a, a.ids[p]); });
 }
 
 // counts[j][c] becomes the pairs of expert j in the chunks before c, the total
@@ -701,7 +737,7 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     hipError_t err = few ? launch(kernel, 1, kAllThreads) : launch(kernel, grid, kChooseThreads);
     if (err == hipSuccess && offsets && !few) {
         if (!a.counts) {
-            err = launch((void *)eb_route_place_few, 1, kAllThreads);
+            err = launch((void *)eb_route_place_few, (N * K + kPart - 1) / kPart, kAllThreads);
         } else {
             if (held > 0) err = launch((void *)eb_route_scan, (held + kWaves - 1) / kWaves, kThreads);
             if (err == hipSuccess) err = launch((void *)eb_route_place, a.chunks, kThreads);

@@ -251,3 +251,14 @@ def test_softmax_of_chosen_far_below_the_largest(device):
         pair[:, 13], pair[:, 12:16:2], pair[:, 15] = 150.0, -INF, -INF  # its group has no second
         r = check(pair, 5, device, ex.EB_SOFTMAX | ex.EB_RENORMALIZE | ex.EB_GROUP_PAIR, groups=10, top_groups=4, least_clear=0.0)
         assert (r.ids != 13).all() and (r.weights > 0).all()
+
+
+@pytest.mark.parametrize("N,E,K,lo,hi", [(341, 64, 3, 0, 64), (342, 64, 3, 5, 40), (2048, 160, 6, 80, 100), (4096, 8, 4, 0, 8), (4095, 6, 4, 2, 3),
+                                         (2047, 1024, 8, 0, 1024), (16384, 3, 1, 0, 3), (16385, 3, 1, 0, 3), (300, 80, 50, 7, 80)])
+@pytest.mark.parametrize("skewed", [False, True])
+def test_pairs_placed_by_several_workgroups(N, E, K, lo, hi, skewed, device):
+    x = torch.randn(N, E, generator=torch.Generator().manual_seed(N))
+    if skewed:  # runs of tokens with the same choice, and tokens without any
+        x[:N // 2] = torch.arange(E, 0, -1.0)
+        x[N // 2:N // 2 + 100] = -INF
+    check(x, K, device, ex.EB_SOFTMAX | ex.EB_RENORMALIZE, lo=lo, hi=hi)
