@@ -303,7 +303,7 @@ struct KernelPlan {
     int32_t band;    // the grid holds a multiple of so many slot tiles
 };
 
-// Slots of a workgroup: 256, 128, 64, 32 (by 256 weight rows).
+// Slots and weight rows of a workgroup: 256 x 256, 128 x 256, 64 x 128, 32 x 128.
 enum class TileSize { kHuge, kLarge, kMedium, kSmall };
 
 KernelPlan stream_kernel(bool gate, bool fp8);

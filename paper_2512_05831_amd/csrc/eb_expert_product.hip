@@ -21,47 +21,46 @@ constexpr int64_t kMostSize = (int64_t)1 << 30;
 int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1 : 2; }
 
 // The kernel for a call, from its mean of slots per expert (the counts are on
-// the device) and the workgroups that each kernel then has.  Measured, us of GPU
-// time a call, with slots a third around the mean:
-//   Stream against small tiles.  Its time is its workgroups', 16 slots by 16
-//   rows each, whatever the other's is per block of K: one expert of 2048 x 4096,
-//   100 slots (896 workgroups) 15.1 and 25.2 in the 8-bit unit, 17.9 and 28.0 in
-//   the 16-bit one; 200 slots (1664) 29.9 and 25.4, 22.6 and 28.1; 400 slots 52
-//   and 25.5, 38.5 and 28.3.  With a gate a workgroup has twice the rows (100
-//   slots 13.9 and 25.0, 400 slots 42.9 and 25.0), with 8-bit outputs eight times
+// the device) and how many pieces of so many slots by so many weight rows it then
+// has.  Measured, us of GPU time a call, with slots a third around the mean:
+//   Stream against small tiles.  Its time is its pieces', 16 by 16, whatever the
+//   other's is per block of K: one expert of 2048 x 4096, 100 slots (896 pieces)
+//   15.1 and 25.2 in the 8-bit unit, 17.9 and 28.0 in the 16-bit one; 200 slots (1664)
+//   29.9 and 25.4, 22.6 and 28.1; 400 slots 52 and 25.5, 38.5 and 28.3.  The same with a
+//   gate (100 slots 13.9 and 25.0, 400 slots 42.9 and 25.0) and with 8-bit outputs
 //   (1000 x 1520: 200 slots 9.4 and 14.4; 16 experts of 2048 x 1024, 16 slots: 15.5
-//   and 11.3), with both it holds 256 rows of all K as a tile does: 45.9 and 27.8.
+//   and 11.3); with both a workgroup holds 256 rows of all K as a tile does: 45.9 and
+//   27.8.  (Small tiles of 256 rows; those of 128 since then take a quarter less.)
 //   Larger tiles read their operands less often, smaller ones fill the GPU and
 //   waste less of an expert's last tile.  Huge against large, 16384 slots of one
 //   expert of 4096 x 3328: 195 and 213 in the 8-bit unit, 346 and 363 in the 16-bit
 //   one; 64 experts of 2048 x 3328, 512 slots each: 287 and 272, gated with 8-bit
-//   outputs 470 and 417; 2048 slots each: equal within 1 %.  16 experts of 2048 x 1024: large against
-//   medium, 8-bit unit, 200 slots (256 tiles) 16.8 and 17.8, 900 slots 43.6 and
-//   46.2; 16-bit unit 200 slots 33.8 and 25.0, 400 slots (512 tiles) 41.6 and 44.0.
-//   Medium against small: 8-bit unit, 100 slots (256 tiles) 13.1 and 13.4, 200
-//   slots 17.8 and 22.7; 16-bit unit 100 slots 17.0 and 17.4 (32 experts of 1024 x
-//   2048, also 256 tiles: 36.6 and 26.6), 200 slots (512 tiles) 25.0 and 28.8.
-KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t width, int64_t ldx, int64_t ldw, bool gathered,
-                         int64_t x_rows, bool gate, int32_t out_type)
+//   outputs 470 and 417; 2048 slots each: equal within 1 %.  16 experts of 2048 x
+//   1024: large against medium (of 256 rows), 8-bit unit, 200 slots (256 tiles) 16.8
+//   and 17.8, 900 slots 43.6 and 46.2; 16-bit unit 200 slots 33.8 and 25.0, 400 slots
+//   (512 tiles) 41.6 and 44.0.
+//   Medium against small, 16-bit unit: 4000 slots by 1000 x 1520 (504 tiles) 18.0 and
+//   20.5, 16 experts of 512 x 2048 with 375 slots (384) 22.1 and 24.2; but 32 experts
+//   of 1024 x 2048 with 100 slots (512) 29.9 and 26.6.  8-bit unit: 16 experts of 512 x
+//   2048 with 375 slots 15.4 and 18.7 (medium of 256 rows).
+KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t ldx, int64_t ldw, bool gathered, int64_t x_rows, bool gate,
+                         int32_t out_type)
 {
     const bool fp8 = out_type == EB_FP8, wide = fp8 || out_type == EB_F32;
     // The tile kernel addresses x (a slot tile's rows, or all where they are
     // gathered) and an expert's weights with 32 bits.
     constexpr int64_t kMost32 = (int64_t)1 << 32;
-    const KernelPlan stream = stream_kernel(gate, fp8);
-    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 256) * ldx >= kMost32) return stream;
+    if (x_rows == 0 || N * ldw >= kMost32 || (gathered ? x_rows : 256) * ldx >= kMost32) return stream_kernel(gate, fp8);
     const int64_t mean = (M + E - 1) / E;
-    auto tiles = [&](const KernelPlan &p) {
-        return std::min<int64_t>(E, M) * ((mean + p.height - 1) / p.height) * ((width + p.columns - 1) / p.columns);
+    auto pieces = [&](int64_t slots, int64_t rows) {
+        return std::min<int64_t>(E, M) * ((mean + slots - 1) / slots) * ((N + rows - 1) / rows);
     };
-    if (!(gate && fp8) && tiles(stream) * (fp8 ? 8 : gate ? 2 : 1) <= (wide ? 1536 : 1024)) return stream;
-    const KernelPlan huge = tile_kernel(gate, out_type, TileSize::kHuge);
-    if (mean >= 4096 && tiles(huge) >= 512) return huge;
-    const KernelPlan large = tile_kernel(gate, out_type, TileSize::kLarge);
-    if (tiles(large) >= (wide ? 512 : 256)) return large;
-    const KernelPlan medium = tile_kernel(gate, out_type, TileSize::kMedium);
-    if (tiles(medium) >= (wide ? 320 : 192)) return medium;
-    return tile_kernel(gate, out_type, TileSize::kSmall);
+    if (!(gate && fp8) && pieces(16, 16) <= (wide ? 1536 : 1024)) return stream_kernel(gate, fp8);
+    const TileSize size = mean >= 4096 && pieces(256, 256) >= 512                         ? TileSize::kHuge
+                          : pieces(128, 256) >= (wide ? 512 : 256)                        ? TileSize::kLarge
+                          : pieces(64, 128) >= (wide && mean < 128 ? 640 : 384)           ? TileSize::kMedium
+                                                                                          : TileSize::kSmall;
+    return tile_kernel(gate, out_type, size);
 }
 
 int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
@@ -123,7 +122,7 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     const int es = element_bytes(out_type);
     a.vector_out = ldo * es % 16 == 0 && (uintptr_t)out % 16 == 0;
 
-    const KernelPlan plan = choose_kernel(M, E, N, width, ldx, ldw, tokens != nullptr, x_rows, gate, out_type);
+    const KernelPlan plan = choose_kernel(M, E, N, ldx, ldw, tokens != nullptr, x_rows, gate, out_type);
     a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
     // At most one tile per expert is not full.
     const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);

@@ -9,10 +9,12 @@ namespace {
 template <bool kWide, bool kGate, bool kFp8>
 KernelPlan plan_of(TileSize size)
 {
-    if (size == TileSize::kHuge) return tile_plan<TileShape<8, 2, kWide, kGate, kFp8>>();
-    if (size == TileSize::kLarge) return tile_plan<TileShape<8, 1, kWide, kGate, kFp8>>();
-    if (size == TileSize::kMedium) return tile_plan<TileShape<4, 1, kWide, kGate, kFp8>>();
-    return tile_plan<TileShape<2, 1, kWide, kGate, kFp8>>();
+    if (size == TileSize::kHuge) return tile_plan<TileShape<8, 4, 2, kWide, kGate, kFp8>>();
+    if (size == TileSize::kLarge) return tile_plan<TileShape<8, 4, 1, kWide, kGate, kFp8>>();
+    // Gated 8-bit outputs: 256 rows too, for a whole block of outputs.
+    constexpr int kRows = kGate && kFp8 ? 4 : 2;
+    if (size == TileSize::kMedium) return tile_plan<TileShape<4, kRows, 1, kWide, kGate, kFp8>>();
+    return tile_plan<TileShape<2, kRows, 1, kWide, kGate, kFp8>>();
 }
 
 } // namespace

@@ -307,3 +307,15 @@ def test_tiles_of_256_slots(out, act, M, N, K, counts, device):
         close_fp8(*got, case)
     else:
         close(got, case, out)
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.float16, torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_RELU, ex.EB_ACT_SILU_GATE])
+@pytest.mark.parametrize("M,N,K,counts", [(1601, 2050, 300, None), (1990, 1672, 385, None), (4500, 716, 520, [1501, 0, 1400, 90, 1509]), (1000, 130, 1050, None)])
+def test_tiles_of_64_and_32_slots(out, act, M, N, K, counts, device):
+    case = Case(M, N, K, device, E=1 if counts is None else len(counts), act=act, bias=N != 716, counts=counts, gather=None if counts is None else 900)
+    got = case.run(out_dtype=out)
+    if out == torch.float8_e4m3fn:
+        close_fp8(*got, case)
+    else:
+        close(got, case, out)
