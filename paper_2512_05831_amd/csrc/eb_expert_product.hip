@@ -24,13 +24,13 @@ int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1
 // the device) and how many pieces of so many slots by so many weight rows it then
 // has.  Measured, us of GPU time a call, with slots a third around the mean:
 //   Stream against small tiles.  Its time is its pieces', 16 by 16, whatever the
-//   other's is per block of K: one expert of 2048 x 4096, 100 slots (896 pieces)
-//   15.1 and 25.2 in the 8-bit unit, 17.9 and 28.0 in the 16-bit one; 200 slots (1664)
-//   29.9 and 25.4, 22.6 and 28.1; 400 slots 52 and 25.5, 38.5 and 28.3.  The same with a
-//   gate (100 slots 13.9 and 25.0, 400 slots 42.9 and 25.0) and with 8-bit outputs
-//   (1000 x 1520: 200 slots 9.4 and 14.4; 16 experts of 2048 x 1024, 16 slots: 15.5
-//   and 11.3); with both a workgroup holds 256 rows of all K as a tile does: 45.9 and
-//   27.8.  (Small tiles of 256 rows; those of 128 since then take a quarter less.)
+//   other's is per block of K.  8-bit unit: one expert of 1000 x 1520, 200 slots (819
+//   pieces) 6.5 and 7.7, 300 slots (1197) 7.9 and 7.7; of 2048 x 4096, 64 slots (512) 10.7
+//   and 19.7, 200 slots (1664) 25.2 and 20.1; 4 experts of 1024 x 512, 64 slots (1024) 6.9
+//   and 5.3; a gate changes little.  16-bit unit: 1000 x 1520, 200 slots 7.7 and 9.4; 2048 x
+//   4096, 128 slots (1024) 18.7 and 20.6, 200 slots 28.5 and 20.7; 16 experts of 1024 x
+//   1024, 8 slots (1024) 6.9 and 7.3.  For 8-bit outputs a workgroup holds 128 rows (with a
+//   gate 256): 1000 x 1520 9.2 and 9.8, but 2048 x 4096 25.3 and 20.6, 1024 x 512 7.1 and 6.2.
 //   Larger tiles read their operands less often, smaller ones fill the GPU and
 //   waste less of an expert's last tile.  Huge against large, 16384 slots of one
 //   expert of 4096 x 3328: 195 and 213 in the 8-bit unit, 346 and 363 in the 16-bit
@@ -55,7 +55,7 @@ KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t ldx, int64_t l
     auto pieces = [&](int64_t slots, int64_t rows) {
         return std::min<int64_t>(E, M) * ((mean + slots - 1) / slots) * ((N + rows - 1) / rows);
     };
-    if (!(gate && fp8) && pieces(16, 16) <= (wide ? 1536 : 1024)) return stream_kernel(gate, fp8);
+    if (!fp8 && pieces(16, 16) <= (wide ? 1024 : 896)) return stream_kernel(gate, fp8);
     const TileSize size = mean >= 4096 && pieces(256, 256) >= 512                         ? TileSize::kHuge
                           : pieces(128, 256) >= (wide ? 512 : 256)                        ? TileSize::kLarge
                           : pieces(64, 128) >= (wide && mean < 128 ? 640 : 384)           ? TileSize::kMedium

@@ -1,5 +1,7 @@
 // eb_expert_product for few slots of few experts: bound by latency and by the
-// weights' way to the few compute units that have them.
+// weights' way to the few compute units that have them (one slot by 2048 x 1024 3.4
+// us; 64 by 2048 x 4096 10.7).  And for operands beyond 32-bit offsets: all
+// addresses here have 64 bits.
 //
 // A workgroup of eight waves takes up to 16 slots of an expert and a run of its
 // weight rows: kAcross waves side by side, each with kRows tiles of 16 rows, and

@@ -319,3 +319,16 @@ def test_tiles_of_64_and_32_slots(out, act, M, N, K, counts, device):
         close_fp8(*got, case)
     else:
         close(got, case, out)
+
+
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_RELU, ex.EB_ACT_SILU_GATE])
+def test_gathered_rows_past_32_bits(act, device):
+    """Tokens at byte offsets past 2^32, every type of output."""
+    case = Case(90, 420, 300, device, E=3, act=act, bias=True, counts=[33, 0, 50], gather=280, x_pitch=304)
+    case.tokens[::9] = -1
+    wide = torch.full((280, 1 << 24), 0x7F, dtype=torch.uint8, device=device)
+    wide[:, :300] = case.x.contiguous().view(torch.uint8)
+    case.x = wide.view(torch.float8_e4m3fn)[:, :300]
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        close(case.run(out_dtype=dtype), case, dtype)
+    close_fp8(*case.run(out_dtype=torch.float8_e4m3fn), case)
