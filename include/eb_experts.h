@@ -137,7 +137,7 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  * with a scale for each block of 128.
  *
  *   M            slots (output rows), >= 0, < 2^31.
- *   E            experts, >= 1.
+ *   E            experts, 1 .. 2^30.
  *   N, K         rows of a weight matrix (outputs before EB_ACT_SILU_GATE) and
  *                its columns (inputs), each 1 .. 2^30.
  *   x            device e4m3 [x_rows, K], 16-byte aligned, rows ldx (>= K, a
@@ -182,8 +182,8 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  * them cut off: about 1.5e-5 of the size of a sum of normal values, far below
  * the outputs' rounding.  Equal calls give equal bits.
  * Errors: EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED
- * for sizes one launch does not hold (2^23 tiles), EB_ERR_HIP when a launch
- * fails.
+ * for M, E, N or K past their ends and sizes one launch does not hold (2^23
+ * tiles), EB_ERR_HIP when a launch fails.
  */
 int eb_expert_product(int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
                       const float *x_scales, int64_t ldxs, const int32_t *tokens, const void *w, int64_t ldw,

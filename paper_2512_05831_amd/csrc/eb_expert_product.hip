@@ -76,8 +76,9 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     const bool gate = act == EB_ACT_SILU_GATE, fp8 = out_type == EB_FP8;
     if (gate && N % 2 != 0) return fail(EB_ERR_INVALID, "%s: a gate needs an even N", who);
     if (!offsets && E != 1) return fail(EB_ERR_INVALID, "%s: several experts need offsets", who);
-    if (M > std::numeric_limits<int32_t>::max() || N > kMostSize || K > kMostSize)
-        return fail(EB_ERR_UNSUPPORTED, "%s: M of 2^31 and more, or N or K above 2^30", who);
+    // E too: slot_tile counts experts up to the wave past the last in 32 bits.
+    if (M > std::numeric_limits<int32_t>::max() || E > kMostSize || N > kMostSize || K > kMostSize)
+        return fail(EB_ERR_UNSUPPORTED, "%s: M of 2^31 and more, or E, N or K above 2^30", who);
     if (M == 0) return EB_OK;
     if (!x || !x_scales || !w || !w_scales || !out || (fp8 && !out_scales))
         return fail(EB_ERR_INVALID, "%s: NULL x, w, out or their scales", who);

@@ -1,0 +1,15 @@
+"""Limits of the experts' C calls on the host: what lies past them is refused before a
+device is touched.
+"""
+from paper_2512_05831_amd import eb, experts as ex
+from test_experts_host import U, code_of, product
+
+
+def test_product_refuses_experts_beyond_32_bit_steps():
+    """The kernels walk the experts 64 at a time in 32 bits: within 64 of 2^31 that count would wrap, and a workgroup
+    past the last tile would never end."""
+    for E in ((1 << 30) + 1, (1 << 31) - 64, (1 << 31) - 1):
+        assert code_of(product, E=E, ldo=256) == U
+        assert code_of(product, E=E, N=16, ldo=16, out_type=ex.EB_FP8, out_scales_ptr=0x7F0000000000, ldos=4) == U
+    product(E=1 << 30, M=0, x_rows=0, ldxs=0)
+    assert eb.EB_ERR_UNSUPPORTED == U
