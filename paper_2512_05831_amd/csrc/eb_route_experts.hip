@@ -336,7 +336,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t n, int lane, 
     } else if (!a.sigmoid) {
         w = id < 0 ? 0.f : w / total;
     }
-    weight = w * a.scale;
+    weight = id < 0 ? 0.f : w * a.scale; // the scale may be infinite or NaN
 }
 
 // The pair's expert as one of this GPU's, or -1.
