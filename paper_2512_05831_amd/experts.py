@@ -214,7 +214,7 @@ def _quantize(torch, x, block_rows, stream):
         ldx = _pitch(x[0], "x") if m else cols
         if m > 1 and rows == 1:
             ldx = x.stride(0)
-        elif m > 1 and x.stride(0) != rows * ldx:
+        elif m > 1 and rows > 1 and x.stride(0) != rows * ldx:
             raise ValueError("x's matrices must be stacked row after row")
     dtype, pitch, blocks = _code(x.dtype), (cols + 15) & -16, (cols + BLOCK - 1) // BLOCK
     q = x.new_empty((rows, pitch) if dim == 2 else (m, rows, pitch), dtype=torch.float8_e4m3fn)
