@@ -285,8 +285,10 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
         x_scales = x_scales.t().contiguous().t()
         by_block = rows
     ldxs = by_block if kb > 1 else rows
-    if w_scales.dtype != f32 or not w_scales.is_contiguous() or w_scales.numel() != (2 if gate else 1) * E * blocks * kb:
-        raise ValueError("w_scales must be contiguous fp32, a scale per 128 x 128 of w")
+    halves = 2 if gate else 1
+    if w_scales.dtype != f32 or not w_scales.is_contiguous() or w_scales.numel() != halves * E * blocks * kb or \
+            w_scales.dim() < 2 or w_scales.shape[-1] != kb or w_scales.shape[-2] not in (blocks, halves * blocks):
+        raise ValueError("w_scales must be contiguous fp32 [.., blocks of N, ceil(K/128)], a scale per 128 x 128 of w")
     M, offsets_ptr, tokens_ptr, bias_ptr = rows, None, None, None
     if offsets is not None:
         if offsets.dtype != i32 or not offsets.is_contiguous() or offsets.numel() != E + 1:
@@ -297,8 +299,8 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
             raise ValueError("tokens must be contiguous int32")
         M, tokens_ptr = tokens.numel(), tokens.data_ptr()
     if bias is not None:
-        if bias.dtype != f32 or not bias.is_contiguous() or bias.numel() != E * N:
-            raise ValueError("bias must be contiguous fp32 [E, N]")
+        if bias.dtype != f32 or not bias.is_contiguous() or bias.shape != (E, N) and (E > 1 or bias.shape != (N,)):
+            raise ValueError("bias must be contiguous fp32 [E, N], or [N] of one expert")
         bias_ptr = bias.data_ptr()
     _same_device(dev, x_scales, w, w_scales, offsets, tokens, bias, out)
     scales_ptr, scales = None, None

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import experts as ex
-from test_gpu_expert_product import blocks
+from test_gpu_expert_product import Case, blocks
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +17,29 @@ def test_stacks_without_rows(shape, block_rows, device):
     m, rows, cols = shape
     assert q.shape == shape and q.dtype == torch.float8_e4m3fn
     assert s.shape == (m, rows if block_rows == 1 else blocks(rows), blocks(cols))
+
+
+@pytest.mark.parametrize("E", [1, 3])
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_SILU_GATE])
+def test_scales_and_bias_of_another_shape(E, act, device):
+    """As many values in another order: a transposed matrix of scales, a bias by output, then expert."""
+    case = Case(40, 300, 600, device, E=E, act=act, bias=True, counts=[40 // E + (e < 40 % E) for e in range(E)])
+    want = case.run(out_dtype=torch.float32)
+    good, bias = case.ws, case.bias
+    for same in (good.clone(), good.view(E, -1, good.shape[-2], good.shape[-1])) + ((good[0],) if E == 1 else ()):
+        case.ws = same
+        assert torch.equal(case.run(out_dtype=torch.float32), want)
+    if act == ex.EB_ACT_SILU_GATE:  # as the halves' own matrices
+        case.ws = good.view(2 * E, -1, good.shape[-1])
+        assert torch.equal(case.run(out_dtype=torch.float32), want)
+    for bad in (good.transpose(-1, -2).contiguous(), good.flatten(), good.reshape(1, -1), good.reshape(-1, 1)):
+        case.ws = bad
+        with pytest.raises(ValueError):
+            case.run(out_dtype=torch.float32)
+    case.ws = good
+    for bad in (bias.t().contiguous(), bias.reshape(-1, 1)) + ((bias.flatten(),) if E > 1 else ()):
+        case.bias = bad
+        with pytest.raises(ValueError):
+            case.run(out_dtype=torch.float32)
+    case.bias = bias[0] if E == 1 else bias
+    assert torch.equal(case.run(out_dtype=torch.float32), want)
