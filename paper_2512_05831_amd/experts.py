@@ -304,6 +304,8 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
         bias_ptr = bias.data_ptr()
     _same_device(dev, x_scales, w, w_scales, offsets, tokens, bias, out)
     scales_ptr, scales = None, None
+    if out is not None and out_dtype not in (None, out.dtype):
+        raise ValueError("out is of another type than out_dtype")
     code = _code(out.dtype if out is not None else torch.bfloat16 if out_dtype is None else out_dtype, fp8=True)
     if code == EB_FP8:
         if out is not None:

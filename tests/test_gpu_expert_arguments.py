@@ -43,3 +43,12 @@ def test_scales_and_bias_of_another_shape(E, act, device):
             case.run(out_dtype=torch.float32)
     case.bias = bias[0] if E == 1 else bias
     assert torch.equal(case.run(out_dtype=torch.float32), want)
+
+
+def test_out_of_another_type_than_asked_for(device):
+    case = Case(8, 64, 128, device)
+    out = torch.empty(8, 64, dtype=torch.bfloat16, device=device)
+    for dtype in (torch.float32, torch.float16, torch.float8_e4m3fn):
+        with pytest.raises(ValueError):
+            case.run(out=out, out_dtype=dtype)
+    assert torch.equal(case.run(out=out, out_dtype=torch.bfloat16), case.run())
