@@ -365,9 +365,13 @@ class ExpertLayer:
         Returns fp32 [B, D]."""
         import torch
 
+        if x.dim() != 2 or x.shape[1] != self.K:
+            raise ValueError("x must be [B, K]")
         B = int(x.shape[0])
         if scores is None:
             scores = x.float() @ self.router.t()
+        elif scores.shape != (B, self.router.shape[0]):
+            raise ValueError("scores must be [B, experts]")
         r = route(scores, self.top, self.mode, self.bias, self.groups, self.top_groups, self.scale, self.shard_lo,
                   self.shard_lo + self.E)
         q, s = quantize_fp8(x)

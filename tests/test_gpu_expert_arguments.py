@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import experts as ex
+from test_gpu_expert_layer import layer_of
 from test_gpu_expert_product import Case, blocks
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +53,15 @@ def test_out_of_another_type_than_asked_for(device):
         with pytest.raises(ValueError):
             case.run(out=out, out_dtype=dtype)
     assert torch.equal(case.run(out=out, out_dtype=torch.bfloat16), case.run())
+
+
+def test_layer_refuses_scores_of_another_shape(device):
+    layer = layer_of(8, 256, 128, 64, 2, ex.EB_ACT_RELU, device)
+    x = torch.randn(10, 256, device=device)
+    layer.forward(x, torch.zeros(10, 8, device=device))
+    for scores in (torch.zeros(9, 8, device=device), torch.zeros(11, 8, device=device), torch.zeros(10, 9, device=device), torch.zeros(80, device=device)):
+        with pytest.raises(ValueError):
+            layer.forward(x, scores)
+    for bad in (x[:, :200], x[0], x.view(2, 5, 256)):
+        with pytest.raises(ValueError):
+            layer.forward(bad, torch.zeros(bad.shape[0], 8, device=device))
