@@ -1,6 +1,8 @@
 """Arguments of the experts' wrappers and of ``ExpertLayer``: calls without work, shapes
 that do not fit, streams and devices.
 """
+import contextlib
+
 import pytest
 import torch
 
@@ -65,3 +67,35 @@ def test_layer_refuses_scores_of_another_shape(device):
     for bad in (x[:, :200], x[0], x.view(2, 5, 256)):
         with pytest.raises(ValueError):
             layer.forward(bad, torch.zeros(bad.shape[0], 8, device=device))
+
+
+class Entered:
+    """Stands for torch.cuda.device: notes which GPU is made current."""
+
+    def __init__(self):
+        self.devices = []
+
+    def __call__(self, device):
+        self.devices.append(device.index)
+        return contextlib.nullcontext()
+
+
+def test_calls_go_to_the_tensors_gpu(device, monkeypatch):
+    """With another GPU current the tensors' own is made so: the default stream is the current GPU's."""
+    case = Case(8, 64, 128, device)
+    layer = layer_of(8, 256, 128, 64, 2, ex.EB_ACT_RELU, device)
+    x, scores = torch.randn(4, 256, device=device), torch.randn(4, 8, device=device)
+    want = case.run(), ex.quantize_fp8(x), ex.route(scores, 2), layer.forward(x, scores)
+    entered = Entered()
+    monkeypatch.setattr(torch.cuda, "device", entered)
+    calls = (lambda: case.run(), lambda: ex.quantize_fp8(x), lambda: ex.route(scores, 2), lambda: layer.forward(x, scores))
+    for call in calls:
+        call()
+    assert entered.devices == []  # this GPU is current
+    monkeypatch.setattr(ex, "_gpu", lambda: device.index + 1)
+    for call, result in zip(calls, want):
+        entered.devices.clear()
+        got = call()
+        assert entered.devices and set(entered.devices) == {device.index}
+        for a, b in zip(got if isinstance(got, tuple) else (got,), result if isinstance(result, tuple) else (result,)):
+            assert torch.equal(a.view(torch.uint8) if a.dtype == torch.float8_e4m3fn else a, b.view(torch.uint8) if b.dtype == torch.float8_e4m3fn else b)
