@@ -47,7 +47,8 @@ enum { EB_ACT_NONE = 0, EB_ACT_RELU = 1, EB_ACT_SILU_GATE = 2 };
  * eb_route_experts_workspace -- device workspace, in bytes, of eb_route_experts
  * for N tokens, K of E experts per token and the shard [shard_lo, shard_hi): 0
  * for few pairs.  Returns EB_ERR_INVALID for NULL bytes or bad sizes,
- * EB_ERR_UNSUPPORTED beyond eb_route_experts' limits.  Touches no device state.
+ * EB_ERR_UNSUPPORTED beyond eb_route_experts' limits on E, K and N * K.  Touches
+ * no device state.
  */
 int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo, int32_t shard_hi, size_t *bytes);
 

@@ -755,8 +755,8 @@ int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo
 {
     if (!bytes || N < 0 || K < 1 || K > E || shard_lo < 0 || shard_hi < shard_lo || shard_hi > E)
         return fail(EB_ERR_INVALID, "eb_route_experts_workspace: NULL bytes or a bad size");
-    if (E > kMostExperts || N > (int64_t)std::numeric_limits<int32_t>::max() / K)
-        return fail(EB_ERR_UNSUPPORTED, "eb_route_experts_workspace: more than 1024 experts or 2^31 - 1 pairs");
+    if (E > kMostExperts || K > kMostTop || N > (int64_t)std::numeric_limits<int32_t>::max() / K)
+        return fail(EB_ERR_UNSUPPORTED, "eb_route_experts_workspace: more than 1024 experts, 64 per token or 2^31 - 1 pairs");
     *bytes = workspace_of(N, K, shard_hi - shard_lo);
     return EB_OK;
 }

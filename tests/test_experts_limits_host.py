@@ -2,7 +2,7 @@
 device is touched.
 """
 from paper_2512_05831_amd import eb, experts as ex
-from test_experts_host import U, code_of, product
+from test_experts_host import U, code_of, product, route
 
 
 def test_product_refuses_experts_beyond_32_bit_steps():
@@ -13,3 +13,11 @@ def test_product_refuses_experts_beyond_32_bit_steps():
         assert code_of(product, E=E, N=16, ldo=16, out_type=ex.EB_FP8, out_scales_ptr=0x7F0000000000, ldos=4) == U
     product(E=1 << 30, M=0, x_rows=0, ldxs=0)
     assert eb.EB_ERR_UNSUPPORTED == U
+
+
+def test_workspace_refuses_what_the_route_refuses():
+    """More experts per token than eb_route_experts takes: no size for a call that cannot be made."""
+    assert ex.eb_route_experts_workspace(1000, 1024, 64, 0, 1024) > 0
+    for K in (65, 1024):
+        assert code_of(route, N=1000, E=1024, ld=1024, K=K, shard_hi=1024) == U
+        assert code_of(ex.eb_route_experts_workspace, N=1000, E=1024, K=K, shard_lo=0, shard_hi=1024) == U
