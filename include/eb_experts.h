@@ -42,6 +42,9 @@ enum { EB_RENORMALIZE = 0x100, EB_GROUP_PAIR = 0x200 };
 
 /* What eb_expert_product applies to its sums. */
 enum { EB_ACT_NONE = 0, EB_ACT_RELU = 1, EB_ACT_SILU_GATE = 2 };
+/* OR-ed into it: 16-bit outputs from sums as exact as those of other types,
+ * whatever the call's size. */
+enum { EB_EXACT_SUMS = 0x100 };
 
 /*
  * eb_route_experts_workspace -- device workspace, in bytes, of eb_route_experts
@@ -163,7 +166,7 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  *   bias         device fp32 [E, N] added to the sums, or NULL.
  *   act          EB_ACT_NONE; EB_ACT_RELU: max(v, 0); EB_ACT_SILU_GATE (even
  *                N): with g = v[n], u = v[N/2 + n], n < N/2, the output is
- *                g / (1 + exp(-g)) * u, N/2 wide.
+ *                g / (1 + exp(-g)) * u, N/2 wide.  Optionally | EB_EXACT_SUMS.
  *   out_type     EB_F32, EB_F16, EB_BF16 or EB_FP8.
  *   out          device, rows ldo elements (>= the output's width) apart,
  *                element-aligned.  EB_FP8: e4m3, 16-byte aligned, ldo a
@@ -176,12 +179,15 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  *             x_scales[b, row] * w_scales[e, n/128, b] * (sum over b's inputs k
  *             of x[row, k] * w[e, n, k])
  *
- * in fp32, rounded once to the output's type.  For fp32 and 8-bit outputs the
- * products and sums are exact to fp32's rounding.  For 16-bit outputs large
- * calls use the 8-bit matrix unit, which adds the products of eight
- * neighbouring inputs with what lies more than 13 bits below the largest of
- * them cut off: about 1.5e-5 of the size of a sum of normal values, far below
- * the outputs' rounding.  Equal calls give equal bits.
+ * in fp32, rounded once to the output's type.  For fp32 and 8-bit outputs, and
+ * with EB_EXACT_SUMS for all, the products and sums are exact to fp32's rounding.
+ * For 16-bit outputs all but small calls otherwise use the 8-bit matrix unit, at
+ * up to twice the rate.  It adds the products of eight neighbouring inputs with
+ * what lies more than 13 bits below the largest of them cut off, so a sum is off
+ * by less than 2^-10 of the largest product of each eight: about 1.5e-5 of the
+ * size of a sum of normal values, but all of what small products add beside one
+ * 2^13 times as large, also where large ones cancel.  Equal calls give equal bits;
+ * the same row in calls of other sizes need not.
  * Errors: EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED
  * for M, E, N or K past their ends and sizes one launch does not hold (2^23
  * tiles), EB_ERR_HIP when a launch fails.

@@ -307,6 +307,6 @@ struct KernelPlan {
 enum class TileSize { kHuge, kLarge, kMedium, kSmall };
 
 KernelPlan stream_kernel(bool gate, bool fp8);
-KernelPlan tile_kernel(bool gate, int32_t out_type, TileSize size);
+KernelPlan tile_kernel(bool gate, bool fp8, bool wide, TileSize size);
 
 } // namespace eb_product

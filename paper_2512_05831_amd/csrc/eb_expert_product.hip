@@ -44,9 +44,9 @@ int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1
 //   of 1024 x 2048 with 100 slots (512) 29.9 and 26.6.  8-bit unit: 16 experts of 512 x
 //   2048 with 375 slots 15.4 and 18.7 (medium of 256 rows).
 KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t ldx, int64_t ldw, bool gathered, int64_t x_rows, bool gate,
-                         int32_t out_type)
+                         int32_t out_type, bool exact)
 {
-    const bool fp8 = out_type == EB_FP8, wide = fp8 || out_type == EB_F32;
+    const bool fp8 = out_type == EB_FP8, wide = fp8 || out_type == EB_F32 || exact;
     // The tile kernel addresses x (a slot tile's rows, or all where they are
     // gathered) and an expert's weights with 32 bits.
     constexpr int64_t kMost32 = (int64_t)1 << 32;
@@ -60,7 +60,7 @@ KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t ldx, int64_t l
                           : pieces(128, 256) >= (wide ? 512 : 256)                        ? TileSize::kLarge
                           : pieces(64, 128) >= (wide && mean < 128 ? 640 : 384)           ? TileSize::kMedium
                                                                                           : TileSize::kSmall;
-    return tile_kernel(gate, out_type, size);
+    return tile_kernel(gate, fp8, wide, size);
 }
 
 int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *x, int64_t ldx, int64_t x_rows,
@@ -70,6 +70,8 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
 {
     constexpr int64_t kMax = std::numeric_limits<int64_t>::max();
     if (M < 0 || E < 1 || N < 1 || K < 1 || x_rows < 0) return fail(EB_ERR_INVALID, "%s: M or x_rows below 0, or E, N or K below 1", who);
+    const bool exact = (act & EB_EXACT_SUMS) != 0;
+    act &= ~EB_EXACT_SUMS;
     if (act != EB_ACT_NONE && act != EB_ACT_RELU && act != EB_ACT_SILU_GATE) return fail(EB_ERR_INVALID, "%s: unknown act", who);
     if (out_type != EB_F32 && out_type != EB_F16 && out_type != EB_BF16 && out_type != EB_FP8)
         return fail(EB_ERR_INVALID, "%s: unknown out_type", who);
@@ -123,7 +125,7 @@ int product_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, co
     const int es = element_bytes(out_type);
     a.vector_out = ldo * es % 16 == 0 && (uintptr_t)out % 16 == 0;
 
-    const KernelPlan plan = choose_kernel(M, E, N, ldx, ldw, tokens != nullptr, x_rows, gate, out_type);
+    const KernelPlan plan = choose_kernel(M, E, N, ldx, ldw, tokens != nullptr, x_rows, gate, out_type, exact);
     a.column_tiles = (int32_t)((width + plan.columns - 1) / plan.columns);
     // At most one tile per expert is not full.
     const int64_t most_tiles = std::min<int64_t>(offsets ? M / plan.height + E : (M + plan.height - 1) / plan.height, M);

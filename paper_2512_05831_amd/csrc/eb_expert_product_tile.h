@@ -322,7 +322,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void eb_product_tile(ProductArgs a)
 
     finish<R, T, S::kGate>(a, tile.expert, column, sum);
     if constexpr (S::kWide && !S::kFp8) {
-        // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.
+        // fp32: a lane's four outputs are 16 bytes, four lanes' 64 of a line.  (16-bit
+        // outputs of exact sums: half of that.)
         int32_t slot[T];
 #pragma unroll
         for (int t = 0; t < T; ++t) slot[t] = slot_of[(across_t * T + t) * 16 + lane % 16];

@@ -19,13 +19,16 @@ KernelPlan plan_of(TileSize size)
 
 } // namespace
 
-// 16-bit outputs: the 8-bit matrix unit.  fp32 and 8-bit outputs (whose scales
-// are fp32): the 16-bit unit, exact.
-KernelPlan tile_kernel(bool gate, int32_t out_type, TileSize size)
+// `wide`: the 16-bit matrix unit, exact.  fp32 and 8-bit outputs (whose scales are
+// fp32) always, 16-bit outputs where the caller asks for it: they are then stored
+// as fp32 ones are, four of a token by a lane.  bf16 out in the 8-bit unit and exact:
+// 16384 slots by 4096 x 3328 205 and 336 us, 65536 of 64 experts by 1024 x 1024 96 and
+// 150, 2048 by 1000 x 1512 11.1 and 12.8; 0.5 % of the last outputs differ, in their last bit.
+KernelPlan tile_kernel(bool gate, bool fp8, bool wide, TileSize size)
 {
-    if (out_type == EB_F16 || out_type == EB_BF16) return gate ? plan_of<false, true, false>(size) : plan_of<false, false, false>(size);
-    if (out_type == EB_FP8) return gate ? plan_of<true, true, true>(size) : plan_of<true, false, true>(size);
-    return gate ? plan_of<true, true, false>(size) : plan_of<true, false, false>(size);
+    if (fp8) return gate ? plan_of<true, true, true>(size) : plan_of<true, false, true>(size);
+    if (wide) return gate ? plan_of<true, true, false>(size) : plan_of<true, false, false>(size);
+    return gate ? plan_of<false, true, false>(size) : plan_of<false, false, false>(size);
 }
 
 } // namespace eb_product

@@ -24,6 +24,7 @@ EB_FP8 = 3
 EB_SOFTMAX, EB_SIGMOID = 0, 1
 EB_RENORMALIZE, EB_GROUP_PAIR = 0x100, 0x200
 EB_ACT_NONE, EB_ACT_RELU, EB_ACT_SILU_GATE = 0, 1, 2
+EB_EXACT_SUMS = 0x100
 BLOCK = 128
 
 _lib = None
@@ -259,7 +260,9 @@ def product(x, x_scales, w, w_scales, offsets=None, tokens=None, bias=None, act:
     None, as ``route`` gives them; ``bias``: fp32 [N] or [E, N].  Returns the
     output [slots, width] of ``out_dtype`` (bfloat16), or for float8_e4m3fn
     (output, scales [slots, ceil(width/128)]).  Slots of no expert are not
-    written.  ``out``: the floating-point output, with unit column stride."""
+    written.  ``out``: the floating-point output, with unit column stride.
+    ``act`` | EB_EXACT_SUMS: 16-bit outputs too from sums exact to fp32's
+    rounding."""
     import torch
 
     if stream is None and -1 < x.get_device() == _gpu():
@@ -289,7 +292,7 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
     if wk != K:
         raise ValueError("w must be [N, K] or [E, N, K]")
     ldx, kb = _pitch(x, "x"), (K + BLOCK - 1) // BLOCK
-    gate = act == EB_ACT_SILU_GATE
+    gate = act & ~EB_EXACT_SUMS == EB_ACT_SILU_GATE
     width = N // 2 if gate else N
     blocks = (width + BLOCK - 1) // BLOCK
     if x_scales.dtype != f32 or x_scales.shape != (rows, kb):
@@ -361,7 +364,7 @@ class ExpertLayer:
         if w_up.dim() != 3 or w_down.dim() != 3 or router.dim() != 2:
             raise ValueError("w_up and w_down must be 3-D, router 2-D")
         E, N, K = w_up.shape
-        gate = act == EB_ACT_SILU_GATE
+        gate = act & ~EB_EXACT_SUMS == EB_ACT_SILU_GATE
         if gate and N % 2 or tuple(w_down.shape[::2]) != (E, N // 2 if gate else N) or router.shape[1] != K:
             raise ValueError("w_up [E, N, K], w_down [E, D, N or N / 2] and router [experts, K] do not fit")
         self.E, self.K, self.D, self.top, self.act, self.mode = E, K, int(w_down.shape[1]), top, act, mode

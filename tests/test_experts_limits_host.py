@@ -2,7 +2,7 @@
 device is touched.
 """
 from paper_2512_05831_amd import eb, experts as ex
-from test_experts_host import U, code_of, product, route
+from test_experts_host import I, U, code_of, product, route
 
 
 def test_product_refuses_experts_beyond_32_bit_steps():
@@ -21,3 +21,10 @@ def test_workspace_refuses_what_the_route_refuses():
     for K in (65, 1024):
         assert code_of(route, N=1000, E=1024, ld=1024, K=K, shard_hi=1024) == U
         assert code_of(ex.eb_route_experts_workspace, N=1000, E=1024, K=K, shard_lo=0, shard_hi=1024) == U
+
+
+def test_product_rejects_unknown_bits_of_act():
+    for act in (ex.EB_EXACT_SUMS | 3, 0x200, ex.EB_EXACT_SUMS | 0x200, -1):
+        assert code_of(product, act=act) == I
+    assert code_of(product, act=ex.EB_EXACT_SUMS | ex.EB_ACT_SILU_GATE, N=255) == I
+    product(act=ex.EB_EXACT_SUMS, M=0, x_rows=0, ldxs=0)
