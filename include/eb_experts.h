@@ -166,7 +166,8 @@ int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x,
  *   bias         device fp32 [E, N] added to the sums, or NULL.
  *   act          EB_ACT_NONE; EB_ACT_RELU: max(v, 0); EB_ACT_SILU_GATE (even
  *                N): with g = v[n], u = v[N/2 + n], n < N/2, the output is
- *                g / (1 + exp(-g)) * u, N/2 wide.  Optionally | EB_EXACT_SUMS.
+ *                g / (1 + exp(-g)) * u, N/2 wide, the quotient within 4 + |g|
+ *                ulp of fp32, or 2^-119.  Optionally | EB_EXACT_SUMS.
  *   out_type     EB_F32, EB_F16, EB_BF16 or EB_FP8.
  *   out          device, rows ldo elements (>= the output's width) apart,
  *                element-aligned.  EB_FP8: e4m3, 16-byte aligned, ldo a

@@ -23,7 +23,7 @@ KernelPlan plan_of(TileSize size)
 // fp32) always, 16-bit outputs where the caller asks for it: they are then stored
 // as fp32 ones are, four of a token by a lane.  bf16 out in the 8-bit unit and exact:
 // 16384 slots by 4096 x 3328 205 and 336 us, 65536 of 64 experts by 1024 x 1024 96 and
-// 150, 2048 by 1000 x 1512 11.1 and 12.8; 0.5 % of the last outputs differ, in their last bit.
+// 150, 2048 by 1000 x 1512 11.1 and 12.8; of the last, 0.5 % of the outputs differ, in their last bit.
 KernelPlan tile_kernel(bool gate, bool fp8, bool wide, TileSize size)
 {
     if (fp8) return gate ? plan_of<true, true, true>(size) : plan_of<true, false, true>(size);

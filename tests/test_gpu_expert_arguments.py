@@ -99,3 +99,36 @@ def test_calls_go_to_the_tensors_gpu(device, monkeypatch):
         assert entered.devices and set(entered.devices) == {device.index}
         for a, b in zip(got if isinstance(got, tuple) else (got,), result if isinstance(result, tuple) else (result,)):
             assert torch.equal(a.view(torch.uint8) if a.dtype == torch.float8_e4m3fn else a, b.view(torch.uint8) if b.dtype == torch.float8_e4m3fn else b)
+
+
+def test_layer_without_tokens(device):
+    layer = layer_of(8, 256, 128, 64, 2, ex.EB_ACT_SILU_GATE, device)
+    assert layer.forward(torch.empty(0, 256, device=device)).shape == (0, 64)
+
+
+@pytest.mark.parametrize("M", [30, 3000])
+def test_product_and_quantize_on_another_stream(M, device):
+    """The stream that is given carries the call: what it has to wait for is written there just before."""
+    case = Case(M, 512, 700, device, E=3, act=ex.EB_ACT_SILU_GATE, counts=[M // 3, 1, M - M // 3 - 1], gather=200)
+    x = torch.randn(M, 700, device=device)
+    want, want8, wantq = case.run(), case.run(out_dtype=torch.float8_e4m3fn), ex.quantize_fp8(x)
+    wantw = ex.quantize_fp8(x, block_rows=128)
+    held, scales, values = case.x.clone(), case.xs.t().contiguous().t(), x.clone()
+    pitched = torch.zeros(held.shape[0], 704, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)[:, :700]
+    late_x, late_s, late_v = pitched, torch.zeros_like(case.xs.t().contiguous()).t(), torch.zeros_like(x)
+    big = torch.randn(4096, 4096, device=device)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):  # holds the side stream back
+            big = big @ big * 1e-3
+        late_x.view(torch.uint8).copy_(held.view(torch.uint8))
+        late_s.copy_(scales)
+        late_v.copy_(values)
+    case.x, case.xs = late_x, late_s
+    got, got8 = case.run(stream=side), case.run(out_dtype=torch.float8_e4m3fn, stream=side)
+    gotq, gotw = ex.quantize_fp8(late_v, stream=side), ex.quantize_fp8(late_v, block_rows=128, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    for mine, other in ((got8, want8), (gotq, wantq), (gotw, wantw)):
+        assert torch.equal(mine[0].view(torch.uint8), other[0].view(torch.uint8)) and torch.equal(mine[1], other[1])

@@ -45,3 +45,53 @@ def test_large_products_among_small_ones(dtype, M, N, act, device):
     assert torch.equal(wide[:, 5:5 + N], exact.to(dtype)) and (wide[:, :5] == 7.0).all() and (wide[:, 5 + N:] == 7.0).all()
     off = (call(act, out_dtype=dtype).double() - exact).abs()
     assert (off <= 448.0 ** 2 * 2.0 ** -10 * (1 + 2.0 ** -8) + 2.0 ** -8 * exact.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("K", [640, 3328, 1000])
+@pytest.mark.parametrize("act", [ex.EB_ACT_NONE, ex.EB_ACT_RELU])
+def test_small_integers_are_rounded_once(dtype, M, N, K, act, device):
+    """Products below 2^5 and sums below 2^17: exact in either matrix unit, then one rounding."""
+    g = torch.Generator().manual_seed(M + K)
+    pitch = -(-K // 16) * 16
+    x, w = integers(M, pitch, g, device), integers(N, pitch, g, device)
+    xs, ws = unit_scales(M, N, K, device)
+    got = ex.product(x.to(FP8)[:, :K], xs * 0.5, w.to(FP8)[:, :K], ws * 4.0, act=act, out_dtype=dtype)
+    want = 2 * x[:, :K].double() @ w[:, :K].double().t()
+    want = want.clamp(min=0) if act == ex.EB_ACT_RELU else want
+    assert torch.equal(got, want.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,N", SIZES)
+def test_sums_that_cancel(dtype, M, N, device):
+    """Two blocks of 128 whose exact sums are each other's opposite, their inputs in another order: what is left is
+    the two sums' error, each at most 1.5e-5 (and a tenth) of the sums' root mean square."""
+    g = torch.Generator().manual_seed(N)
+    draw = lambda rows: (torch.randn(rows, 128, generator=g) * 100).clamp(-448, 448).to(FP8).float().to(device)  # noqa: E731
+    x, w, order = draw(M), draw(N), torch.randperm(128, generator=g).to(device)
+    xs, ws = unit_scales(M, N, 256, device)
+    scale = 2.0 ** -10  # keeps fp16 from its ends
+    got = ex.product(torch.cat([x, x[:, order]], 1).to(FP8), xs * scale, torch.cat([w, -w[:, order]], 1).to(FP8), ws, out_dtype=dtype)
+    rms = (x.double() @ w.double().t()).pow(2).mean().sqrt() * scale
+    assert got.double().pow(2).mean().sqrt() <= 2 * 1.1 * 1.5e-5 * rms
+
+
+@pytest.mark.parametrize("M", [16, 400, 20000])
+def test_gate_over_its_range(M, device):
+    """g / (1 + exp(-g)) for any g: one input under a scale, and a bias of 1 for what is gated.  Within 4 + |g| ulp, or
+    2^-119 (a reciprocal below fp32's normal numbers)."""
+    N = 256
+    g = torch.linspace(-130, 130, M, device=device)
+    g[: M // 4] = torch.linspace(-4, 4, M // 4, device=device)
+    w = torch.zeros(N, 16, device=device)
+    w[: N // 2, 0] = 1.0
+    x = torch.zeros(M, 16, device=device)
+    x[:, 0] = 1.0
+    bias = torch.zeros(N, device=device)
+    bias[N // 2:] = 1.0
+    y = ex.product(x.to(FP8), g[:, None], w.to(FP8), torch.ones(2, 1, device=device), bias=bias, act=ex.EB_ACT_SILU_GATE, out_dtype=torch.float32)
+    d = g.double()
+    want = (d * torch.sigmoid(d))[:, None]
+    assert ((y.double() - want).abs() <= (4 + d.abs()[:, None]) * 2.0 ** -23 * want.abs() + 2.0 ** -119).all()
