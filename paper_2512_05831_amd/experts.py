@@ -357,10 +357,19 @@ class ExpertLayer:
     128 x 128; ``router``: [experts, K] fp32, whose rows give the scores of all
     experts.  Row-wise over several GPUs, a GPU holds the experts
     [shard_lo, shard_lo + E) of them, as a row shard of a table holds rows: its
-    results are partial sums, to be added over the GPUs (``sum_partials``)."""
+    results are partial sums, to be added over the GPUs (``sum_partials``).
+
+    ``row_dtype``: the type in which the experts' rows wait to be joined, fp32,
+    fp16 or bf16 (the default: one rounding to 8 bits of mantissa, beside hidden
+    values that have 4; half of fp32's bytes, and the 8-bit matrix unit for the
+    second product: 16384 tokens, 4 of 32 experts of 1024 x 512, 393 us, in fp32
+    417).  The joined sums are fp32.  ``act`` | EB_EXACT_SUMS holds
+    for both products."""
 
     def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = EB_SOFTMAX | EB_RENORMALIZE,
-                 bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0, shard_lo: int = 0):
+                 bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0, shard_lo: int = 0, row_dtype=None):
+        import torch
+
         if w_up.dim() != 3 or w_down.dim() != 3 or router.dim() != 2:
             raise ValueError("w_up and w_down must be 3-D, router 2-D")
         E, N, K = w_up.shape
@@ -370,6 +379,8 @@ class ExpertLayer:
         self.E, self.K, self.D, self.top, self.act, self.mode = E, K, int(w_down.shape[1]), top, act, mode
         self.router, self.bias, self.groups, self.top_groups, self.scale = router, bias, groups, top_groups, scale
         self.shard_lo = shard_lo
+        self.row_dtype = torch.bfloat16 if row_dtype is None else row_dtype
+        _code(self.row_dtype)
         # Under a gate each half of the rows is blocked on its own.
         parts = 2 if gate else 1
         q, s = quantize_fp8(w_up.contiguous().view(E * parts, N // parts, K), block_rows=BLOCK)
@@ -399,7 +410,7 @@ class ExpertLayer:
                   self.shard_lo + self.E)
         q, s = quantize_fp8(x)
         h, hs = product(q, s, self.w_up, self.up_scales, r.offsets, r.tokens, act=self.act, out_dtype=torch.float8_e4m3fn)
-        y = product(h, hs, self.w_down, self.down_scales, r.offsets, out_dtype=torch.bfloat16)
+        y = product(h, hs, self.w_down, self.down_scales, r.offsets, act=self.act & EB_EXACT_SUMS, out_dtype=self.row_dtype)
         bags = torch.arange(0, B * self.top + 1, self.top, dtype=torch.int32, device=x.device)
         # A token is a bag of its pairs' slots; a pair without one (-1) is skipped.
         slots = eb.EmbeddingBagTables([y])

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import experts as ex
+from test_gpu_expert_layer import layer_of
 
 pytestmark = pytest.mark.gpu
 SIZES = [(40, 200), (300, 1000), (2048, 1664), (2048, 4096), (8192, 4100)]
@@ -95,3 +96,26 @@ def test_gate_over_its_range(M, device):
     d = g.double()
     want = (d * torch.sigmoid(d))[:, None]
     assert ((y.double() - want).abs() <= (4 + d.abs()[:, None]) * 2.0 ** -23 * want.abs() + 2.0 ** -119).all()
+
+
+@pytest.mark.parametrize("rows", [None, torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("exact", [0, ex.EB_EXACT_SUMS])
+@pytest.mark.parametrize("B", [5, 1500])
+def test_layer_joins_rows_of_the_type_asked_for(rows, exact, B, device):
+    """The layer's result is the weighted sum of the second product's rows in that type: top products and sums in fp32."""
+    top = 3
+    g = torch.Generator(device=device).manual_seed(B)
+    w_up, w_down, router, x, scores = (torch.randn(*n, generator=g, device=device) for n in ((8, 768, 256), (8, 200, 384), (8, 256), (B, 256), (B, 8)))
+    layer = ex.ExpertLayer(w_up / 16, w_down / 16, router, top, act=ex.EB_ACT_SILU_GATE | exact, row_dtype=rows)
+    r = ex.route(scores, top)
+    h, hs = ex.product(*ex.quantize_fp8(x), layer.w_up, layer.up_scales, r.offsets, r.tokens, act=ex.EB_ACT_SILU_GATE, out_dtype=FP8)
+    y = ex.product(h, hs, layer.w_down, layer.down_scales, r.offsets, act=exact, out_dtype=rows or torch.bfloat16).double()
+    each = y[r.slots.long()] * r.weights.double()[:, :, None]
+    off = (layer.forward(x, scores).double() - each.sum(1)).abs()
+    assert (off <= 2 * top * 2.0 ** -24 * each.abs().sum(1)).all()
+
+
+def test_layer_refuses_rows_of_other_types(device):
+    for rows in (FP8, torch.float64, torch.int32):
+        with pytest.raises(ValueError):
+            layer_of(2, 16, 16, 16, 1, ex.EB_ACT_RELU, device, row_dtype=rows)
