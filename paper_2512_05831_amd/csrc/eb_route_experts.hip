@@ -695,8 +695,9 @@ int route_impl(const char *who, int64_t N, int32_t E, int32_t K, const void *sco
     const hipStream_t s = (hipStream_t)stream;
     if (N == 0) {
         if (!offsets) return EB_OK;
-        hipLaunchKernelGGL(eb_route_none, dim3(1), dim3(kThreads), 0, s, offsets, held + 1);
-        const hipError_t err = hipGetLastError();
+        int32_t n = held + 1;
+        void *args[] = {&offsets, &n};
+        const hipError_t err = hipLaunchKernel((const void *)eb_route_none, dim3(1), dim3(kThreads), args, 0, s);
         return err == hipSuccess ? EB_OK : fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
     }
     RouteArgs a{};

@@ -132,3 +132,18 @@ def test_product_and_quantize_on_another_stream(M, device):
     assert torch.equal(got, want)
     for mine, other in ((got8, want8), (gotq, wantq), (gotw, wantw)):
         assert torch.equal(mine[0].view(torch.uint8), other[0].view(torch.uint8)) and torch.equal(mine[1], other[1])
+
+
+def test_an_older_error_is_not_the_calls(device):
+    """An error that another call left with the runtime on this thread is not reported as the route's."""
+    from paper_2512_05831_amd import eb
+
+    runtime = eb.library()  # its runtime's functions are found through it
+    x = torch.empty(0, 32, device=device)
+    ex.route(x, 4)
+    assert runtime.hipSetDevice(1 << 20) != 0
+    try:
+        r = ex.route(x, 4, shard_lo=8, shard_hi=24)
+    finally:
+        runtime.hipGetLastError()
+    assert r.offsets.tolist() == [0] * 17
