@@ -18,7 +18,7 @@ import functools
 from typing import NamedTuple
 
 from . import eb
-from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, _check, _stream_ptr
+from .eb import EB_BF16, EB_F16, EB_F32, EB_SUM, _check
 
 EB_FP8 = 3
 EB_SOFTMAX, EB_SIGMOID = 0, 1
@@ -107,6 +107,16 @@ def _gpu() -> int:
     return _gpu()
 
 
+def _raw_stream(index: int) -> int:
+    """The hipStream_t of GPU ``index``'s current stream; from the second call on
+    torch's own query itself, where it offers one."""
+    global _raw_stream
+    import torch
+
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(index)
+
+
 def _place(torch, x, stream):
     """Where a call on ``x`` belongs, as a context.  Under a ``stream``
     allocations are the stream's: what the caching allocator hands out again is
@@ -192,7 +202,7 @@ def _route(torch, scores, top, mode, bias, groups, top_groups, scale, lo, hi, gr
     rc = lib.eb_route_experts(
         N, E, top, scores.data_ptr(), dtype, ld, bias_ptr, mode, groups, top_groups, scale, lo, hi, ids.data_ptr(),
         weights.data_ptr(), offsets.data_ptr() if grouped else None, tokens.data_ptr() if grouped else None,
-        slots.data_ptr() if grouped else None, ws.data_ptr() if nbytes else None, nbytes, _stream_ptr(stream, dev))
+        slots.data_ptr() if grouped else None, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index) if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)
     return Route(ids, weights, offsets, tokens, slots)
@@ -243,7 +253,7 @@ def _quantize(torch, x, block_rows, stream):
         scales = x.new_empty((m, _blocks(rows), blocks), dtype=torch.float32)
         lds, shaped = 0, scales if dim == 3 else scales[0]
     rc = (_lib or library()).eb_quantize_fp8(m, rows, cols, x.data_ptr(), dtype, ldx, block_rows, q.data_ptr(), pitch,
-                                             scales.data_ptr(), lds, _stream_ptr(stream, x.device))
+                                             scales.data_ptr(), lds, _raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)
     return (q if pitch == cols else q[..., :cols]), shaped
@@ -302,9 +312,9 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
         x_scales = x_scales.t().contiguous().t()
         by_block = rows
     ldxs = by_block if kb > 1 else rows
-    halves = 2 if gate else 1
-    if w_scales.dtype != f32 or not w_scales.is_contiguous() or w_scales.numel() != halves * E * blocks * kb or \
-            w_scales.dim() < 2 or w_scales.shape[-1] != kb or w_scales.shape[-2] not in (blocks, halves * blocks):
+    lines = 2 * blocks if gate else blocks
+    if w_scales.dtype != f32 or not w_scales.is_contiguous() or w_scales.shape != ((lines, kb) if w.dim() == 2 else (E, lines, kb)) and (
+            w_scales.numel() != E * lines * kb or w_scales.shape[-1:] != (kb,) or w_scales.shape[-2:-1] not in ((lines,), (blocks,))):
         raise ValueError("w_scales must be contiguous fp32 [.., blocks of N, ceil(K/128)], a scale per 128 x 128 of w")
     M, offsets_ptr, tokens_ptr, bias_ptr = rows, None, None, None
     if offsets is not None:
@@ -321,7 +331,7 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
         bias_ptr = bias.data_ptr()
     _same_device(dev, x_scales, w, w_scales, offsets, tokens, bias, out)
     scales_ptr, scales = None, None
-    if out is not None and out_dtype not in (None, out.dtype):
+    if out is not None and out_dtype is not None and out_dtype != out.dtype:
         raise ValueError("out is of another type than out_dtype")
     code = _code(out.dtype if out is not None else torch.bfloat16 if out_dtype is None else out_dtype, fp8=True)
     if code == EB_FP8:
@@ -340,7 +350,7 @@ def _product(torch, x, x_scales, w, w_scales, offsets, tokens, bias, act, out_dt
         ldo = _pitch(out, "out")
     rc = (_lib or library()).eb_expert_product(
         M, E, N, K, x.data_ptr(), ldx, rows, x_scales.data_ptr(), ldxs, tokens_ptr, w.data_ptr(), ldw, w_scales.data_ptr(),
-        offsets_ptr, bias_ptr, act, code, out.data_ptr(), ldo, scales_ptr, M, _stream_ptr(stream, dev))
+        offsets_ptr, bias_ptr, act, code, out.data_ptr(), ldo, scales_ptr, M, _raw_stream(dev.index) if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)
     if code == EB_FP8:
