@@ -96,8 +96,9 @@ int eb_route_experts_workspace(int64_t N, int32_t E, int32_t K, int32_t shard_lo
  *                bytes, 4-byte aligned, owned by the caller; contents not
  *                kept.  May be NULL where that is 0, or offsets NULL.
  *
- * Scores, sums and weights are fp32 whatever the type of x.  Equal calls give
- * equal bits.  Errors: EB_ERR_INVALID for an argument outside the above,
+ * Scores, sums and weights are fp32 whatever the type of x; a softmax's
+ * exponentials are within 2 ulp, and 0 below 2^-126.  Equal calls give equal bits.
+ * Errors: EB_ERR_INVALID for an argument outside the above,
  * EB_ERR_UNSUPPORTED for E, K, groups or N * K beyond the limits or 2^28 tokens
  * and more, EB_ERR_HIP when a launch fails.  N == 0 writes zero offsets.
  */
@@ -130,7 +131,7 @@ int eb_route_experts(int64_t N, int32_t E, int32_t K, const void *scores, int32_
  * even.  The value held is q * scale.  A block with an infinity or a NaN has the
  * scale NaN and only NaNs.  Errors:
  * EB_ERR_INVALID for an argument outside the above, EB_ERR_UNSUPPORTED for
- * sizes one launch does not hold (2^24 strips of 16 rows by 512 columns, or of
+ * sizes one launch does not hold (2^24 strips of 16 rows by 256 columns, or of
  * 128 x 128), EB_ERR_HIP when a launch fails.
  */
 int eb_quantize_fp8(int32_t matrices, int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx,

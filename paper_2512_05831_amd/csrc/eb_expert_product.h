@@ -16,8 +16,9 @@
 // The 8-bit matrix unit adds the products of eight neighbouring k with the bits
 // cut that lie more than 13 below the largest of the eight: measured 1.5e-5 of
 // the root mean square of sums of 128 normal values, with either instruction
-// (16x16x128, 16x16x32).  The 16-bit unit is exact to fp32 on the same values,
-// widened (9e-9), at half the rate.
+// (16x16x128, 16x16x32), and in general less than 2^-10 of the largest of each
+// eight.  The 16-bit unit is exact to fp32 on the same values, widened (9e-9), at
+// half the rate.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -42,7 +42,10 @@ int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1
 //   Medium against small, 16-bit unit: 4000 slots by 1000 x 1520 (504 tiles) 18.0 and
 //   20.5, 16 experts of 512 x 2048 with 375 slots (384) 22.1 and 24.2; but 32 experts
 //   of 1024 x 2048 with 100 slots (512) 29.9 and 26.6.  8-bit unit: 16 experts of 512 x
-//   2048 with 375 slots 15.4 and 18.7 (medium of 256 rows).
+//   2048 with 375 slots 15.4 and 18.7 (medium of 256 rows).  Pieces are counted with 128
+//   rows where medium and small tiles have 256 too (a gate with 8-bit outputs).  Tiles against
+//   each other have not been timed for means below 100 slots, nor for one GPU's shard, whose
+//   M holds every GPU's slots.
 KernelPlan choose_kernel(int64_t M, int32_t E, int64_t N, int64_t ldx, int64_t ldw, bool gathered, int64_t x_rows, bool gate,
                          int32_t out_type, bool exact)
 {

@@ -20,10 +20,11 @@
 // so it is the global addresses that are permuted.)
 //
 // Measured on random normal values in long runs: 16384 slots by 4096 x 3328 in the
-// 8-bit unit 195 us, 2.3 PFLOP/s (four waves 212); 65536 gathered slots of 64
-// experts by 2048 x 1024, gated, in the 16-bit unit 264 us, 1.04 PFLOP/s (eight
-// waves 286).  Zeros take four fifths of that time: the clock falls with the bits
-// that change, which is also why fewer copies count.  In the 16-bit unit a wave
+// 8-bit unit 203 us, 2.2 PFLOP/s (against four waves, timed in turn, 195 and 212;
+// 206 where all slots gather the same 256 rows: not the fetches); 65536 gathered
+// slots of 64 experts by 2048 x 1024, gated, in the 16-bit unit 264 us, 1.04 PFLOP/s
+// (eight waves 286).  Zeros take four fifths of that time: the clock falls with the bits
+// that change, which is also why fewer copies to LDS count.  In the 16-bit unit a wave
 // widens 12 tiles for 32 products (192 conversions at half rate beside 128 matrix
 // instructions): the vector unit is as busy as the matrix unit.
 #pragma once

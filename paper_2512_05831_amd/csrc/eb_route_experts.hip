@@ -24,7 +24,7 @@
 //         the lanes of a wave that hold the same expert find each other by
 //         ballots over the expert's bits) and writes them.
 // Choose is bound by vector instructions: 16384 tokens of 256 experts with sigmoid,
-// bias and pairs of groups 16 us (0.85 issued a cycle) for 16.8 MB that a copy would
+// bias and pairs of groups 16 us (0.82 issued a cycle) for 16.8 MB that a copy would
 // read in 4; scan and place are 4.5 and 5 us of latency there.
 // A launch costs more than the work of a small batch (2.4 us of the caller's time):
 // up to 16 tokens, or 128 of at most 64 experts, one workgroup does all of it (us
@@ -32,7 +32,7 @@
 // 6.8 and 7.2; but 64 tokens, 8 of 256 22.5 and 13.8).  Up to kFewPairs pairs there is
 // no scan: each workgroup that places kPart pairs counts all of them (8000 pairs of
 // 64 experts 13.7, three launches 17.6, on the GPU 10.8 and 11.3; 16000 pairs 13.9 and
-// 17.6, on the GPU 13.5 and 11.5).
+// 17.6, on the GPU 13.5 and 11.5: there it is the caller's time that is bought).
 
 #include <hip/hip_runtime.h>
 
