@@ -5,8 +5,10 @@
 ``csrc/eb_gather_narrow.hip``, ``csrc/eb_gather_narrow_weighted.hip``,
 ``csrc/eb_gather_wave.hip``, ``csrc/eb_gather_wave_weighted.hip``,
 ``csrc/eb_exchange.hip``, ``csrc/eb_ceiling.hip`` (the bandwidth probe the
-benchmark uses) and the experts' operators (``csrc/eb_route_experts.hip``,
-``csrc/eb_quantize_fp8.hip``, ``csrc/eb_expert_product*.hip``) and writes
+benchmark uses), the experts' operators (``csrc/eb_route_experts.hip``,
+``csrc/eb_quantize_fp8.hip``, ``csrc/eb_expert_product*.hip``) and those that
+train them (``csrc/eb_layer_norm*.hip``, ``csrc/eb_activation.hip``,
+``csrc/eb_sort_rows.hip``, ``csrc/eb_weight_gradient.hip``) and writes
 ``libeb.so`` next to this file.
 """
 from __future__ import annotations
@@ -22,7 +24,9 @@ SRCS = [os.path.join(HERE, "csrc", f)
                   "eb_gather_narrow_weighted.hip", "eb_gather_wave.hip",
                   "eb_gather_wave_weighted.hip", "eb_exchange.hip", "eb_ceiling.hip",
                   "eb_route_experts.hip", "eb_quantize_fp8.hip", "eb_expert_product.hip",
-                  "eb_expert_product_stream.hip", "eb_expert_product_tile.hip")]
+                  "eb_expert_product_stream.hip", "eb_expert_product_tile.hip",
+                  "eb_layer_norm.hip", "eb_layer_norm_backward.hip", "eb_activation.hip",
+                  "eb_sort_rows.hip", "eb_weight_gradient.hip")]
 LIB = os.path.join(HERE, "libeb.so")
 ARCH = "gfx950"
 

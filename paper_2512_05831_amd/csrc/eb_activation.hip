@@ -1,0 +1,253 @@
+// The experts' activation, of values that wait in 8 bits or in floating point, and
+// its gradient (include/eb_train.h): eb_activation, eb_activation_backward.
+//
+//   relu: h = max(v, 0), dv = dh where v > 0
+//   gate: h = g p u, dg = dh u p (1 + g (1 - p)), du = dh g p, p = 1 / (1 + e^-g)
+//
+// Element by element but for the scales: bound by memory.  Eight neighbours a lane,
+// 16 lanes a block of 128 that shares a scale; a workgroup takes 16 rows and up to
+// kSteps blocks along them, so that scales that are neighbours in memory are read and
+// written together.
+
+#include <type_traits>
+
+#include "eb_train.h"
+
+namespace {
+
+using namespace eb_train;
+
+constexpr int kThreads = 256;
+constexpr int kRows = kThreads / kLanes; // rows of a workgroup
+constexpr int kSteps = 2;                // block columns of a workgroup
+
+struct ActArgs {
+    const void *v, *dh;
+    Scales v_scales;
+    Out out;
+    int64_t rows, cols, ldv, lddh;
+    int64_t width;  // of v: cols, or under a gate twice that
+    int64_t blocks; // block columns that the workgroups walk
+    bool gate;
+};
+
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269502f)); }
+
+// Columns c .. c + 7 of v, of which those in [lo, hi) count.
+template <typename T>
+__device__ __forceinline__ void load_v(const ActArgs &a, int64_t row, int64_t c, int64_t lo, int64_t hi, float *f)
+{
+    const Raw<T> r = load_raw((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
+    widen8(r, f);
+    if constexpr (sizeof(T) == 1) scale8(f, scales_at(a.v_scales, row, c, hi));
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void eb_activate(ActArgs a)
+{
+    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
+    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    if (row >= a.rows) return;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int64_t c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        if (b0 + s >= a.blocks) return;
+        float g[kEach], h[kEach];
+        load_v<T>(a, row, c, 0, a.cols, g);
+        if (a.gate) {
+            float u[kEach];
+            load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) h[i] = g[i] > 0.f ? g[i] : g[i] == g[i] ? 0.f : g[i];
+        }
+        store_out(a.out, row, c, a.cols, h, a.out.type == EB_FP8 ? max_lanes<kLanes>(most8(h)) : 0);
+    }
+}
+
+__device__ __forceinline__ float d_gate(float dh, float g, float u)
+{
+    const float p = sigmoid(g);
+    return dh * u * p * (1.f + g * (1.f - p));
+}
+
+// dg and du by the lane that has both g and u: floating-point outputs, and 8-bit
+// ones whose blocks do not lie across the border between dg and du.
+template <typename D, typename T>
+__global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
+{
+    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
+    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    if (row >= a.rows) return;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int64_t c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        if (b0 + s >= a.blocks) return;
+        float dh[kEach], g[kEach], d[kEach];
+        widen8(load_raw((const D *)a.dh + row * a.lddh, c, a.cols), dh);
+        load_v<T>(a, row, c, 0, a.cols, g);
+        const bool fp8 = a.out.type == EB_FP8;
+        if (!a.gate) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) d[i] = g[i] > 0.f ? dh[i] : 0.f;
+            store_out(a.out, row, c, a.cols, d, fp8 ? max_lanes<kLanes>(most8(d)) : 0);
+            continue;
+        }
+        float u[kEach], e[kEach];
+        load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            d[i] = d_gate(dh[i], g[i], u[i]);
+            e[i] = dh[i] * g[i] * sigmoid(g[i]);
+        }
+        if (fp8) {
+            store_out(a.out, row, c, a.width, d, max_lanes<kLanes>(most8(d)));
+            store_out(a.out, row, a.cols + c, a.width, e, max_lanes<kLanes>(most8(e)));
+        } else {
+            store_out(a.out, row, c, a.cols, d, 0);
+            Out second = a.out;
+            second.p = (char *)a.out.p + a.cols * (a.out.type == EB_F32 ? 4 : 2);
+            store_out(second, row, c, a.cols, e, 0);
+        }
+    }
+}
+
+// A lane of a block of dv, which may lie across the border, takes dg where its
+// columns are g's, du where they are u's; dh, g and u are read for each.
+template <typename D, typename T>
+__global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
+{
+    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
+    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    if (row >= a.rows) return;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int64_t at = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        if (b0 + s >= a.blocks) return;
+        float d[kEach] = {}, e[kEach] = {}, dh[kEach], g[kEach], u[kEach];
+        auto both = [&](int64_t c, bool first) {
+            widen8(load_raw((const D *)a.dh + row * a.lddh, c, a.cols), dh);
+            load_v<T>(a, row, c, 0, a.cols, g);
+            if (first) {
+                load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) d[i] = c + i < a.cols ? d_gate(dh[i], g[i], u[i]) : 0.f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) e[i] = c + i >= 0 && c + i < a.cols ? dh[i] * g[i] * sigmoid(g[i]) : 0.f;
+            }
+        };
+        if (at < a.cols) both(at, true);
+        if (at + kEach > a.cols) both(at - a.cols, false);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) d[i] = at + i < a.cols ? d[i] : e[i];
+        store_out(a.out, row, at, a.width, d, max_lanes<kLanes>(most8(d)));
+    }
+}
+
+int check(const char *who, int64_t rows, int64_t cols, int32_t act, int32_t v_type, int32_t out_type)
+{
+    if (rows < 0 || cols < 1) return fail(EB_ERR_INVALID, "%s: negative rows, or no columns", who);
+    if (act != EB_ACT_RELU && act != EB_ACT_SILU_GATE) return fail(EB_ERR_INVALID, "%s: act must be EB_ACT_RELU or EB_ACT_SILU_GATE", who);
+    if ((!floating(v_type) && v_type != EB_FP8) || (!floating(out_type) && out_type != EB_FP8))
+        return fail(EB_ERR_INVALID, "%s: unknown v_type or out_type", who);
+    if (cols > (int64_t)1 << 29) return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^29 columns", who);
+    return EB_OK;
+}
+
+int launch_rows(const char *who, void *kernel, ActArgs &a, void *stream)
+{
+    const int64_t strips = (a.blocks + kSteps - 1) / kSteps, lines = a.rows / kRows + (a.rows % kRows != 0);
+    return launch(who, kernel, lines > kMax32 / strips ? kMax32 : lines * strips, kThreads, &a, stream);
+}
+
+int act_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const void *v, int32_t v_type, int64_t ldv, const float *v_scales,
+             int64_t ldvs, int32_t out_type, void *h, int64_t ldh, float *h_scales, int64_t ldhs, void *stream)
+{
+    if (int rc = check(who, rows, cols, act, v_type, out_type)) return rc;
+    ActArgs a{};
+    a.gate = act == EB_ACT_SILU_GATE;
+    a.width = a.gate ? 2 * cols : cols;
+    if (int rc = check_matrix(who, "v", v, v_type, rows, a.width, ldv, v_scales, ldvs)) return rc;
+    if (int rc = check_matrix(who, "h", h, out_type, rows, cols, ldh, h_scales, ldhs)) return rc;
+    if (rows == 0) return EB_OK;
+    a.v = v;
+    a.v_scales = {v_scales, ldvs};
+    a.out = {h, h_scales, ldh, ldhs, out_type};
+    a.rows = rows;
+    a.cols = cols;
+    a.ldv = ldv;
+    a.blocks = (cols + kBlock - 1) / kBlock;
+    void *kernel = v_type == EB_F32   ? (void *)eb_activate<float>
+                   : v_type == EB_F16 ? (void *)eb_activate<_Float16>
+                   : v_type == EB_FP8 ? (void *)eb_activate<Fp8>
+                                      : (void *)eb_activate<Bf16>;
+    return launch_rows(who, kernel, a, stream);
+}
+
+template <typename D>
+void *back_kernel(int32_t v_type, bool across)
+{
+    if (v_type == EB_F32) return across ? (void *)eb_activate_back_across<D, float> : (void *)eb_activate_back<D, float>;
+    if (v_type == EB_F16) return across ? (void *)eb_activate_back_across<D, _Float16> : (void *)eb_activate_back<D, _Float16>;
+    if (v_type == EB_FP8) return across ? (void *)eb_activate_back_across<D, Fp8> : (void *)eb_activate_back<D, Fp8>;
+    return across ? (void *)eb_activate_back_across<D, Bf16> : (void *)eb_activate_back<D, Bf16>;
+}
+
+int back_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const void *dh, int32_t dh_type, int64_t lddh, const void *v,
+              int32_t v_type, int64_t ldv, const float *v_scales, int64_t ldvs, int32_t out_type, void *dv, int64_t lddv, float *dv_scales,
+              int64_t lddvs, void *stream)
+{
+    if (int rc = check(who, rows, cols, act, v_type, out_type)) return rc;
+    if (!floating(dh_type)) return fail(EB_ERR_INVALID, "%s: unknown dh_type", who);
+    ActArgs a{};
+    a.gate = act == EB_ACT_SILU_GATE;
+    a.width = a.gate ? 2 * cols : cols;
+    if (int rc = check_matrix(who, "dh", dh, dh_type, rows, cols, lddh, nullptr, 0)) return rc;
+    if (int rc = check_matrix(who, "v", v, v_type, rows, a.width, ldv, v_scales, ldvs)) return rc;
+    if (int rc = check_matrix(who, "dv", dv, out_type, rows, a.width, lddv, dv_scales, lddvs)) return rc;
+    if (rows == 0) return EB_OK;
+    a.v = v;
+    a.dh = dh;
+    a.v_scales = {v_scales, ldvs};
+    a.out = {dv, dv_scales, lddv, lddvs, out_type};
+    a.rows = rows;
+    a.cols = cols;
+    a.ldv = ldv;
+    a.lddh = lddh;
+    const bool across = a.gate && out_type == EB_FP8 && cols % kBlock != 0;
+    a.blocks = ((across ? a.width : cols) + kBlock - 1) / kBlock;
+    void *kernel = dh_type == EB_F32   ? back_kernel<float>(v_type, across)
+                   : dh_type == EB_F16 ? back_kernel<_Float16>(v_type, across)
+                                       : back_kernel<Bf16>(v_type, across);
+    return launch_rows(who, kernel, a, stream);
+}
+
+} // namespace
+
+extern "C" int eb_activation(int64_t rows, int64_t cols, int32_t act, const void *v, int32_t v_type, int64_t ldv, const float *v_scales,
+                             int64_t ldvs, int32_t out_type, void *h, int64_t ldh, float *h_scales, int64_t ldhs, void *stream)
+{
+    try {
+        return act_impl("eb_activation", rows, cols, act, v, v_type, ldv, v_scales, ldvs, out_type, h, ldh, h_scales, ldhs, stream);
+    } catch (...) {
+        return eb_detail::unexpected_exception("eb_activation");
+    }
+}
+
+extern "C" int eb_activation_backward(int64_t rows, int64_t cols, int32_t act, const void *dh, int32_t dh_type, int64_t lddh, const void *v,
+                                      int32_t v_type, int64_t ldv, const float *v_scales, int64_t ldvs, int32_t out_type, void *dv,
+                                      int64_t lddv, float *dv_scales, int64_t lddvs, void *stream)
+{
+    try {
+        return back_impl("eb_activation_backward", rows, cols, act, dh, dh_type, lddh, v, v_type, ldv, v_scales, ldvs, out_type, dv, lddv,
+                         dv_scales, lddvs, stream);
+    } catch (...) {
+        return eb_detail::unexpected_exception("eb_activation_backward");
+    }
+}

@@ -1,0 +1,177 @@
+// Layer norm (include/eb_train.h): eb_layer_norm.
+//
+//   m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  n = (x - m) r,  y = n w + b
+//
+// A row stays in registers between the two sums and the outputs, so x is read and
+// y written once: bound by memory.  A wave holds up to kSteps * 512 columns, 8
+// neighbours a lane and step (16 lanes are a block of 128 that shares a scale); one
+// wave takes a row, or four.
+
+#include <type_traits>
+
+#include "eb_train.h"
+
+namespace {
+
+using namespace eb_train;
+
+constexpr int kThreads = 256;
+constexpr int kStride = kWave * kEach; // columns of a wave's step
+
+struct NormArgs {
+    const void *x;
+    const float *weight, *bias;
+    float *mean, *rstd;
+    Out y, kept;
+    int64_t rows, cols, ldx;
+    float eps;
+};
+
+// A sum over the kWaves waves of a row, in every lane.
+template <int kWaves>
+__device__ __forceinline__ float sum_row(float v, float *shared, int wave)
+{
+    v = sum_lanes<kWave>(v);
+    if constexpr (kWaves > 1) {
+        __syncthreads(); // the last sum has been read
+        if (threadIdx.x % kWave == 0) shared[wave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) v += shared[i];
+    }
+    return v;
+}
+
+__device__ __forceinline__ void normalise8(const NormArgs &a, int64_t row, int64_t c, const float *f, float mean, float rstd)
+{
+    if (c >= ((a.cols + kBlock - 1) & ~(int64_t)(kBlock - 1))) return; // whole blocks: their 16 lanes stay together
+    const int64_t left = a.cols - c;
+    float n[kEach], y[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) n[i] = i < left ? (f[i] - mean) * rstd : 0.f;
+    if (a.kept.p) store_out(a.kept, row, c, a.cols, n, max_lanes<kLanes>(most8(n)));
+    float w[kEach], b[kEach];
+    if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
+    if (a.bias) widen8(load_raw(a.bias, c, a.cols), b);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        y[i] = a.weight ? n[i] * w[i] : n[i];
+        if (a.bias) y[i] += b[i];
+    }
+    store_out(a.y, row, c, a.cols, y, a.y.type == EB_FP8 ? max_lanes<kLanes>(most8(y)) : 0);
+}
+
+// kSteps * 512 columns a wave; kLoop: any number of them, read again for each sum.
+template <typename T, int kSteps, int kWaves, bool kLoop>
+__global__ __launch_bounds__(kThreads) void eb_layer_norm_rows(NormArgs a)
+{
+    __shared__ float shared[kWaves];
+    constexpr int kRows = kThreads / kWave / kWaves;
+    const int wave = threadIdx.x / kWave % kWaves;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kWave / kWaves;
+    if (row >= a.rows) return; // whole workgroups where waves share a row
+    const T *x = (const T *)a.x + row * a.ldx;
+    const int64_t first = (wave * kWave + threadIdx.x % kWave) * kEach;
+    constexpr int64_t kAll = (int64_t)kStride * kWaves;
+    float f[kLoop ? 1 : kSteps][kEach];
+    float sum = 0.f;
+    auto over = [&](auto &&each) {
+        if constexpr (kLoop) {
+            for (int64_t c = first; c < ((a.cols + kBlock - 1) & ~(int64_t)(kBlock - 1)); c += kAll) {
+                widen8(load_raw(x, c, a.cols), f[0]);
+                each(c, f[0]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) each(first + i * kAll, f[i]);
+        }
+    };
+    if constexpr (!kLoop) {
+        Raw<T> raw[kSteps];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(x, first + i * kAll, a.cols);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) widen8(raw[i], f[i]);
+    }
+    over([&](int64_t, const float *v) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum += v[i];
+    });
+    const float mean = sum_row<kWaves>(sum, shared, wave) / (float)a.cols;
+    float square = 0.f;
+    over([&](int64_t c, const float *v) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const float d = c + i < a.cols ? v[i] - mean : 0.f;
+            square = fmaf(d, d, square);
+        }
+    });
+    const float rstd = 1.f / sqrtf(sum_row<kWaves>(square, shared, wave) / (float)a.cols + a.eps);
+    if (threadIdx.x % (kWaves * kWave) == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    over([&](int64_t c, const float *v) { normalise8(a, row, c, v, mean, rstd); });
+}
+
+struct Plan {
+    void *kernel;
+    int rows; // of a workgroup
+};
+
+template <typename T>
+Plan plan_of(int64_t rows, int64_t cols)
+{
+    if (cols > 8 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 1, 4, true>, 1};
+    if (cols > 8 * kStride) return {(void *)(cols > 4 * 4 * kStride ? eb_layer_norm_rows<T, 8, 4, false> : eb_layer_norm_rows<T, 4, 4, false>), 1};
+    if (cols > 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 1, false>, 4};
+    if (cols > 2 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 1, false>, 4};
+    if (cols > kStride) return {(void *)eb_layer_norm_rows<T, 2, 1, false>, 4};
+    return {(void *)eb_layer_norm_rows<T, 1, 1, false>, 4};
+}
+
+int norm_impl(const char *who, int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx, const float *weight, const float *bias,
+              float eps, int32_t out_type, void *y, int64_t ldy, float *y_scales, int64_t ldys, void *kept, int64_t ldk, float *kept_scales,
+              int64_t ldks, float *mean, float *rstd, void *stream)
+{
+    if (rows < 0 || cols < 1) return fail(EB_ERR_INVALID, "%s: negative rows, or no columns", who);
+    if (!floating(dtype) || (!floating(out_type) && out_type != EB_FP8)) return fail(EB_ERR_INVALID, "%s: unknown dtype or out_type", who);
+    if (!(eps >= 0.f)) return fail(EB_ERR_INVALID, "%s: eps below 0", who);
+    if (cols > (int64_t)1 << 30) return fail(EB_ERR_UNSUPPORTED, "%s: more than 2^30 columns", who);
+    if (int rc = check_matrix(who, "x", x, dtype, rows, cols, ldx, nullptr, 0)) return rc;
+    if (int rc = check_matrix(who, "y", y, out_type, rows, cols, ldy, y_scales, ldys)) return rc;
+    if (kept)
+        if (int rc = check_matrix(who, "kept", kept, EB_FP8, rows, cols, ldk, kept_scales, ldks)) return rc;
+    if (rows == 0) return EB_OK;
+    NormArgs a{};
+    a.x = x;
+    a.weight = weight;
+    a.bias = bias;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.y = {y, y_scales, ldy, ldys, out_type};
+    a.kept = {kept, kept_scales, ldk, ldks, EB_FP8};
+    a.rows = rows;
+    a.cols = cols;
+    a.ldx = ldx;
+    a.eps = eps;
+    const Plan plan = dtype == EB_F32   ? plan_of<float>(rows, cols)
+                      : dtype == EB_F16 ? plan_of<_Float16>(rows, cols)
+                                        : plan_of<Bf16>(rows, cols);
+    return launch(who, plan.kernel, rows / plan.rows + (rows % plan.rows != 0), kThreads, &a, stream);
+}
+
+} // namespace
+
+extern "C" int eb_layer_norm(int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx, const float *weight, const float *bias,
+                             float eps, int32_t out_type, void *y, int64_t ldy, float *y_scales, int64_t ldys, void *kept, int64_t ldk,
+                             float *kept_scales, int64_t ldks, float *mean, float *rstd, void *stream)
+{
+    try {
+        return norm_impl("eb_layer_norm", rows, cols, x, dtype, ldx, weight, bias, eps, out_type, y, ldy, y_scales, ldys, kept, ldk,
+                         kept_scales, ldks, mean, rstd, stream);
+    } catch (...) {
+        return eb_detail::unexpected_exception("eb_layer_norm");
+    }
+}

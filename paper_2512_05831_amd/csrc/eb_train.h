@@ -1,0 +1,248 @@
+// Shared by what trains a layer of experts (eb_layer_norm*.hip, eb_activation.hip,
+// eb_sort_rows.hip, eb_weight_gradient*); not part of the C ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <limits>
+
+#include "../../include/eb.h"
+#include "../../include/eb_experts.h"
+#include "../../include/eb_train.h"
+#include "eb_experts.h"
+#include "eb_internal.h"
+
+namespace eb_train {
+
+using namespace eb_experts;
+using eb_detail::fail;
+
+constexpr int kEach = 8;               // neighbouring values that a lane holds
+constexpr int kLanes = kBlock / kEach; // lanes of a block that shares a scale
+constexpr int64_t kMax64 = std::numeric_limits<int64_t>::max();
+constexpr int64_t kMax32 = std::numeric_limits<int32_t>::max();
+
+struct Fp8 {
+    uint8_t bits;
+};
+
+// Accesses of any alignment: the hardware's, at their full width.
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef int i32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+// Eight neighbouring values as they lie in memory.
+template <typename T>
+struct Raw {
+    T v[kEach];
+};
+
+// Those from column c of a row; zeros outside [0, cols).
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int64_t c, int64_t cols)
+{
+    Raw<T> r;
+    if (c >= 0 && c + kEach <= cols) {
+        if constexpr (sizeof(T) == 1) {
+            const i32x2_any w = *(const i32x2_any *)(row + c);
+            __builtin_memcpy(&r, &w, 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const i32x4_any w = *(const i32x4_any *)((const char *)(row + c) + 16 * i);
+                __builtin_memcpy((char *)&r + 16 * i, &w, 16);
+            }
+        }
+    } else {
+        __builtin_memset(&r, 0, sizeof(r));
+        if (c < cols && c + kEach > 0) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (c + i >= 0 && c + i < cols) r.v[i] = row[c + i];
+        }
+    }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw<T> &r, float *f)
+{
+    if constexpr (sizeof(T) == 1) {
+        int w[2];
+        __builtin_memcpy(w, &r, 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f[4 * i + 0] = __builtin_amdgcn_cvt_f32_fp8(w[i], 0);
+            f[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(w[i], 1);
+            f[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(w[i], 2);
+            f[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(w[i], 3);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) f[i] = widen(r.v[i]);
+    }
+}
+
+// The scales of an 8-bit matrix: that of row r's block b at b * ld + r.
+struct Scales {
+    const float *p;
+    int64_t ld;
+};
+
+// Columns c .. c + 7 of a row of an 8-bit matrix lie in one block, or in two.
+struct TwoScales {
+    float first, second;
+    int border; // values from this one on have the second
+};
+
+__device__ __forceinline__ TwoScales scales_at(const Scales &s, int64_t row, int64_t c, int64_t cols)
+{
+    TwoScales t{0.f, 0.f, kEach};
+    const int64_t lo = c > 0 ? c : 0, hi = c + kEach - 1 < cols - 1 ? c + kEach - 1 : cols - 1;
+    if (lo > hi) return t;
+    const int64_t b = lo / kBlock;
+    t.first = s.p[b * s.ld + row];
+    t.second = t.first;
+    if (hi / kBlock != b) {
+        t.second = s.p[(b + 1) * s.ld + row];
+        t.border = (int)((b + 1) * kBlock - c);
+    }
+    return t;
+}
+
+__device__ __forceinline__ void scale8(float *f, const TwoScales &t)
+{
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] *= i < t.border ? t.first : t.second;
+}
+
+__device__ __forceinline__ int most8(const float *f)
+{
+    int m = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) m = max(m, magnitude(f[i]));
+    return m;
+}
+
+// Eight values as e4m3 under the scale of a block whose largest magnitude has the
+// bits `most`; `left`: how many of them there are (the others are zeros).
+__device__ __forceinline__ int2 eight_bits(const float *f, int most, int64_t left)
+{
+    const float by = kMostFp8 / fmaxf(__int_as_float(most), kMostFp8 * kLeastScale);
+    int2 v;
+    v.x = pack_fp8(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
+    v.y = pack_fp8(f[4] * by, f[5] * by, f[6] * by, f[7] * by);
+    if (most >= 0x7F800000) { // an infinity or a NaN: only NaNs
+        const uint64_t all = 0x7F7F7F7F7F7F7F7Full, some = left >= 8 ? all : left <= 0 ? 0 : all >> 8 * (8 - left);
+        v.x = (int)some;
+        v.y = (int)(some >> 32);
+    }
+    return v;
+}
+
+__device__ __forceinline__ uint32_t pack16(_Float16 a, _Float16 b)
+{
+    uint16_t x, y;
+    __builtin_memcpy(&x, &a, 2);
+    __builtin_memcpy(&y, &b, 2);
+    return x | (uint32_t)y << 16;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    uint32_t w;
+    __builtin_memcpy(&w, &v, 4);
+    return w;
+}
+
+// Eight fp32 values to columns c .. c + 7 of a row in a floating-point type (a
+// code of eb.h), each rounded once to nearest even; those past cols are left out.
+__device__ __forceinline__ void store8(void *row, int type, int64_t c, int64_t cols, const float *f)
+{
+    if (type == EB_F32) {
+        float *to = (float *)row + c;
+        if (c + kEach <= cols) {
+            const i32x4_any lo = {__float_as_int(f[0]), __float_as_int(f[1]), __float_as_int(f[2]), __float_as_int(f[3])};
+            const i32x4_any hi = {__float_as_int(f[4]), __float_as_int(f[5]), __float_as_int(f[6]), __float_as_int(f[7])};
+            *(i32x4_any *)to = lo;
+            *(i32x4_any *)(to + 4) = hi;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (c + i < cols) to[i] = f[i];
+        }
+        return;
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = type == EB_F16 ? pack16((_Float16)f[2 * i], (_Float16)f[2 * i + 1]) : pack_bf16(f[2 * i], f[2 * i + 1]);
+    uint16_t *to = (uint16_t *)row + c;
+    if (c + kEach <= cols) {
+        const i32x4_any v = {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+        *(i32x4_any *)to = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (c + i < cols) to[i] = (uint16_t)(w[i / 2] >> 16 * (i % 2));
+    }
+}
+
+// A matrix that a kernel writes: floating point, or 8 bits with scales.
+struct Out {
+    void *p;
+    float *scales;
+    int64_t ld, lds;
+    int32_t type;
+};
+
+// Columns c .. c + 7 of a row; in 8 bits the 16 lanes of a block call together
+// (`most`: bits of the block's largest magnitude), the row padded to 16 bytes.
+__device__ __forceinline__ void store_out(const Out &o, int64_t row, int64_t c, int64_t cols, const float *f, int most)
+{
+    if (c >= ((cols + 15) & ~(int64_t)15)) return;
+    if (o.type == EB_FP8) {
+        *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits(f, most, cols - c);
+        if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = block_scale(most);
+    } else if (c < cols) {
+        store8((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
+    }
+}
+
+// Host side: checks shared by the entry points.
+
+inline int element_bytes(int32_t type) { return type == EB_F32 ? 4 : type == EB_FP8 ? 1 : 2; }
+inline bool floating(int32_t type) { return type == EB_F32 || type == EB_F16 || type == EB_BF16; }
+
+// A matrix of rows x cols in `type`, its rows ld elements apart; an 8-bit one with
+// its scales.
+inline int check_matrix(const char *who, const char *what, const void *p, int32_t type, int64_t rows, int64_t cols,
+                        int64_t ld, const float *scales, int64_t lds)
+{
+    const int es = element_bytes(type);
+    if (rows == 0) return EB_OK;
+    if (!p) return fail(EB_ERR_INVALID, "%s: %s is NULL", who, what);
+    if (ld < cols) return fail(EB_ERR_INVALID, "%s: rows of %s overlap", who, what);
+    if ((uintptr_t)p % es != 0) return fail(EB_ERR_INVALID, "%s: %s is not aligned to its elements", who, what);
+    if (ld > kMax64 / 4 / rows) return fail(EB_ERR_UNSUPPORTED, "%s: %s exceeds 2^63 bytes", who, what);
+    if (type != EB_FP8) return EB_OK;
+    if ((uintptr_t)p % 16 != 0 || ld % 16 != 0)
+        return fail(EB_ERR_INVALID, "%s: %s in 8 bits must be a multiple of 16 bytes, in its address and between rows", who, what);
+    if (!scales || lds < rows) return fail(EB_ERR_INVALID, "%s: %s in 8 bits needs its scales, as many apart as it has rows", who, what);
+    if (lds > kMax64 / 4 / ((cols + kBlock - 1) / kBlock)) return fail(EB_ERR_UNSUPPORTED, "%s: the scales of %s exceed 2^63 bytes", who, what);
+    return EB_OK;
+}
+
+inline int launch(const char *who, void *kernel, int64_t grid, int threads, void *args, void *stream)
+{
+    // A launch's threads are counted in 32 bits.
+    if (grid > std::numeric_limits<uint32_t>::max() / threads) return fail(EB_ERR_UNSUPPORTED, "%s: more work than one launch holds", who);
+    void *list[] = {args};
+    const hipError_t err = hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), list, 0, (hipStream_t)stream);
+    return err == hipSuccess ? EB_OK : fail(EB_ERR_HIP, "%s: kernel launch failed: %s", who, hipGetErrorString(err));
+}
+
+} // namespace eb_train

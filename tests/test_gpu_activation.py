@@ -1,0 +1,149 @@
+"""GPU parity of eb_activation and eb_activation_backward with their formulas in 64 bits.
+
+v in 8 bits is value times scale, one rounding (u = 2^-24) in each of g and u; p =
+1 / (1 + exp(-g)) is within (5 + |g|) 2^-23 of itself, that rounding of g's included,
+or 2^-119.  h: 2^-23 (8 + 2 |g|) |h|.  dg = dh u p T with T = 1 + g (1 - p): 1 - p errs by
+p's error and a rounding, so T by |g| ((5 + |g|) 2^-23 p + 2^-23) and 2 u of its parts.
+"""
+import pytest
+import torch
+
+from paper_2512_05831_amd import eb, experts as ex, train
+from train_util import FP8, U, WIDE, as_type, check, check8, generator
+
+pytestmark = pytest.mark.gpu
+GATE, RELU = ex.EB_ACT_SILU_GATE, ex.EB_ACT_RELU
+TINY = 2.0 ** -116
+SIZES = [(1, 1), (1, 128), (3, 5), (2, 64), (17, 127), (16, 128), (33, 130), (5, 200), (40, 256), (9, 1000), (64, 1024), (7, 1512)]
+
+
+def forward(v, act):
+    if act == RELU:
+        return v.clamp(min=0), U * v.abs()
+    g, u = v.chunk(2, 1)
+    h = g * torch.sigmoid(g) * u
+    return h, 2 * U * (8 + 2 * g.abs()) * h.abs() + TINY * (1 + g.abs()) * u.abs()
+
+
+def backward(dh, v, act):
+    if act == RELU:
+        return torch.where(v > 0, dh, 0.0), torch.zeros_like(v)
+    g, u = v.chunk(2, 1)
+    p, q = torch.sigmoid(g), torch.sigmoid(-g)
+    T, ep = 1 + g * q, (5 + g.abs()) * 2 * U
+    eT = g.abs() * (ep * p + 2 * U) + 2 * U * (1 + (g * q).abs())
+    dg, du = dh * u * p * T, dh * g * p
+    edg = (dh * u).abs() * p * (T.abs() * (ep + 8 * U) + eT) + TINY * (dh * u).abs() * (1 + g.abs())
+    return torch.cat([dg, du], 1), torch.cat([edg, (ep + 6 * U) * du.abs() + TINY * (dh * g).abs()], 1)
+
+
+def inputs(rows, cols, act, dtype, device, seed=0):
+    g = generator(device, rows + cols + seed)
+    width = cols * (2 if act == GATE else 1)
+    v = 3 * torch.randn(rows, width, generator=g, device=device) * torch.rand(rows, 1, generator=g, device=device).mul_(2).exp2_()
+    return (*as_type(v, dtype), torch.randn(rows, cols, generator=g, device=device) * 0.1)
+
+
+def check_both(v, s, values, dh, act, out):
+    h, dv = train.activation(v, s, act=act, out_dtype=out), train.activation_backward(dh, v, s, act=act, out_dtype=out)
+    want_h, want_dv = forward(values, act), backward(dh.double(), values, act)
+    if out == FP8:
+        check8(*h, *want_h)
+        check8(*dv, *want_dv)
+    else:
+        check(h, *want_h, out)
+        check(dv, *want_dv, out)
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("act", [GATE, RELU])
+@pytest.mark.parametrize("v_type", [FP8] + WIDE)
+def test_matrix(rows, cols, act, v_type, device):
+    v, s, values, dh = inputs(rows, cols, act, v_type, device)
+    for dh_type, out in ((torch.bfloat16, FP8), (torch.float32, torch.float32), (torch.float16, torch.bfloat16), (torch.float32, torch.float16),
+                         (torch.float16, FP8)):
+        check_both(v, s, values, dh.to(dh_type), act, out)
+
+
+@pytest.mark.parametrize("v_type", [FP8, torch.bfloat16])
+def test_strided(v_type, device):
+    """Views of wider matrices, scales of more rows than are taken."""
+    v, s, values, dh = inputs(60, 333, GATE, v_type, device)
+    dh = dh.to(torch.float16)
+    for rows in (slice(4, 41), slice(0, 60, 3), slice(59, 60)):
+        check_both(v[rows], None if s is None else s[rows], values[rows], dh[rows], GATE, FP8)
+    if v_type != FP8:
+        check_both(v[:, 5:405], None, values[:, 5:405], dh[:, 1:201], GATE, torch.float32)
+    # scales row after row
+    if s is not None:
+        check_both(v, s.contiguous(), values, dh, GATE, torch.bfloat16)
+
+
+def test_extremes(device):
+    """Large and small g, where p is 0, 1 and between; zeros; NaN and infinity."""
+    g = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 20.0, -20.0, 80.0, -80.0, 87.0, -87.0, 90.0, -90.0, 200.0, -200.0, 1e4, -1e4, -1.2784645, 5.0], device=device)
+    v = torch.cat([g, torch.linspace(-2, 2, g.numel(), device=device)])[None].contiguous()
+    dh = torch.ones(1, g.numel(), device=device)
+    check_both(v, None, v.double(), dh, GATE, torch.float32)
+    v[0, 0], v[0, g.numel() + 4] = float("nan"), float("inf")
+    h = train.activation(v, out_dtype=torch.float32)
+    dv = train.activation_backward(dh, v, out_dtype=torch.float32)
+    assert h[0, 0].isnan() and h[0, 4] == float("inf") and not h[0, 5:].isnan().any()
+    assert dv[0, 0].isnan() and dv[0, g.numel()].isnan() and not dv[0, 5:18].isnan().any()
+    q, s = train.activation(v, out_dtype=FP8)
+    assert q.float().isnan().all() and s.isnan().all()  # one block
+    r = torch.tensor([[float("nan"), float("inf"), -float("inf"), 0.0, -0.0, 2.0, -2.0]], device=device)
+    h = train.activation(r, act=RELU, out_dtype=torch.float32)
+    assert h[0, 0].isnan() and h[0, 1:].tolist() == [float("inf"), 0, 0, 0, 2, 0]
+    d = train.activation_backward(torch.full((1, 7), 3.0, device=device), r, act=RELU, out_dtype=torch.float32)
+    assert d[0].tolist() == [0, 3, 0, 0, 0, 3, 0]
+    nan = train.activation_backward(torch.full((1, 7), float("nan"), device=device), r, act=RELU, out_dtype=torch.float32)
+    assert nan.isnan().tolist() == [[False, True, False, False, False, True, False]]
+
+
+def test_backward_is_the_slope(device):
+    """Against differences of the definition, in 64 bits."""
+    v = torch.randn(4, 300, generator=generator(device, 1), device=device)
+    dh = torch.randn(4, 150, generator=generator(device, 2), device=device)
+    d = torch.randn(4, 300, generator=generator(device, 3), device=device).double()
+    f = lambda v: (v[:, :150] * torch.sigmoid(v[:, :150]) * v[:, 150:] * dh.double()).sum()  # noqa: E731
+    dv = train.activation_backward(dh, v, out_dtype=torch.float32).double()
+    t = 1e-5
+    slope = (f(v.double() + t * d) - f(v.double() - t * d)) / (2 * t)
+    assert abs(slope - (dv * d).sum()) <= 64 * U * (dv * d).abs().sum() + 1e-8 * (dv * d).abs().sum()
+
+
+def test_after_the_product(device):
+    """As the layer has it: the product's 8 bits, then the activation; near the product with the activation in it."""
+    g = generator(device, 4)
+    x, w = torch.randn(50, 256, generator=g, device=device), torch.randn(512, 256, generator=g, device=device) / 16
+    q, s = ex.quantize_fp8(x)
+    wq, ws = ex.quantize_fp8(w.view(2, 256, 256), block_rows=128)
+    v, vs = ex.product(q, s, wq.reshape(512, 256), ws.reshape(4, 2), out_dtype=FP8)
+    h = train.activation(v, vs, out_dtype=torch.float32).double()
+    want = ex.product(q, s, wq.reshape(512, 256), ws.reshape(4, 2), act=GATE, out_dtype=torch.float32).double()
+    full = ex.product(q, s, wq.reshape(512, 256), ws.reshape(4, 2), out_dtype=torch.float32).double()
+    step = full.abs() * 2.0 ** -4 + vs.double().repeat_interleave(128, 1) * 2.0 ** -9
+    gg, uu = full.chunk(2, 1)
+    eg, eu = step.chunk(2, 1)
+    # |d(silu)/dg| <= 1.1
+    assert ((h - want).abs() <= 1.1 * eg * (uu.abs() + eu) + torch.nn.functional.silu(gg).abs() * eu + 1e-5 * (1 + want.abs())).all()
+
+
+def test_no_rows_and_refusals(device):
+    v = torch.zeros(4, 64, device=device)
+    q, s = ex.quantize_fp8(v)
+    assert train.activation(v[:0]).shape == (0, 32)
+    assert train.activation_backward(v[:0, :32], v[:0], out_dtype=FP8)[0].shape == (0, 64)
+    dh = torch.zeros(4, 32, device=device)
+    for bad in (lambda: train.activation(v[:, :63]), lambda: train.activation(q), lambda: train.activation(q, s[:3]), lambda: train.activation(v, s),
+                lambda: train.activation(v.cpu()), lambda: train.activation(v.double()), lambda: train.activation(v.t()),
+                lambda: train.activation(q, s.cpu()), lambda: train.activation(v, out_dtype=torch.int8),
+                lambda: train.activation_backward(dh[:, :31], v), lambda: train.activation_backward(dh[:3], v), lambda: train.activation_backward(q, v),
+                lambda: train.activation_backward(dh, v.cpu())):
+        with pytest.raises(ValueError):
+            bad()
+    for act in (ex.EB_ACT_NONE, 3, GATE | ex.EB_EXACT_SUMS):
+        with pytest.raises(eb.EbError) as e:
+            train.activation(v, act=act)
+        assert e.value.code == eb.EB_ERR_INVALID
