@@ -247,7 +247,8 @@ def _own(s):
     if op == "combine":
         return train.combine(s["y"], s["slots"], s["weights"], out_dtype=DTYPES[c["out"]])
     if op == "combine_back":
-        return train.combine_backward(s["dout"], s["y"], s["slots"], s["weights"], out_dtype=DTYPES[c["out"]])
+        r = train.combine_backward(s["dout"], s["y"], s["slots"], s["weights"], out_dtype=DTYPES[c["out"]])
+        return {k: v for k, v in r._asdict().items() if v is not None}
     return train.weight_gradient(s["dy"], s["x"], offsets=s["offsets"], tokens=s["tokens"], dy_scales=s["dy_scales"], x_scales=s["x_scales"],
                                  out_dtype=DTYPES[c["out"]])
 
