@@ -3,18 +3,25 @@
 //   dw[n, k] = sum over its slots m of dy[m, n] x[token of m, k]
 //
 // with the 16-bit matrix unit.  Both operands lie with the slots one below the other,
-// while the unit wants eight slots of one column in a lane: a thread reads four
-// columns of eight slots, turns them, and puts each column's eight 16-bit values into
-// LDS as one piece of 16 bytes.
-//   8-bit operands are widened on the way.  A slot's scales (of dy and of x, both one
-// number for a tile of 128 x 128, whose edges are those of the scales' blocks) go into
-// one operand as their product S, so that the other one, e4m3 or 16 bits, enters
-// exactly.  The scaled one has up to 28 bits and takes several 16-bit parts where sums
-// have to be exact, each multiplied with the other operand:
-//   beside e4m3 or fp16, two parts in fp16, 22 bits.  Their range is short, so S is
-//     divided by a power of two, kept above the largest S so far; where that grows
-//     the sums are brought to the new one (exactly), and the outputs multiplied by the last;
-//   beside bfloat16, three parts in that, 24 bits.
+// while the unit wants eight slots of one column in a lane.  They are copied as they lie
+// from global memory straight into LDS, the next step's while this one is multiplied,
+// and read from there by the instructions that turn 8 (of 16 bits: 4) rows of 16
+// columns on the way.  8-bit values become 16-bit ones in the wave that read them.
+//   A workgroup has 256 columns of one operand (the "own" one: a wave has 64 of them
+// to itself) by 128 of the other (the "shared" one, which all four waves read), so what
+// is costly to make of a value is made once if the own operand has it.
+//   A slot's scales (of dy and of x) go into the own operand as their product S, one
+// number for a slot and 128 own columns; so that the shared one, e4m3 or 16 bits,
+// enters exactly, and where dy and x both have scales a workgroup's shared columns are
+// one block of them.  Scaled values have up to 28 bits and take several 16-bit parts
+// where sums have to be exact, each multiplied with the shared operand:
+//   beside e4m3 or fp16, two parts in fp16 (22 bits).  Their range is short, so S is
+//     divided by a power of two, kept above the largest S so far; where that grows the
+//     sums are brought to the new one (exactly), and the outputs multiplied by the last;
+//   beside bfloat16, three parts in that (24 bits).
+//   In LDS the 16-byte pieces of a row are permuted with its number (what a lane copies
+// goes where its number says, so it is the global addresses that are permuted): the
+// rows that an instruction reads at a time then lie in different banks.
 #pragma once
 
 #include <type_traits>
@@ -26,160 +33,275 @@ namespace eb_gradient {
 using namespace eb_train;
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;  // columns of either operand
-constexpr int kSlots = 64;  // of a step
-constexpr int kChunks = kSlots / 8;
-constexpr int kQuad = 4;    // columns of a thread
-constexpr int kQuads = kTile / kQuad;
+constexpr int kOwnTile = 256, kSharedTile = 128; // columns of a workgroup
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 struct GradientArgs {
-    const char *dy, *x;
-    Scales dy_scales, x_scales;
+    const char *own, *shared;
+    Scales own_scales, shared_scales;
     const int32_t *tokens, *offsets;
     void *dw;
-    float *partial; // [splits][E][N, K], or NULL
-    int64_t lddy, ldx, x_rows, lddw; // lddy, ldx in bytes
+    float *partial;                 // [splits][E][N, K], or NULL
+    int64_t own_ld, shared_ld;      // in bytes
+    int64_t x_rows, lddw;
+    int32_t own_cols, shared_cols;
     int32_t M, E, N, K;
-    int32_t n_tiles, k_tiles, splits;
+    int32_t own_tiles, shared_tiles, splits;
     int32_t out_type;
     bool accumulate;
 };
 
-struct alignas(16) Piece { // eight slots of a column
+struct alignas(16) Piece { // eight slots of a column, 16 bits each
     uint32_t w[4];
 };
-
-// How an operand of type T enters the matrix unit, in fp16 (kHalf) or bfloat16.
-template <typename T, bool kScaled_, bool kHalf_, bool kExact>
-struct Operand {
-    using Type = T;
-    static constexpr bool kScaled = kScaled_, kHalf = kHalf_;
-    static constexpr bool kBits = !kScaled && std::is_same_v<T, std::conditional_t<kHalf, _Float16, Bf16>>; // as in memory
-    static constexpr bool kSure = kBits || (std::is_same_v<T, Fp8> && !kScaled); // one 16-bit value holds it
-    static constexpr int kParts = !kExact || kSure ? 1 : kHalf || !kScaled ? 2 : 3;
-    static constexpr int kWords = sizeof(T); // 32-bit words of four values
+struct alignas(8) Bytes { // 8 bits each
+    uint32_t w[2];
 };
 
-// Four neighbouring columns of a slot.
-template <typename T>
-__device__ __forceinline__ void load_quad(const char *row, int c, int cols, uint32_t *w)
-{
-    constexpr int n = sizeof(T);
-    typedef int i32_any __attribute__((aligned(1)));
-    if (c + kQuad <= cols) {
-        if constexpr (n == 1) {
-            w[0] = *(const i32_any *)(row + c);
+// Which operand is the own one, and how it enters the unit.
+template <typename D, typename X, bool kExact>
+struct Shape {
+    static constexpr bool kHalf = !std::is_same_v<D, Bf16> && !std::is_same_v<X, Bf16>; // the unit takes fp16, else bfloat16
+    using Unit = std::conditional_t<kHalf, _Float16, Bf16>;
+    // dy, but where x has scales and dy has none, or x alone is of another type than the unit's.
+    static constexpr bool kOwnX = !std::is_same_v<D, Fp8> && !std::is_same_v<X, Unit>;
+    using Own = std::conditional_t<kOwnX, X, D>;
+    using Shared = std::conditional_t<kOwnX, D, X>;
+    static constexpr bool kScaled = std::is_same_v<Own, Fp8>;
+    static constexpr bool kBoth = kScaled && std::is_same_v<Shared, Fp8>;
+    static constexpr bool kShift = kScaled && kHalf;
+    static constexpr bool kAsItIs = std::is_same_v<Own, Unit>;
+    static constexpr int kParts = !kExact || kAsItIs ? 1 : kHalf || !kScaled ? 2 : 3;
+    using OwnPiece = std::conditional_t<kScaled, Bytes, Piece>;
+    static constexpr int kSlots = kScaled ? 64 : 32; // of a step
+};
+
+constexpr int kQuad = 4;                    // neighbouring outputs of a lane
+constexpr int kHalves = kOwnTile / kBlock;  // blocks of scales of the own operand
+constexpr int kInfos = 3;                   // steps whose slots are known at a time
+
+// One step of an operand in LDS, and how it gets there and out of there.
+template <typename T, int kColumns, int kSlots>
+struct Panel {
+    static constexpr uint32_t kRow = kColumns * sizeof(T), kPieces = kRow / 16; // of a slot
+    static constexpr uint32_t kRows = kThreads / kPieces;                       // of a copy by all threads
+    static constexpr int kCopies = kSlots / kRows;
+    static_assert(kSlots % kRows == 0, "whole copies");
+    alignas(16) char bytes[kSlots * kRow];
+
+    // The piece of a row that lies in place `at` of it.
+    static __device__ __forceinline__ uint32_t piece_of(uint32_t row, uint32_t at)
+    {
+        if constexpr (sizeof(T) == 1) return at ^ (kPieces == 16 ? row % 16 : row / 2 % 8);
+        else return at ^ 2 * (row % 4 | row / 8 % 2 * 4);
+    }
+
+    // Where a lane reads from for column tile 0; for tile i that ^ i * kTile.
+    static constexpr uint32_t kTile = 16 * sizeof(T);
+    static __device__ __forceinline__ uint32_t first_of(uint32_t lane)
+    {
+        const uint32_t g = lane / 16, in = lane % 16;
+        if constexpr (sizeof(T) == 1) {
+            const uint32_t row = 8 * g + in / 2;
+            return row * kRow + (kPieces == 16 ? row % 16 : row / 2 % 8) * 16 + in % 2 * 8;
         } else {
-            const i32x2_any v = *(const i32x2_any *)(row + (int64_t)c * n);
-            w[0] = v.x;
-            w[1] = v.y;
-        }
-    } else {
-        T v[kQuad] = {};
-#pragma unroll
-        for (int i = 0; i < kQuad; ++i)
-            if (c + i < cols) v[i] = ((const T *)row)[c + i];
-        __builtin_memcpy(w, v, sizeof(v));
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ void widen_quad(const uint32_t *w, float *f)
-{
-    if constexpr (std::is_same_v<T, Fp8>) {
-        f[0] = __builtin_amdgcn_cvt_f32_fp8(w[0], 0);
-        f[1] = __builtin_amdgcn_cvt_f32_fp8(w[0], 1);
-        f[2] = __builtin_amdgcn_cvt_f32_fp8(w[0], 2);
-        f[3] = __builtin_amdgcn_cvt_f32_fp8(w[0], 3);
-    } else {
-        T v[kQuad];
-        __builtin_memcpy(v, w, sizeof(v));
-#pragma unroll
-        for (int i = 0; i < kQuad; ++i) f[i] = widen(v[i]);
-    }
-}
-
-// Two values in 16 bits, and what that leaves of them.
-template <bool kHalf>
-__device__ __forceinline__ uint32_t pack_part(float &a, float &b)
-{
-    if constexpr (kHalf) {
-        const _Float16 x = (_Float16)a, y = (_Float16)b;
-        a -= (float)x;
-        b -= (float)y;
-        return pack16(x, y);
-    } else {
-        const uint32_t w = pack_bf16(a, b);
-        a -= __uint_as_float(w << 16);
-        b -= __uint_as_float(w & 0xFFFF0000u);
-        return w;
-    }
-}
-
-// The eight slots' four columns, turned: `to` is the first column's piece, the
-// others kQuads pieces apart, the next parts kChunks * kTile.
-template <typename O>
-__device__ __forceinline__ void turn(const uint32_t (*raw)[O::kWords], const float *scale, Piece *to)
-{
-    Piece part[O::kParts][kQuad];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { // slots 2 i and 2 i + 1
-        const uint32_t *a = raw[2 * i], *b = raw[2 * i + 1];
-        if constexpr (O::kBits) {
-#pragma unroll
-            for (int j = 0; j < kQuad; ++j) part[0][j].w[i] = __builtin_amdgcn_perm(b[j / 2], a[j / 2], j % 2 ? 0x07060302 : 0x05040100);
-        } else {
-            float f[kQuad], g[kQuad];
-            widen_quad<typename O::Type>(a, f);
-            widen_quad<typename O::Type>(b, g);
-#pragma unroll
-            for (int j = 0; j < kQuad; ++j) {
-                if constexpr (O::kScaled) {
-                    f[j] *= scale[2 * i];
-                    g[j] *= scale[2 * i + 1];
-                }
-#pragma unroll
-                for (int p = 0; p < O::kParts; ++p) part[p][j].w[i] = pack_part<O::kHalf>(f[j], g[j]);
-            }
+            return (8 * g + in / 4) * kRow + (in / 4 | g % 2 * 4) * 32 + in % 4 * 8;
         }
     }
+
+    // Columns 16 tile .. + 15 of slots 8 g .. 8 g + 7, g = step / 8 + lane / 16: column lane % 16.
+    __device__ __forceinline__ std::conditional_t<sizeof(T) == 1, Bytes, Piece> read(int step, uint32_t first, uint32_t tile) const
+    {
+        typedef __attribute__((address_space(3))) char Lds;
+        const auto from = (const Lds *)bytes + ((first ^ tile * kTile) + step * kRow);
+        if constexpr (sizeof(T) == 1) {
+            typedef int i32x2 __attribute__((ext_vector_type(2)));
+            return __builtin_bit_cast(Bytes, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)from));
+        } else {
+            typedef short i16x4 __attribute__((ext_vector_type(4)));
+            const i16x4 v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from),
+                                __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(from + 4 * kRow))};
+            return __builtin_bit_cast(Piece, v);
+        }
+    }
+};
+
+__device__ const i32x4 kZeros = {0, 0, 0, 0};
+
+// 16 bytes of a row that may have any alignment; zeros past `left` bytes.
+__device__ __forceinline__ i32x4 load_any(const char *at, int64_t left)
+{
+    if (left >= 16) return *(const i32x4_any *)at;
+    uint32_t w[4] = {};
 #pragma unroll
-    for (int p = 0; p < O::kParts; ++p)
+    for (int i = 0; i < 8; ++i)
+        if (2 * i < left) w[i / 2] |= (uint32_t)((const uint16_t *)at)[i] << i % 2 * 16;
+    return i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+
+__device__ __forceinline__ Piece widened(const Bytes &b)
+{
+    Piece p;
 #pragma unroll
-        for (int j = 0; j < kQuad; ++j) to[p * kChunks * kTile + j * kQuads] = part[p][j];
+    for (int i = 0; i < 4; ++i)
+        p.w[i] = __builtin_bit_cast(uint32_t, i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.w[i / 2], 1.f, true)
+                                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.w[i / 2], 1.f, false));
+    return p;
 }
 
 template <bool kHalf>
 __device__ __forceinline__ f32x4 multiply(const Piece &a, const Piece &b, f32x4 c)
 {
-    if constexpr (kHalf) {
-        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    if constexpr (kHalf)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    } else {
+    else
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Scales of the eight slots of a lane, as the own operand's parts are made with them.
+template <bool kHalf>
+struct EightScales;
+template <>
+struct EightScales<true> {
+    f16x2 first[4], rest[4]; // S rounded to fp16, and what that leaves
+};
+template <>
+struct EightScales<false> {
+    float s[8];
+};
+
+// The own operand's parts, made of a piece in LDS and taken one after the other.
+template <typename S, typename Take>
+__device__ __forceinline__ void each_part(const typename S::OwnPiece &piece, const EightScales<S::kHalf> &scale, Take &&take)
+{
+    if constexpr (S::kAsItIs) {
+        take(piece);
+    } else if constexpr (S::kShift) {
+        Piece first, rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f16x2 q = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], 1.f, true)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], 1.f, false);
+            const f16x2 v = q * scale.first[i];
+            first.w[i] = __builtin_bit_cast(uint32_t, v);
+            if constexpr (S::kParts == 2) { // what v's rounding left of q * first (exactly), and q * rest, rounded once
+                const f16x2 left = __builtin_elementwise_fma(q, scale.first[i], -v);
+                rest.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, scale.rest[i], left));
+            }
+        }
+        take(first);
+        if constexpr (S::kParts == 2) take(rest);
+    } else {
+        float f[kEach];
+        if constexpr (S::kScaled) {
+            Raw<Fp8> raw;
+            __builtin_memcpy(&raw, &piece, 8);
+            widen8(raw, f);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) f[i] *= scale.s[i];
+        } else {
+            Raw<_Float16> raw;
+            __builtin_memcpy(&raw, &piece, 16);
+            widen8(raw, f);
+        }
+#pragma unroll
+        for (int p = 0; p < S::kParts; ++p) {
+            Piece part;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = pack_bf16(f[2 * i], f[2 * i + 1]);
+                part.w[i] = w;
+                f[2 * i] -= __uint_as_float(w << 16);
+                f[2 * i + 1] -= __uint_as_float(w & 0xFFFF0000u);
+            }
+            take(part);
+        }
     }
 }
 
-// D, X: types of dy and x.  Four waves of 64 x 64 outputs; x's columns are the rows
-// of the matrix unit's result, so a lane has four neighbouring outputs.
-template <typename D, typename X, bool kExact>
+// Workgroups are dealt to the 8 XCDs in turn.  Each takes runs of tiles that have the
+// same own columns, and so share them in its L2, the runs in turn: every expert's tiles
+// spread over the XCDs, whatever its slots.
+__device__ __forceinline__ uint32_t tile_in_order(uint32_t index, uint32_t count, uint32_t run)
+{
+    constexpr uint32_t kXcds = 8;
+    const uint32_t whole = count / kXcds / run * (kXcds * run);
+    if (index >= whole) return index;
+    const uint32_t xcd = index % kXcds, nth = index / kXcds;
+    return (nth / run * kXcds + xcd) * run + nth % run;
+}
+
+template <typename T>
+__device__ __forceinline__ void write_out(T *to, bool accumulate, float v)
+{
+    *to = (T)(accumulate ? (float)*to + v : v);
+}
+
+// Four neighbouring outputs of row n from column k on, `left` of them there.
+__device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial, int e, int n, int k, const float *v)
+{
+    const int left = a.K - k;
+    if (partial) {
+        float *to = partial + (int64_t)n * a.K + k;
+        if (left >= kQuad) {
+            const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+            *(i32x4_any *)to = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kQuad; ++j)
+                if (j < left) to[j] = v[j];
+        }
+        return;
+    }
+    const int64_t place = ((int64_t)e * a.N + n) * a.lddw + k;
+    if (left >= kQuad && !a.accumulate) {
+        if (a.out_type == EB_F32) {
+            const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+            *(i32x4_any *)((float *)a.dw + place) = w;
+        } else {
+            const bool half = a.out_type == EB_F16;
+            const i32x2_any w = {(int)(half ? pack16((_Float16)v[0], (_Float16)v[1]) : pack_bf16(v[0], v[1])),
+                                 (int)(half ? pack16((_Float16)v[2], (_Float16)v[3]) : pack_bf16(v[2], v[3]))};
+            *(i32x2_any *)((uint16_t *)a.dw + place) = w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kQuad; ++j) {
+        if (j >= left) break;
+        if (a.out_type == EB_F32) write_out((float *)a.dw + place + j, a.accumulate, v[j]);
+        else if (a.out_type == EB_F16) write_out((_Float16 *)a.dw + place + j, a.accumulate, v[j]);
+        else write_out((__bf16 *)a.dw + place + j, a.accumulate, v[j]);
+    }
+}
+
+// kDirect: 16-bit operands lie so that 16 bytes can be copied to LDS at a time (8-bit
+// ones always do); else they go through registers.
+template <typename D, typename X, bool kExact, bool kDirect>
 __global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
 {
-    constexpr bool kFp8D = std::is_same_v<D, Fp8>, kFp8X = std::is_same_v<X, Fp8>, kScaled = kFp8D || kFp8X;
-    constexpr bool kHalf = !std::is_same_v<D, Bf16> && !std::is_same_v<X, Bf16>;
-    constexpr bool kShift = kHalf && kScaled; // scales are divided by a power of two
-    using OD = Operand<D, kFp8D && !kFp8X, kHalf, kExact>;
-    using OX = Operand<X, kFp8X, kHalf, kExact>;
-    __shared__ Piece of_dy[OD::kParts][kChunks][kTile], of_x[OX::kParts][kChunks][kTile];
-    __shared__ int32_t row_of[2][kSlots]; // of x; -1: the slot adds nothing
-    __shared__ float scale_of[2][kSlots];
-    __shared__ int most_of[2]; // the exponent of the largest scale of a step
+    using S = Shape<D, X, kExact>;
+    using Own = typename S::Own;
+    using Shared = typename S::Shared;
+    constexpr int kSlots = S::kSlots;
+    using OwnPanel = Panel<Own, kOwnTile, kSlots>;
+    using SharedPanel = Panel<Shared, kSharedTile, kSlots>;
+    constexpr bool kOwnDirect = kDirect || sizeof(Own) == 1, kSharedDirect = kDirect || sizeof(Shared) == 1;
+    constexpr int kSharedTiles = kSharedTile / 16, kOwnTiles = kOwnTile / 64; // 16 x 16 tiles of a wave
+    // What is copied to while another step is read is a variable of its own: the
+    // compiler then sees that those reads need not wait for the copies.
+    __shared__ OwnPanel own_even, own_odd;
+    __shared__ SharedPanel shared_even, shared_odd;
+    __shared__ int64_t offset_of[kInfos][kSlots]; // of a slot's row of x; -1: the slot adds nothing
+    __shared__ std::conditional_t<S::kHalf, _Float16, float> first_of[kInfos][kHalves][kSlots], rest_of[kInfos][kHalves][kSlots];
+    __shared__ int shift_of[kInfos][kHalves];
 
-    uint32_t at = blockIdx.x;
-    const int k_tile = at % a.k_tiles;
-    at /= a.k_tiles;
-    const int n_tile = at % a.n_tiles;
-    at /= a.n_tiles;
+    uint32_t at = tile_in_order(blockIdx.x, gridDim.x, a.shared_tiles);
+    const int shared_tile = at % a.shared_tiles;
+    at /= a.shared_tiles;
+    const int own_tile = at % a.own_tiles;
+    at /= a.own_tiles;
     const int split = at % a.splits, e = at / a.splits;
     int begin = 0, end = a.M;
     if (a.offsets) {
@@ -188,161 +310,190 @@ __global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
     }
     const int64_t each = (((int64_t)end - begin + a.splits - 1) / a.splits + kSlots - 1) / kSlots * kSlots;
     begin = (int)min(begin + split * each, (int64_t)end);
-    end = (int)min(begin + each, (int64_t)end);
+    end = a.x_rows == 0 ? begin : (int)min(begin + each, (int64_t)end);
 
-    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
-    const int chunk = t / kQuads, quad = t % kQuads;
-    const int n0 = n_tile * kTile, k0 = k_tile * kTile;
+    const int t = threadIdx.x, lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
+    const int own0 = own_tile * kOwnTile, shared0 = shared_tile * kSharedTile;
 
-    // A slot's row of x, and its scale, a step ahead of the operands themselves.
-    auto row_at = [&](int64_t m) {
-        if (m >= end) return -1;
-        const int r = a.tokens ? a.tokens[m] : (int)m;
-        return r >= 0 && r < a.x_rows ? r : -1;
+    // A step's slots: where their rows of x are, and their scales; by the first threads
+    // (kSlots for each block of own columns), two steps ahead.
+    const bool informs = t < kHalves * kSlots;
+    const int slot = threadIdx.x % kSlots, half = threadIdx.x / kSlots;
+    // Loads whose values wait until they are needed, from places that are there (a step
+    // has slots, and x rows); what they say of slots that are not is left out then.
+    auto token_at = [&](int64_t m) { return a.tokens ? a.tokens[min(m, (int64_t)end - 1)] : (int)min(m, (int64_t)end); };
+    auto row_of = [&](int64_t m, int token) { return m < end && token >= 0 && token < a.x_rows ? token : -1; };
+    const int64_t block = min((int64_t)own_tile * kHalves + half, ((int64_t)a.own_cols - 1) / kBlock);
+    float own_scale = 0.f, shared_scale = 1.f;
+    auto load_scales = [&](int64_t m, int row) {
+        if constexpr (S::kScaled) own_scale = a.own_scales.p[block * a.own_scales.ld + (S::kOwnX ? max(row, 0) : min(m, (int64_t)end - 1))];
+        if constexpr (S::kBoth) shared_scale = a.shared_scales.p[shared_tile * a.shared_scales.ld + max(row, 0)];
     };
-    auto scale_at = [&](int64_t m, int row) {
-        float s = row < 0 ? 0.f : 1.f;
-        if (row >= 0 && kFp8D) s = a.dy_scales.p[n_tile * a.dy_scales.ld + m];
-        if (row >= 0 && kFp8X) s *= a.x_scales.p[k_tile * a.x_scales.ld + row];
-        return s;
-    };
-    // By the first wave, whose lanes have a slot each.
-    auto put = [&](int of, int row, float s) {
-        row_of[of][t] = row;
-        if constexpr (kScaled) scale_of[of][t] = s;
-        if constexpr (kShift) {
-            const int bits = magnitude(s), most = max_lanes<kWave>(bits < 0x7F800000 ? bits >> 23 : 0);
-            if (t == 0) most_of[of] = most;
-        }
-    };
-    uint32_t raw_dy[8][OD::kWords], raw_x[8][OX::kWords];
-    auto load = [&](int64_t m, const int32_t *rows) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = rows[chunk * 8 + i];
-#pragma unroll
-            for (int j = 0; j < OD::kWords; ++j) raw_dy[i][j] = 0;
-#pragma unroll
-            for (int j = 0; j < OX::kWords; ++j) raw_x[i][j] = 0;
-            if (row >= 0) {
-                load_quad<D>(a.dy + (m + chunk * 8 + i) * a.lddy, n0 + quad * kQuad, a.N, raw_dy[i]);
-                load_quad<X>(a.x + row * a.ldx, k0 + quad * kQuad, a.K, raw_x[i]);
+    int next_shift = -200; // below any scale's exponent
+    auto put = [&](int of, int row) {
+        if (half == 0) offset_of[of][slot] = row < 0 ? -1 : row * (S::kOwnX ? a.own_ld : a.shared_ld);
+        if constexpr (S::kScaled) {
+            float s = row < 0 ? 0.f : own_scale * shared_scale;
+            if constexpr (S::kShift) {
+                // 448 S / 2^shift stays below 2^15; a new shift leaves room for S to grow 4 times.
+                constexpr int kMostLeft = 5, kRoom = 2;
+                static_assert(kSlots == kWave, "a wave has a step's scales of a block");
+                const int bits = magnitude(s), most = max_lanes<kWave>(bits < 0x7F800000 ? bits >> 23 : 0) - 127;
+                if (most - next_shift > kMostLeft) next_shift = most - kMostLeft + kRoom;
+                if (slot == 0) shift_of[of][half] = next_shift;
+                s = ldexpf(s, -next_shift);
+                const _Float16 first = (_Float16)s;
+                first_of[of][half][slot] = first;
+                if constexpr (kExact) rest_of[of][half][slot] = (_Float16)(s - (float)first);
+            } else {
+                first_of[of][half][slot] = s;
             }
         }
     };
 
-    f32x4 sum[4][4] = {}; // [columns of dy][columns of x]
-    const int wk = wave % 2, wn = wave / 2;
-    constexpr int kMostLeft = 5; // 2^6 above the largest e4m3 value, 2^15 and less
-    int next_row = -1, shift = -200; // below any scale's exponent
-    if (begin < end) {
-        if (t < kSlots) {
-            const int row = row_at(begin + t);
-            put(0, row, scale_at((int64_t)begin + t, row));
-            next_row = row_at((int64_t)begin + kSlots + t);
+    // Copies of a step that begins with slot m, 16 bytes a lane.  Direct ones take 16
+    // bytes of zeros in place of what is not there.
+    const auto zeros = (const char *)&kZeros;
+    const uint32_t thread = t;
+    i32x4 own_raw[kOwnDirect ? 1 : OwnPanel::kCopies], shared_raw[kSharedDirect ? 1 : SharedPanel::kCopies];
+    // dy's rows follow each other: where the thread's first one is from a step's start on.
+    constexpr uint32_t kRowsOfDy = S::kOwnX ? SharedPanel::kRows : OwnPanel::kRows;
+    const int64_t dy_ld = S::kOwnX ? a.shared_ld : a.own_ld, of_dy = thread / (kThreads / kRowsOfDy) * dy_ld;
+    auto copy = [&](auto &panel, auto direct, auto of_x, i32x4 *raw, const char *base, uint32_t left, int64_t m, int of) {
+        using P = std::remove_reference_t<decltype(panel)>;
+        const char *dy = base + m * dy_ld;
+#pragma unroll
+        for (int p = 0; p < P::kCopies; ++p) {
+            const uint32_t row = p * P::kRows + thread / P::kPieces, byte = P::piece_of(row, thread % P::kPieces) * 16;
+            const int64_t x = offset_of[of][row];
+            const char *from = decltype(of_x)::value ? base + x : dy + p * (int64_t)P::kRows * dy_ld + of_dy;
+            from += byte;
+            if constexpr (decltype(direct)::value) {
+                from = x < 0 || byte >= left ? zeros : from;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                                 (__attribute__((address_space(3))) void *)(panel.bytes + (p * kThreads + wave * kWave) * 16), 16, 0, 0);
+            } else {
+                raw[p] = load_any(from, x < 0 ? 0 : (int64_t)left - byte);
+            }
         }
-        __syncthreads();
-        load(begin, row_of[0]);
-    }
-    int turn_of = 0;
-    for (int64_t m = begin; m < end; m += kSlots, turn_of ^= 1) {
-        float next_scale = 0.f;
-        const int row = next_row;
-        if (kScaled && t < kSlots) next_scale = scale_at(m + kSlots + t, row);
-        float scale[8];
-        if constexpr (kScaled) {
+    };
+    auto left_of = [](int cols, int first, int width, int size) { return (uint32_t)(min(cols - first, width) * size); };
+    const uint32_t own_left = left_of(a.own_cols, own0, kOwnTile, sizeof(Own)), shared_left = left_of(a.shared_cols, shared0, kSharedTile, sizeof(Shared));
+    auto copy_step = [&](auto &own, auto &shared, int64_t m, int of) {
+        copy(own, std::bool_constant<kOwnDirect>(), std::bool_constant<S::kOwnX>(), own_raw, a.own + (int64_t)own0 * sizeof(Own), own_left, m, of);
+        copy(shared, std::bool_constant<kSharedDirect>(), std::bool_constant<!S::kOwnX>(), shared_raw, a.shared + (int64_t)shared0 * sizeof(Shared),
+             shared_left, m, of);
+    };
+    auto store_step = [&](auto &own, auto &shared) { // what went through registers
+        if constexpr (!kOwnDirect) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) scale[i] = scale_of[turn_of][chunk * 8 + i];
+            for (int p = 0; p < OwnPanel::kCopies; ++p) *(i32x4 *)(own.bytes + (p * kThreads + t) * 16) = own_raw[p];
         }
-        if constexpr (kShift) {
-            // 448 S / 2^shift stays below 2^15; a new shift leaves room for S to grow 16 times.
-            const int most = __builtin_amdgcn_readfirstlane(most_of[turn_of]) - 127;
-            if (most - shift > kMostLeft) {
-                const int to = most - kMostLeft + 4;
+        if constexpr (!kSharedDirect) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int p = 0; p < SharedPanel::kCopies; ++p) *(i32x4 *)(shared.bytes + (p * kThreads + t) * 16) = shared_raw[p];
+        }
+    };
+
+    // x's columns are the rows of the unit's result, of which a lane has four neighbours.
+    f32x4 sum[kSharedTiles][kOwnTiles] = {};
+    int shift = -200;
+    const int own_half = wave * 64 / kBlock;
+    const uint32_t shared_first = SharedPanel::first_of(lane), own_first = OwnPanel::first_of(lane) ^ wave * kOwnTiles * OwnPanel::kTile;
+    auto multiply_step = [&](const OwnPanel &own, const SharedPanel &shared, int of) {
+        if constexpr (S::kShift) {
+            const int to = __builtin_amdgcn_readfirstlane(shift_of[of][own_half]);
+            if (to != shift) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                for (int i = 0; i < kSharedTiles; ++i)
+#pragma unroll
+                    for (int j = 0; j < kOwnTiles; ++j)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) sum[i][j][r] = ldexpf(sum[i][j][r], shift - to);
                 shift = to;
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) scale[i] = ldexpf(scale[i], -shift);
         }
-        __syncthreads(); // the last step's operands have been read
-        turn<OD>(raw_dy, scale, &of_dy[0][chunk][quad]);
-        turn<OX>(raw_x, scale, &of_x[0][chunk][quad]);
-        if (t < kSlots) {
-            put(turn_of ^ 1, row, next_scale);
-            next_row = row_at(m + 2 * kSlots + t);
+#pragma unroll
+        for (int s = 0; s < kSlots; s += 32) {
+            Piece other[kSharedTiles];
+#pragma unroll
+            for (int i = 0; i < kSharedTiles; ++i) {
+                if constexpr (sizeof(Shared) == 1) other[i] = widened(shared.read(s, shared_first, i));
+                else other[i] = shared.read(s, shared_first, i);
+            }
+            EightScales<S::kHalf> scale;
+            const int c = s + lane / 16 * 8;
+            if constexpr (S::kShift) {
+                __builtin_memcpy(scale.first, &first_of[of][own_half][c], 16);
+                if constexpr (kExact) __builtin_memcpy(scale.rest, &rest_of[of][own_half][c], 16);
+            } else if constexpr (S::kScaled) {
+                __builtin_memcpy(scale.s, &first_of[of][own_half][c], 32);
+            }
+#pragma unroll
+            for (int j = 0; j < kOwnTiles; ++j) {
+                each_part<S>(own.read(s, own_first, j), scale, [&](const Piece &part) {
+#pragma unroll
+                    for (int i = 0; i < kSharedTiles; ++i)
+                        sum[i][j] = S::kOwnX ? multiply<S::kHalf>(part, other[i], sum[i][j]) : multiply<S::kHalf>(other[i], part, sum[i][j]);
+                });
+                // The sums stay where they are: else the compiler moves them about, and runs out of registers.
+#pragma unroll
+                for (int i = 0; i < kSharedTiles; ++i) asm volatile("" : "+v"(sum[i][j]));
+            }
+        }
+    };
+
+    int row = -1, token = -1, of = 0;
+    // A step: the copies of the one after it go out, then it is multiplied.
+    auto step = [&](auto &own, auto &shared, auto &next_own, auto &next_shared, int64_t m) {
+        __syncthreads(); // its copies are there, what was read of the others too
+        const int next = of == kInfos - 1 ? 0 : of + 1, after = next == kInfos - 1 ? 0 : next + 1;
+        if (informs) {
+            put(after, row);
+            row = row_of(m + 3 * kSlots + slot, token);
+            load_scales(m + 3 * kSlots + slot, row);
+            token = token_at(m + 4 * kSlots + slot);
+        }
+        const bool more = m + kSlots < end;
+        if (more) copy_step(next_own, next_shared, m + kSlots, next);
+        multiply_step(own, shared, of);
+        if (more) store_step(next_own, next_shared);
+        of = next;
+    };
+    if (begin < end) {
+        if (informs) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const int64_t m = (int64_t)begin + i * kSlots + slot;
+                row = row_of(m, token_at(m));
+                load_scales(m, row);
+                if (i < 2) put(i, row);
+            }
+            token = token_at((int64_t)begin + 3 * kSlots + slot);
         }
         __syncthreads();
-        if (m + kSlots < end) load(m + kSlots, row_of[turn_of ^ 1]);
-#pragma unroll
-        for (int s = 0; s < kSlots / 32; ++s) {
-            const int c = s * 4 + lane / 16;
-            Piece x[OX::kParts][4], y[OD::kParts][4];
-#pragma unroll
-            for (int p = 0; p < OX::kParts; ++p)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[p][j] = of_x[p][c][j * kQuads + wk * 16 + lane % 16];
-#pragma unroll
-            for (int p = 0; p < OD::kParts; ++p)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[p][j] = of_dy[p][c][j * kQuads + wn * 16 + lane % 16];
-#pragma unroll
-            for (int q = 0; q < OD::kParts; ++q)
-#pragma unroll
-                for (int p = 0; p < OX::kParts; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) sum[i][j] = multiply<kHalf>(x[p][j], y[q][i], sum[i][j]);
+        copy_step(own_even, shared_even, begin, 0);
+        store_step(own_even, shared_even);
+        for (int64_t m = begin; m < end; m += 2 * kSlots) {
+            step(own_even, shared_even, own_odd, shared_odd, m);
+            if (m + kSlots < end) step(own_odd, shared_odd, own_even, shared_even, m + kSlots);
         }
     }
 
-    // Lane l has column l % 16 of the unit's result (dy's) and rows 4 (l / 16) + r.
+    // Lane l has column l % 16 of the unit's result (dy's) and rows 4 (l / 16) + r (x's).
     float *partial = a.partial ? a.partial + ((int64_t)split * a.E + e) * a.N * a.K : nullptr;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = n0 + wn * 64 + lane % 16 * kQuad + i;
-        if (n >= a.N) continue;
+    for (int j = 0; j < kOwnTiles; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int k = k0 + wk * 64 + (lane / 16 * 4 + r) * kQuad;
-            if (k >= a.K) continue;
+        for (int i = 0; i < kSharedTiles; ++i) {
+            const int own = own0 + wave * 64 + j * 16, shared = shared0 + i * 16;
+            const int n = (S::kOwnX ? shared : own) + lane % 16, k = (S::kOwnX ? own : shared) + lane / 16 * kQuad;
+            if (n >= a.N || k >= a.K) continue;
             float v[kQuad];
 #pragma unroll
-            for (int j = 0; j < kQuad; ++j) v[j] = kShift ? ldexpf(sum[i][j][r], shift) : sum[i][j][r];
-            const int left = a.K - k;
-            if (partial) {
-                float *to = partial + (int64_t)n * a.K + k;
-                if (left >= kQuad) {
-                    const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
-                    *(i32x4_any *)to = w;
-                } else {
-                    for (int j = 0; j < left; ++j) to[j] = j == 0 ? v[0] : j == 1 ? v[1] : v[2];
-                }
-                continue;
-            }
-            const int64_t place = ((int64_t)e * a.N + n) * a.lddw + k;
-#pragma unroll
-            for (int j = 0; j < kQuad; ++j) {
-                if (j >= left) break;
-                if (a.out_type == EB_F32) {
-                    float *to = (float *)a.dw + place + j;
-                    *to = a.accumulate ? *to + v[j] : v[j];
-                } else if (a.out_type == EB_F16) {
-                    _Float16 *to = (_Float16 *)a.dw + place + j;
-                    *to = (_Float16)(a.accumulate ? (float)*to + v[j] : v[j]);
-                } else {
-                    __bf16 *to = (__bf16 *)a.dw + place + j;
-                    *to = (__bf16)(a.accumulate ? (float)*to + v[j] : v[j]);
-                }
-            }
+            for (int r = 0; r < kQuad; ++r) v[r] = S::kShift ? ldexpf(sum[i][j][r], shift) : sum[i][j][r];
+            write_quad(a, partial, e, n, k, v);
         }
-    }
 }
 
 } // namespace eb_gradient

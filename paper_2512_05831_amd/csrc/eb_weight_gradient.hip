@@ -2,6 +2,7 @@
 // its kernel.
 
 #include <algorithm>
+#include <utility>
 
 #include "eb_weight_gradient.h"
 
@@ -19,16 +20,9 @@ __global__ __launch_bounds__(kThreads) void eb_gradient_join(GradientArgs a)
         float v = 0.f;
         for (int s = 0; s < a.splits; ++s) v += a.partial[s * all + i];
         const int64_t place = i / a.K * a.lddw + i % a.K;
-        if (a.out_type == EB_F32) {
-            float *to = (float *)a.dw + place;
-            *to = a.accumulate ? *to + v : v;
-        } else if (a.out_type == EB_F16) {
-            _Float16 *to = (_Float16 *)a.dw + place;
-            *to = (_Float16)(a.accumulate ? (float)*to + v : v);
-        } else {
-            __bf16 *to = (__bf16 *)a.dw + place;
-            *to = (__bf16)(a.accumulate ? (float)*to + v : v);
-        }
+        if (a.out_type == EB_F32) write_out((float *)a.dw + place, a.accumulate, v);
+        else if (a.out_type == EB_F16) write_out((_Float16 *)a.dw + place, a.accumulate, v);
+        else write_out((__bf16 *)a.dw + place, a.accumulate, v);
     }
 }
 
@@ -40,13 +34,14 @@ int check_sizes(const char *who, int64_t M, int32_t E, int64_t N, int64_t K)
     return EB_OK;
 }
 
-int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
+int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-// Parts that an expert's slots are split into where there are few tiles.
+// Parts that an expert's slots are split into where there are few tiles (counted with
+// dy as the own operand; with x it is nearly as many).
 int32_t splits_of(int64_t M, int32_t E, int64_t N, int64_t K)
 {
     constexpr int64_t kEnough = 512, kLeastSlots = 256, kMostSplits = 64;
-    const int64_t n = tiles_of(N), k = tiles_of(K);
+    const int64_t n = tiles_of(N, kOwnTile), k = tiles_of(K, kSharedTile);
     if (E >= kEnough || n >= kEnough || k >= kEnough || E * n * k >= kEnough) return 1;
     const int64_t mean = (M + E - 1) / E;
     return (int32_t)std::max<int64_t>(1, std::min(std::min(kEnough / (E * n * k), mean / kLeastSlots), kMostSplits));
@@ -58,16 +53,28 @@ int64_t workspace_of(int64_t M, int32_t E, int64_t N, int64_t K)
     return splits > 1 ? splits * E * N * K * 4 : 0;
 }
 
+struct Choice {
+    void *kernel;
+    bool own_x;
+};
+
 template <typename D, typename X>
-void *kernel_of(bool exact)
+Choice choice_of(bool exact, bool direct)
 {
-    return exact ? (void *)eb_gradient_tile<D, X, true> : (void *)eb_gradient_tile<D, X, false>;
+    constexpr bool kX = Shape<D, X, true>::kOwnX;
+    if constexpr (sizeof(D) == 1 && sizeof(X) == 1) direct = true;
+    if (direct) return {exact ? (void *)eb_gradient_tile<D, X, true, true> : (void *)eb_gradient_tile<D, X, false, true>, kX};
+    if constexpr (sizeof(D) == 2 || sizeof(X) == 2)
+        return {exact ? (void *)eb_gradient_tile<D, X, true, false> : (void *)eb_gradient_tile<D, X, false, false>, kX};
+    return {};
 }
 
 template <typename D>
-void *kernel_of(int32_t x_type, bool exact)
+Choice choice_of(int32_t x_type, bool exact, bool direct)
 {
-    return x_type == EB_FP8 ? kernel_of<D, Fp8>(exact) : x_type == EB_F16 ? kernel_of<D, _Float16>(exact) : kernel_of<D, Bf16>(exact);
+    return x_type == EB_FP8   ? choice_of<D, Fp8>(exact, direct)
+           : x_type == EB_F16 ? choice_of<D, _Float16>(exact, direct)
+                              : choice_of<D, Bf16>(exact, direct);
 }
 
 int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *dy, int32_t dy_type, int64_t lddy,
@@ -87,35 +94,47 @@ int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, c
     const int64_t need = workspace_of(M, E, N, K);
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < (size_t)need))
         return fail(EB_ERR_INVALID, "%s: workspace too small or not a multiple of 16 bytes", who);
+    const bool exact = out_type != EB_BF16;
+    auto whole = [](const void *p, int32_t type, int64_t cols, int64_t ld) { // rows of whole pieces of 16 bytes
+        return type == EB_FP8 || ((uintptr_t)p % 16 == 0 && cols % 8 == 0 && ld % 8 == 0);
+    };
+    const bool direct = whole(dy, dy_type, N, lddy) && whole(x, x_type, K, ldx);
+    const Choice choice = dy_type == EB_FP8   ? choice_of<Fp8>(x_type, exact, direct)
+                          : dy_type == EB_F16 ? choice_of<_Float16>(x_type, exact, direct)
+                                              : choice_of<Bf16>(x_type, exact, direct);
     GradientArgs a{};
-    a.dy = (const char *)dy;
-    a.x = (const char *)x;
-    a.dy_scales = {dy_scales, lddys};
-    a.x_scales = {x_scales, ldxs};
+    a.own = (const char *)dy;
+    a.shared = (const char *)x;
+    a.own_scales = {dy_scales, lddys};
+    a.shared_scales = {x_scales, ldxs};
+    a.own_ld = lddy * element_bytes(dy_type);
+    a.shared_ld = ldx * element_bytes(x_type);
+    a.own_cols = (int32_t)N;
+    a.shared_cols = (int32_t)K;
+    if (choice.own_x) {
+        std::swap(a.own, a.shared);
+        std::swap(a.own_scales, a.shared_scales);
+        std::swap(a.own_ld, a.shared_ld);
+        std::swap(a.own_cols, a.shared_cols);
+    }
     a.tokens = tokens;
     a.offsets = offsets;
     a.dw = dw;
     a.partial = need > 0 ? (float *)workspace : nullptr;
-    a.lddy = lddy * element_bytes(dy_type);
-    a.ldx = ldx * element_bytes(x_type);
     a.x_rows = x_rows;
     a.lddw = lddw;
     a.M = (int32_t)M;
     a.E = E;
     a.N = (int32_t)N;
     a.K = (int32_t)K;
-    a.n_tiles = (int32_t)tiles_of(N);
-    a.k_tiles = (int32_t)tiles_of(K);
+    a.own_tiles = (int32_t)tiles_of(a.own_cols, kOwnTile);
+    a.shared_tiles = (int32_t)tiles_of(a.shared_cols, kSharedTile);
     a.splits = splits_of(M, E, N, K);
     a.out_type = out_type;
     a.accumulate = accumulate != 0;
-    const int64_t square = (int64_t)a.n_tiles * a.k_tiles; // below 2^46
+    const int64_t square = (int64_t)a.own_tiles * a.shared_tiles; // below 2^46
     const int64_t grid = square > kMax32 / E / a.splits ? kMax32 : square * E * a.splits;
-    const bool exact = out_type != EB_BF16;
-    void *kernel = dy_type == EB_FP8   ? kernel_of<Fp8>(x_type, exact)
-                   : dy_type == EB_F16 ? kernel_of<_Float16>(x_type, exact)
-                                       : kernel_of<Bf16>(x_type, exact);
-    if (int rc = launch(who, kernel, grid, kThreads, &a, stream)) return rc;
+    if (int rc = launch(who, choice.kernel, grid, kThreads, &a, stream)) return rc;
     if (need == 0) return EB_OK;
     const int64_t all = E * N * K;
     return launch(who, (void *)eb_gradient_join, std::min<int64_t>((all + kThreads - 1) / kThreads, 8192), kThreads, &a, stream);
