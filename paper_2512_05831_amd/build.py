@@ -8,7 +8,7 @@
 benchmark uses), the experts' operators (``csrc/eb_route_experts.hip``,
 ``csrc/eb_quantize_fp8.hip``, ``csrc/eb_expert_product*.hip``) and those that
 train them (``csrc/eb_layer_norm*.hip``, ``csrc/eb_activation.hip``,
-``csrc/eb_sort_rows.hip``, ``csrc/eb_weight_gradient.hip``) and writes
+``csrc/eb_sort_rows.hip``, ``csrc/eb_weight_gradient*.hip``) and writes
 ``libeb.so`` next to this file.
 """
 from __future__ import annotations
@@ -26,7 +26,8 @@ SRCS = [os.path.join(HERE, "csrc", f)
                   "eb_route_experts.hip", "eb_quantize_fp8.hip", "eb_expert_product.hip",
                   "eb_expert_product_stream.hip", "eb_expert_product_tile.hip",
                   "eb_layer_norm.hip", "eb_layer_norm_backward.hip", "eb_activation.hip",
-                  "eb_sort_rows.hip", "eb_weight_gradient.hip")]
+                  "eb_sort_rows.hip", "eb_weight_gradient.hip", "eb_weight_gradient_fp8.hip",
+                  "eb_weight_gradient_f16.hip", "eb_weight_gradient_bf16.hip")]
 LIB = os.path.join(HERE, "libeb.so")
 ARCH = "gfx950"
 

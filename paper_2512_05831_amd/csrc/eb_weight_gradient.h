@@ -33,7 +33,7 @@ namespace eb_gradient {
 using namespace eb_train;
 
 constexpr int kThreads = 256;
-constexpr int kOwnTile = 256, kSharedTile = 128; // columns of a workgroup
+constexpr int kOwnTile = 256; // columns of the own operand, of a workgroup
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -93,8 +93,13 @@ struct Panel {
     // The piece of a row that lies in place `at` of it.
     static __device__ __forceinline__ uint32_t piece_of(uint32_t row, uint32_t at)
     {
-        if constexpr (sizeof(T) == 1) return at ^ (kPieces == 16 ? row % 16 : row / 2 % 8);
-        else return at ^ 2 * (row % 4 | row / 8 % 2 * 4);
+        return at ^ (sizeof(T) == 1 ? swap_of(row) : 2 * swap_of(row));
+    }
+    // 16 rows of 8 bits, one piece each, and 8 of 16 bits, two, fill a line of the banks.
+    static __device__ __forceinline__ uint32_t swap_of(uint32_t row)
+    {
+        if constexpr (sizeof(T) == 1) return row / (16 / kPieces) % kPieces;
+        else return kPieces >= 16 ? row % 4 | row / 8 % 2 * 4 : row / 2 % 2 | row / 8 % 2 * 2;
     }
 
     // Where a lane reads from for column tile 0; for tile i that ^ i * kTile.
@@ -104,9 +109,10 @@ struct Panel {
         const uint32_t g = lane / 16, in = lane % 16;
         if constexpr (sizeof(T) == 1) {
             const uint32_t row = 8 * g + in / 2;
-            return row * kRow + (kPieces == 16 ? row % 16 : row / 2 % 8) * 16 + in % 2 * 8;
+            return row * kRow + swap_of(row) * 16 + in % 2 * 8;
         } else {
-            return (8 * g + in / 4) * kRow + (in / 4 | g % 2 * 4) * 32 + in % 4 * 8;
+            const uint32_t row = 8 * g + in / 4; // and the fourth from it, of the same swap
+            return row * kRow + swap_of(row) * 32 + in % 4 * 8;
         }
     }
 
@@ -278,8 +284,8 @@ __device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial
 
 // kDirect: 16-bit operands lie so that 16 bytes can be copied to LDS at a time (8-bit
 // ones always do); else they go through registers.
-template <typename D, typename X, bool kExact, bool kDirect>
-__global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
+template <typename D, typename X, bool kExact, bool kDirect, int kSharedTile>
+__global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) void eb_gradient_tile(GradientArgs a)
 {
     using S = Shape<D, X, kExact>;
     using Own = typename S::Own;
@@ -327,7 +333,7 @@ __global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
     float own_scale = 0.f, shared_scale = 1.f;
     auto load_scales = [&](int64_t m, int row) {
         if constexpr (S::kScaled) own_scale = a.own_scales.p[block * a.own_scales.ld + (S::kOwnX ? max(row, 0) : min(m, (int64_t)end - 1))];
-        if constexpr (S::kBoth) shared_scale = a.shared_scales.p[shared_tile * a.shared_scales.ld + max(row, 0)];
+        if constexpr (S::kBoth) shared_scale = a.shared_scales.p[shared0 / kBlock * a.shared_scales.ld + max(row, 0)];
     };
     int next_shift = -200; // below any scale's exponent
     auto put = [&](int of, int row) {
@@ -446,7 +452,8 @@ __global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
     int row = -1, token = -1, of = 0;
     // A step: the copies of the one after it go out, then it is multiplied.
     auto step = [&](auto &own, auto &shared, auto &next_own, auto &next_shared, int64_t m) {
-        __syncthreads(); // its copies are there, what was read of the others too
+        __builtin_amdgcn_s_waitcnt(0x0F70); // vmcnt(0): this wave's copies, which a barrier does not wait for
+        __syncthreads();                    // all its copies are there, and the other step's have been read
         const int next = of == kInfos - 1 ? 0 : of + 1, after = next == kInfos - 1 ? 0 : next + 1;
         if (informs) {
             put(after, row);
@@ -495,5 +502,43 @@ __global__ __launch_bounds__(kThreads, 2) void eb_gradient_tile(GradientArgs a)
             write_quad(a, partial, e, n, k, v);
         }
 }
+
+struct Choice {
+    void *kernel;
+    bool own_x;
+};
+
+template <typename D, typename X, int kSharedTile>
+Choice choice_of(bool exact, bool direct)
+{
+    using S = Shape<D, X, true>;
+    if constexpr (S::kAsItIs && !S::kScaled) exact = true; // the same
+    if constexpr (sizeof(D) == 1 && sizeof(X) == 1) direct = true;
+    if (direct && exact) return {(void *)eb_gradient_tile<D, X, true, true, kSharedTile>, S::kOwnX};
+    if constexpr (!S::kAsItIs || S::kScaled)
+        if (direct) return {(void *)eb_gradient_tile<D, X, false, true, kSharedTile>, S::kOwnX};
+    if constexpr (sizeof(D) == 2 || sizeof(X) == 2) {
+        if (exact) return {(void *)eb_gradient_tile<D, X, true, false, kSharedTile>, S::kOwnX};
+        if constexpr (!S::kAsItIs || S::kScaled) return {(void *)eb_gradient_tile<D, X, false, false, kSharedTile>, S::kOwnX};
+    }
+    return {};
+}
+
+template <typename D>
+Choice choice_of(int32_t x_type, bool exact, bool direct, bool narrow)
+{
+    if (narrow)
+        return x_type == EB_FP8   ? choice_of<D, Fp8, 64>(exact, direct)
+               : x_type == EB_F16 ? choice_of<D, _Float16, 64>(exact, direct)
+                                  : choice_of<D, Bf16, 64>(exact, direct);
+    return x_type == EB_FP8   ? choice_of<D, Fp8, 128>(exact, direct)
+           : x_type == EB_F16 ? choice_of<D, _Float16, 128>(exact, direct)
+                              : choice_of<D, Bf16, 128>(exact, direct);
+}
+
+// By dy's type, each in a source of its own.
+Choice choice_fp8(int32_t x_type, bool exact, bool direct, bool narrow);
+Choice choice_f16(int32_t x_type, bool exact, bool direct, bool narrow);
+Choice choice_bf16(int32_t x_type, bool exact, bool direct, bool narrow);
 
 } // namespace eb_gradient

@@ -36,45 +36,41 @@ int check_sizes(const char *who, int64_t M, int32_t E, int64_t N, int64_t K)
 
 int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-// Parts that an expert's slots are split into where there are few tiles (counted with
-// dy as the own operand; with x it is nearly as many).
-int32_t splits_of(int64_t M, int32_t E, int64_t N, int64_t K)
+// How a call is cut up, from its sizes alone (so that its workspace is known without
+// types; tiles are counted with dy as the own operand, with x they are nearly as many).
+// Measured in turn, us a call:
+//   Shared columns 64 or 128.  Narrow tiles let three workgroups share a compute unit,
+//   wide ones read less: one expert, 2048 slots by 1000 x 1512 in bf16 (1536 steps of 64
+//   slots in all) 28.8 and 29.5; 32 experts of 512 x 1024, 256 slots each (2048) 34.6 and
+//   37.3; 16384 by 512 x 512 in bf16 (2048) 32.8 and 39.4; 8192 by 1024 x 1024 in 8 bits (4096)
+//   55.2 and 54.8; 2048 by 2560 x 2048 (5120) 68.8 and 65.2; 16384 by 2048 x 2048 (32768) 300 and 250.
+//   Parts of an expert's slots.  They fill the GPU, and cost 8 bytes of traffic an
+//   output each: 2048 slots by 1000 x 1512 in 2, 4, 8 parts 31.6, 28.8, 32.2; 8192 by 1024 x 1024
+//   in 4, 8, 16 parts 70.9, 55.2, 61.6; 16384 by 2048 x 2048 in 2, 4, 8 parts 309, 250, 273.
+struct Cut {
+    bool narrow;
+    int32_t splits;
+};
+
+Cut cut_of(int64_t M, int32_t E, int64_t N, int64_t K)
 {
-    constexpr int64_t kEnough = 512, kLeastSlots = 256, kMostSplits = 64;
-    const int64_t n = tiles_of(N, kOwnTile), k = tiles_of(K, kSharedTile);
-    if (E >= kEnough || n >= kEnough || k >= kEnough || E * n * k >= kEnough) return 1;
-    const int64_t mean = (M + E - 1) / E;
-    return (int32_t)std::max<int64_t>(1, std::min(std::min(kEnough / (E * n * k), mean / kLeastSlots), kMostSplits));
+    constexpr int64_t kFewSteps = 4096, kWide = 512, kNarrow = 768, kLeastSlots = 512, kMostSplits = 64;
+    const int64_t n = tiles_of(N, kOwnTile), mean = (M + E - 1) / E;
+    auto tiles = [&](int64_t width) { // or `many`, whatever lies above
+        constexpr int64_t many = (int64_t)1 << 20;
+        const int64_t k = tiles_of(K, width);
+        return E >= many || n >= many || k >= many || n * k >= many ? many : std::min(E * n * k, many);
+    };
+    Cut c{};
+    c.narrow = tiles(128) * ((mean + 63) / 64) <= kFewSteps;
+    c.splits = (int32_t)std::max<int64_t>(1, std::min({c.narrow ? kNarrow / tiles(64) : kWide / tiles(128), mean / kLeastSlots, kMostSplits}));
+    return c;
 }
 
 int64_t workspace_of(int64_t M, int32_t E, int64_t N, int64_t K)
 {
-    const int64_t splits = splits_of(M, E, N, K);
+    const int64_t splits = cut_of(M, E, N, K).splits;
     return splits > 1 ? splits * E * N * K * 4 : 0;
-}
-
-struct Choice {
-    void *kernel;
-    bool own_x;
-};
-
-template <typename D, typename X>
-Choice choice_of(bool exact, bool direct)
-{
-    constexpr bool kX = Shape<D, X, true>::kOwnX;
-    if constexpr (sizeof(D) == 1 && sizeof(X) == 1) direct = true;
-    if (direct) return {exact ? (void *)eb_gradient_tile<D, X, true, true> : (void *)eb_gradient_tile<D, X, false, true>, kX};
-    if constexpr (sizeof(D) == 2 || sizeof(X) == 2)
-        return {exact ? (void *)eb_gradient_tile<D, X, true, false> : (void *)eb_gradient_tile<D, X, false, false>, kX};
-    return {};
-}
-
-template <typename D>
-Choice choice_of(int32_t x_type, bool exact, bool direct)
-{
-    return x_type == EB_FP8   ? choice_of<D, Fp8>(exact, direct)
-           : x_type == EB_F16 ? choice_of<D, _Float16>(exact, direct)
-                              : choice_of<D, Bf16>(exact, direct);
 }
 
 int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, const void *dy, int32_t dy_type, int64_t lddy,
@@ -99,9 +95,10 @@ int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, c
         return type == EB_FP8 || ((uintptr_t)p % 16 == 0 && cols % 8 == 0 && ld % 8 == 0);
     };
     const bool direct = whole(dy, dy_type, N, lddy) && whole(x, x_type, K, ldx);
-    const Choice choice = dy_type == EB_FP8   ? choice_of<Fp8>(x_type, exact, direct)
-                          : dy_type == EB_F16 ? choice_of<_Float16>(x_type, exact, direct)
-                                              : choice_of<Bf16>(x_type, exact, direct);
+    const auto [narrow, splits] = cut_of(M, E, N, K);
+    const Choice choice = dy_type == EB_FP8   ? choice_fp8(x_type, exact, direct, narrow)
+                          : dy_type == EB_F16 ? choice_f16(x_type, exact, direct, narrow)
+                                              : choice_bf16(x_type, exact, direct, narrow);
     GradientArgs a{};
     a.own = (const char *)dy;
     a.shared = (const char *)x;
@@ -128,8 +125,8 @@ int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, c
     a.N = (int32_t)N;
     a.K = (int32_t)K;
     a.own_tiles = (int32_t)tiles_of(a.own_cols, kOwnTile);
-    a.shared_tiles = (int32_t)tiles_of(a.shared_cols, kSharedTile);
-    a.splits = splits_of(M, E, N, K);
+    a.shared_tiles = (int32_t)tiles_of(a.shared_cols, narrow ? 64 : 128);
+    a.splits = splits;
     a.out_type = out_type;
     a.accumulate = accumulate != 0;
     const int64_t square = (int64_t)a.own_tiles * a.shared_tiles; // below 2^46
