@@ -31,47 +31,64 @@ struct ActArgs {
     bool gate;
 };
 
-__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269502f)); }
-
-// Columns c .. c + 7 of v, of which those in [lo, hi) count.
-template <typename T>
-__device__ __forceinline__ void load_v(const ActArgs &a, int64_t row, int64_t c, int64_t lo, int64_t hi, float *f)
+// 1 / (1 + exp(-g)): the exponential with the rounding of its argument put right.
+__device__ __forceinline__ float sigmoid(float g)
 {
-    const Raw<T> r = load_raw((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
+    constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f; // together log2(e) to 2^-50
+    const float h = g * -kLog2e, l = fmaf(g, -kRest, fmaf(g, -kLog2e, -h));
+    const float e = __builtin_amdgcn_exp2f(h);
+    // (l is 0 or a NaN where h is infinite or far below: then e stands.)
+    return __builtin_amdgcn_rcpf(1.f + (fabsf(h) < 126.f ? fmaf(e, l * 0.693147182f, e) : e));
+}
+
+// Columns c .. c + 7 of v that lie in [lo, hi); zeros for the others.
+template <typename T>
+__device__ __forceinline__ Raw<T> load_v(const ActArgs &a, int64_t row, int c, int lo, int hi)
+{
+    return load_raw((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
+}
+
+template <typename T>
+__device__ __forceinline__ void widen_v(const ActArgs &a, int64_t row, int c, int hi, const Raw<T> &r, float *f)
+{
     widen8(r, f);
-    if constexpr (sizeof(T) == 1) scale8(f, scales_at(a.v_scales, row, c, hi));
+    if constexpr (sizeof(T) == 1) scale8(f, a.v_scales, row, c, hi);
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void eb_activate(ActArgs a)
 {
-    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
     const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
-    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    const int b0 = blockIdx.x % strips * kSteps, cols = (int)a.cols, width = (int)a.width;
     if (row >= a.rows) return;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-        const int64_t c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        const int c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
         float g[kEach], h[kEach];
-        load_v<T>(a, row, c, 0, a.cols, g);
+        const Raw<T> first = load_v<T>(a, row, c, 0, cols);
         if (a.gate) {
+            const Raw<T> second = load_v<T>(a, row, cols + c, cols, width);
             float u[kEach];
-            load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+            widen_v(a, row, c, cols, first, g);
+            widen_v(a, row, cols + c, width, second, u);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
         } else {
+            widen_v(a, row, c, cols, first, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] > 0.f ? g[i] : g[i] == g[i] ? 0.f : g[i];
         }
-        store_out(a.out, row, c, a.cols, h, a.out.type == EB_FP8 ? max_lanes<kLanes>(most8(h)) : 0);
+        store_out(a.out, row, c, cols, h);
     }
 }
 
-__device__ __forceinline__ float d_gate(float dh, float g, float u)
+// dg and du.
+__device__ __forceinline__ float2 d_gate(float dh, float g, float u)
 {
-    const float p = sigmoid(g);
-    return dh * u * p * (1.f + g * (1.f - p));
+    const float p = sigmoid(g), dp = dh * p;
+    return {dp * u * fmaf(g, 1.f - p, 1.f), dp * g};
 }
 
 // dg and du by the lane that has both g and u: floating-point outputs, and 8-bit
@@ -79,40 +96,45 @@ __device__ __forceinline__ float d_gate(float dh, float g, float u)
 template <typename D, typename T>
 __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
 {
-    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
     const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
-    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    const int b0 = blockIdx.x % strips * kSteps, cols = (int)a.cols, width = (int)a.width;
     if (row >= a.rows) return;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-        const int64_t c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        const int c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
         float dh[kEach], g[kEach], d[kEach];
-        widen8(load_raw((const D *)a.dh + row * a.lddh, c, a.cols), dh);
-        load_v<T>(a, row, c, 0, a.cols, g);
-        const bool fp8 = a.out.type == EB_FP8;
+        const Raw<D> of_h = load_raw((const D *)a.dh + row * a.lddh, c, cols);
+        const Raw<T> first = load_v<T>(a, row, c, 0, cols);
         if (!a.gate) {
+            widen8(of_h, dh);
+            widen_v(a, row, c, cols, first, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) d[i] = g[i] > 0.f ? dh[i] : 0.f;
-            store_out(a.out, row, c, a.cols, d, fp8 ? max_lanes<kLanes>(most8(d)) : 0);
+            store_out(a.out, row, c, cols, d);
             continue;
         }
+        const Raw<T> second = load_v<T>(a, row, cols + c, cols, width);
         float u[kEach], e[kEach];
-        load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+        widen8(of_h, dh);
+        widen_v(a, row, c, cols, first, g);
+        widen_v(a, row, cols + c, width, second, u);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            d[i] = d_gate(dh[i], g[i], u[i]);
-            e[i] = dh[i] * g[i] * sigmoid(g[i]);
+            const float2 v = d_gate(dh[i], g[i], u[i]);
+            d[i] = v.x;
+            e[i] = v.y;
         }
-        if (fp8) {
-            store_out(a.out, row, c, a.width, d, max_lanes<kLanes>(most8(d)));
-            store_out(a.out, row, a.cols + c, a.width, e, max_lanes<kLanes>(most8(e)));
+        Out of_u = a.out;
+        if (a.out.type == EB_FP8) { // whole blocks
+            of_u.p = (char *)a.out.p + cols;
+            of_u.scales = a.out.scales + cols / kBlock * a.out.lds;
         } else {
-            store_out(a.out, row, c, a.cols, d, 0);
-            Out second = a.out;
-            second.p = (char *)a.out.p + a.cols * (a.out.type == EB_F32 ? 4 : 2);
-            store_out(second, row, c, a.cols, e, 0);
+            of_u.p = (char *)a.out.p + cols * (int64_t)(a.out.type == EB_F32 ? 4 : 2);
         }
+        store_out(a.out, row, c, cols, d);
+        store_out(of_u, row, c, cols, e);
     }
 }
 
@@ -121,32 +143,33 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
 template <typename D, typename T>
 __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
 {
-    const int64_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
     const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
-    const int64_t b0 = (int64_t)(blockIdx.x % strips) * kSteps;
+    const int b0 = blockIdx.x % strips * kSteps, cols = (int)a.cols, width = (int)a.width;
     if (row >= a.rows) return;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-        const int64_t at = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
+        const int at = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
-        float d[kEach] = {}, e[kEach] = {}, dh[kEach], g[kEach], u[kEach];
-        auto both = [&](int64_t c, bool first) {
-            widen8(load_raw((const D *)a.dh + row * a.lddh, c, a.cols), dh);
-            load_v<T>(a, row, c, 0, a.cols, g);
-            if (first) {
-                load_v<T>(a, row, a.cols + c, a.cols, a.width, u);
+        float d[kEach] = {}, dh[kEach], g[kEach], u[kEach];
+        auto take = [&](int c, bool first) { // columns c on of dg, or of du
+            const Raw<D> of_h = load_raw((const D *)a.dh + row * a.lddh, c, cols);
+            const Raw<T> of_g = load_v<T>(a, row, c, 0, cols), of_u = load_v<T>(a, row, cols + c, cols, width);
+            widen8(of_h, dh);
+            widen_v(a, row, c, cols, of_g, g);
+            // (Of du's first chunk some columns lie before u, and before dh and g: zeros.)
+            widen8(of_u, u);
+            if (sizeof(T) == 1 && first) scale8(u, a.v_scales, row, cols + c, width);
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) d[i] = c + i < a.cols ? d_gate(dh[i], g[i], u[i]) : 0.f;
-            } else {
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) e[i] = c + i >= 0 && c + i < a.cols ? dh[i] * g[i] * sigmoid(g[i]) : 0.f;
+            for (int i = 0; i < kEach; ++i) {
+                if (c + i < 0 || c + i >= cols) continue;
+                const float2 v = d_gate(dh[i], g[i], u[i]);
+                d[i] = first ? v.x : v.y;
             }
         };
-        if (at < a.cols) both(at, true);
-        if (at + kEach > a.cols) both(at - a.cols, false);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) d[i] = at + i < a.cols ? d[i] : e[i];
-        store_out(a.out, row, at, a.width, d, max_lanes<kLanes>(most8(d)));
+        if (at < cols) take(at, true);
+        if (at + kEach > cols) take(at - cols, false);
+        store_out(a.out, row, at, width, d);
     }
 }
 

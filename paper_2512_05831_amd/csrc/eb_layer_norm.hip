@@ -43,76 +43,115 @@ __device__ __forceinline__ float sum_row(float v, float *shared, int wave)
     return v;
 }
 
-__device__ __forceinline__ void normalise8(const NormArgs &a, int64_t row, int64_t c, const float *f, float mean, float rstd)
+// The outputs of columns c .. c + 7, of which d is x - mean (zeros past cols).
+__device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, const float *d, float rstd)
 {
-    if (c >= ((a.cols + kBlock - 1) & ~(int64_t)(kBlock - 1))) return; // whole blocks: their 16 lanes stay together
-    const int64_t left = a.cols - c;
-    float n[kEach], y[kEach];
+    const int cols = (int)a.cols;
+    if (c >= ((cols + kBlock - 1) & ~(kBlock - 1))) return; // whole blocks: their 16 lanes stay together
+    float n[kEach], y[kEach], w[kEach], b[kEach];
+    if (a.weight) widen8(load_raw(a.weight, c, cols), w);
+    if (a.bias) widen8(load_raw(a.bias, c, cols), b);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) n[i] = i < left ? (f[i] - mean) * rstd : 0.f;
-    if (a.kept.p) store_out(a.kept, row, c, a.cols, n, max_lanes<kLanes>(most8(n)));
-    float w[kEach], b[kEach];
-    if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
-    if (a.bias) widen8(load_raw(a.bias, c, a.cols), b);
+    for (int i = 0; i < kEach; ++i) n[i] = d[i] * rstd;
+    if (a.kept.p) {
+        // n / scale is d times one factor: as exact as d.
+        const int most_d = max_lanes<kLanes>(most8(d)), most = magnitude(__int_as_float(most_d) * rstd);
+        if (__int_as_float(most) <= kMostFp8 * kLeastScale) store_fp8(a.kept, row, c, cols, n, 1.f / kLeastScale, most);
+        else store_fp8(a.kept, row, c, cols, d, kMostFp8 / __int_as_float(most_d), most);
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         y[i] = a.weight ? n[i] * w[i] : n[i];
         if (a.bias) y[i] += b[i];
     }
-    store_out(a.y, row, c, a.cols, y, a.y.type == EB_FP8 ? max_lanes<kLanes>(most8(y)) : 0);
+    store_out(a.y, row, c, cols, y);
 }
 
 // kSteps * 512 columns a wave; kLoop: any number of them, read again for each sum.
 template <typename T, int kSteps, int kWaves, bool kLoop>
-__global__ __launch_bounds__(kThreads) void eb_layer_norm_rows(NormArgs a)
+__global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_rows(NormArgs a)
 {
     __shared__ float shared[kWaves];
     constexpr int kRows = kThreads / kWave / kWaves;
-    const int wave = threadIdx.x / kWave % kWaves;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kWave / kWaves;
+    const int thread_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = thread_wave % kWaves;
+    const int64_t row = (int64_t)blockIdx.x * kRows + thread_wave / kWaves;
     if (row >= a.rows) return; // whole workgroups where waves share a row
     const T *x = (const T *)a.x + row * a.ldx;
-    const int64_t first = (wave * kWave + threadIdx.x % kWave) * kEach;
-    constexpr int64_t kAll = (int64_t)kStride * kWaves;
-    float f[kLoop ? 1 : kSteps][kEach];
-    float sum = 0.f;
-    auto over = [&](auto &&each) {
-        if constexpr (kLoop) {
-            for (int64_t c = first; c < ((a.cols + kBlock - 1) & ~(int64_t)(kBlock - 1)); c += kAll) {
-                widen8(load_raw(x, c, a.cols), f[0]);
-                each(c, f[0]);
-            }
-        } else {
+    const int cols = (int)a.cols, first = wave * kStride + threadIdx.x % kWave * kEach;
+    constexpr int kAll = kStride * kWaves;
+    auto centred = [&](int c, float *f, float mean) {
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) each(first + i * kAll, f[i]);
+        for (int i = 0; i < kEach; ++i) f[i] -= mean;
+        if (c + kEach > cols) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (c + i >= cols) f[i] = 0.f;
         }
     };
-    if constexpr (!kLoop) {
-        Raw<T> raw[kSteps];
+    auto add = [](const float *f, float sum) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(x, first + i * kAll, a.cols);
+        for (int i = 0; i < kEach; ++i) sum += f[i];
+        return sum;
+    };
+    auto add_squares = [](const float *f, float sum) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) widen8(raw[i], f[i]);
-    }
-    over([&](int64_t, const float *v) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) sum += v[i];
-    });
-    const float mean = sum_row<kWaves>(sum, shared, wave) / (float)a.cols;
-    float square = 0.f;
-    over([&](int64_t c, const float *v) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const float d = c + i < a.cols ? v[i] - mean : 0.f;
-            square = fmaf(d, d, square);
+        for (int i = 0; i < kEach; ++i) sum = fmaf(f[i], f[i], sum);
+        return sum;
+    };
+    auto statistics = [&](float mean, float rstd) {
+        if (threadIdx.x % (kWaves * kWave) == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
         }
-    });
-    const float rstd = 1.f / sqrtf(sum_row<kWaves>(square, shared, wave) / (float)a.cols + a.eps);
-    if (threadIdx.x % (kWaves * kWave) == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
+    };
+    const float of = (float)cols;
+    float sum = 0.f, square = 0.f;
+    if constexpr (kLoop) {
+        float f[kEach];
+        const int blocks = (cols + kBlock - 1) & ~(kBlock - 1);
+        for (int c = first; c < cols; c += kAll) {
+            widen8(load_raw(x, c, cols), f);
+            sum = add(f, sum);
+        }
+        const float mean = sum_row<kWaves>(sum, shared, wave) / of;
+        for (int c = first; c < cols; c += kAll) {
+            widen8(load_raw(x, c, cols), f);
+            centred(c, f, mean);
+            square = add_squares(f, square);
+        }
+        const float rstd = 1.f / sqrtf(sum_row<kWaves>(square, shared, wave) / of + a.eps);
+        statistics(mean, rstd);
+        for (int c = first; c < blocks; c += kAll) {
+            widen8(load_raw(x, c, cols), f);
+            centred(c, f, mean);
+            write8(a, row, c, f, rstd);
+        }
+    } else {
+        float f[kSteps][kEach];
+        {
+            Raw<T> raw[kSteps];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(x, first + i * kAll, cols);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                widen8(raw[i], f[i]);
+                sum = add(f[i], sum);
+            }
+        }
+        const float mean = sum_row<kWaves>(sum, shared, wave) / of;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            centred(first + i * kAll, f[i], mean);
+            square = add_squares(f[i], square);
+        }
+        const float rstd = 1.f / sqrtf(sum_row<kWaves>(square, shared, wave) / of + a.eps);
+        statistics(mean, rstd);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            write8(a, row, first + i * kAll, f[i], rstd);
+            __builtin_amdgcn_sched_barrier(0); // not all steps' weights at a time: registers
+        }
     }
-    over([&](int64_t c, const float *v) { normalise8(a, row, c, v, mean, rstd); });
 }
 
 struct Plan {

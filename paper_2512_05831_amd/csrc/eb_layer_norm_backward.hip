@@ -19,7 +19,7 @@ using namespace eb_train;
 
 constexpr int kThreads = 256;
 constexpr int kStride = kWave * kEach; // columns of a wave's step
-constexpr int kMostGroups = 512;       // workgroups that add up dweight and dbias
+constexpr int kMostGroups = 768;       // workgroups that add up dweight and dbias
 
 struct NormBackArgs {
     const void *dy, *x;
@@ -49,52 +49,79 @@ __device__ __forceinline__ float2 sum_row(float2 v, float2 *shared, int wave)
     return v;
 }
 
+template <typename D>
+constexpr int kTypeOf = sizeof(D) == 4 ? EB_F32 : std::is_same_v<D, Bf16> ? EB_BF16 : EB_F16;
+
+// A row's values as they lie in memory.
+template <typename D, typename T, int kSteps>
+struct RawRow {
+    Raw<D> dy[kSteps];
+    Raw<T> x[kSteps];
+    float scale[kSteps]; // of x in 8 bits
+    float rstd, mean;
+};
+
 template <typename D, typename T, int kSteps, int kWaves>
-__global__ __launch_bounds__(kThreads) void eb_layer_norm_back(NormBackArgs a)
+__global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_layer_norm_back(NormBackArgs a)
 {
-    constexpr int kRows = kThreads / kWave / kWaves; // rows that a workgroup holds at a time
-    constexpr int64_t kAll = (int64_t)kStride * kWaves;
+    constexpr int kRows = kWaves > 4 ? 1 : kThreads / kWave / kWaves; // rows that a workgroup holds at a time
+    constexpr int kAll = kStride * kWaves;
+    constexpr bool kFp8 = sizeof(T) == 1;
     __shared__ float2 shared[2][kWaves];
     __shared__ float joined[kRows > 1 ? (kRows - 1) * kSteps * kAll : 1];
-    const int wave = threadIdx.x / kWave % kWaves, of = threadIdx.x / kWave / kWaves;
-    const int64_t first = (wave * kWave + threadIdx.x % kWave) * kEach;
+    const int thread_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = thread_wave % kWaves, of = thread_wave / kWaves;
+    const int cols = (int)a.cols, first = wave * kStride + threadIdx.x % kWave * kEach;
     const float by = 1.f / (float)a.cols;
-    float dw[kSteps][kEach] = {}, db[kSteps][kEach] = {};
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + of; row < a.rows; row += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    float dw[kSteps][kEach] = {}, db[kSteps][kEach] = {}, w[kSteps][kEach];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        if (a.weight) widen8(load_raw(a.weight, first + i * kAll, cols), w[i]);
+        else
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) w[i][j] = 1.f;
+    }
+    auto load = [&](int64_t row) {
+        RawRow<D, T, kSteps> r;
         const D *dy = (const D *)a.dy + row * a.lddy;
         const T *x = (const T *)a.x + row * a.ldx;
-        Raw<D> rd[kSteps];
-        Raw<T> rx[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            rd[i] = load_raw(dy, first + i * kAll, a.cols);
-            rx[i] = load_raw(x, first + i * kAll, a.cols);
+            const int c = first + i * kAll;
+            r.dy[i] = load_raw(dy, c, cols);
+            r.x[i] = load_raw(x, c, cols);
+            if constexpr (kFp8) r.scale[i] = c < cols ? a.x_scales.p[c / kBlock * a.x_scales.ld + row] : 0.f;
         }
-        const float r = a.rstd[row];
-        const float m = sizeof(T) == 1 ? 0.f : a.mean[row];
+        r.rstd = a.rstd[row];
+        r.mean = kFp8 ? 0.f : a.mean[row];
+        return r;
+    };
+    int turn = 0;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + of;
+    RawRow<D, T, kSteps> next;
+    if (row < a.rows) next = load(row);
+    for (; row < a.rows; row += step, turn ^= 1) {
+        const RawRow<D, T, kSteps> now = next;
+        if (row + step < a.rows) next = load(row + step); // on its way while this one is worked on
         float g[kSteps][kEach], n[kSteps][kEach];
         float2 sums = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const int64_t c = first + i * kAll;
-            widen8(rd[i], g[i]);
-            widen8(rx[i], n[i]);
-            if constexpr (sizeof(T) == 1) {
-                const float s = c < a.cols ? a.x_scales.p[c / kBlock * a.x_scales.ld + row] : 0.f;
+            const int c = first + i * kAll;
+            widen8(now.dy[i], g[i]);
+            widen8(now.x[i], n[i]);
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) n[i][j] *= s;
-            } else {
+            for (int j = 0; j < kEach; ++j) n[i][j] = kFp8 ? n[i][j] * now.scale[i] : (n[i][j] - now.mean) * now.rstd;
+            if (!kFp8 && c + kEach > cols) {
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) n[i][j] = c + j < a.cols ? (n[i][j] - m) * r : 0.f;
+                for (int j = 0; j < kEach; ++j)
+                    if (c + j >= cols) n[i][j] = 0.f;
             }
-            float w[kEach];
-            if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 dw[i][j] = fmaf(g[i][j], n[i][j], dw[i][j]);
                 db[i][j] += g[i][j];
-                if (a.weight) g[i][j] *= w[j];
+                g[i][j] *= w[i][j];
                 sums.x += g[i][j];
                 sums.y = fmaf(g[i][j], n[i][j], sums.y);
             }
@@ -103,12 +130,12 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back(NormBackArgs a)
         const float c1 = sums.x * by, c2 = sums.y * by;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const int64_t c = first + i * kAll;
-            if (c >= a.cols) break;
+            const int c = first + i * kAll;
+            if (c >= cols) break;
             float d[kEach];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) d[j] = r * (g[i][j] - c1 - n[i][j] * c2);
-            store8((D *)a.dx + row * a.lddx, sizeof(D) == 4 ? EB_F32 : std::is_same_v<D, Bf16> ? EB_BF16 : EB_F16, c, a.cols, d);
+            for (int j = 0; j < kEach; ++j) d[j] = now.rstd * (g[i][j] - c1 - n[i][j] * c2);
+            store8((D *)a.dx + row * a.lddx, kTypeOf<D>, c, cols, d);
         }
     }
     if (!a.partial) return;
@@ -139,16 +166,16 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back(NormBackArgs a)
     float *to = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const int64_t c = first + i * kAll;
-        if (c >= a.cols) break;
-        store8(to, EB_F32, c, a.cols, dw[i]);
-        store8(to + a.cols, EB_F32, c, a.cols, db[i]);
+        const int c = first + i * kAll;
+        if (c >= cols) break;
+        store8(to, EB_F32, c, cols, dw[i]);
+        store8(to + a.cols, EB_F32, c, cols, db[i]);
     }
 }
 
 // Rows that registers do not hold: dy and x are read twice for dx,
 template <typename D, typename T>
-__device__ __forceinline__ void long_values(const NormBackArgs &a, int64_t row, int64_t c, float r, float m, float *d, float *n)
+__device__ __forceinline__ void long_values(const NormBackArgs &a, int64_t row, int c, float r, float m, float *d, float *n)
 {
     widen8(load_raw((const D *)a.dy + row * a.lddy, c, a.cols), d);
     widen8(load_raw((const T *)a.x + row * a.ldx, c, a.cols), n);
@@ -166,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_long(NormBackArgs
     const float r = a.rstd[row], m = sizeof(T) == 1 ? 0.f : a.mean[row];
     float2 sums = {0.f, 0.f};
     float d[kEach], n[kEach], w[kEach];
-    for (int64_t c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
+    for (int c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
         long_values<D, T>(a, row, c, r, m, d, n);
         if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
 #pragma unroll
@@ -178,12 +205,12 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_long(NormBackArgs
     }
     sums = sum_row<kWaves>(sums, shared, threadIdx.x / kWave);
     const float c1 = sums.x / (float)a.cols, c2 = sums.y / (float)a.cols;
-    for (int64_t c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
+    for (int c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
         long_values<D, T>(a, row, c, r, m, d, n);
         if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) d[j] = r * ((a.weight ? d[j] * w[j] : d[j]) - c1 - n[j] * c2);
-        store8((D *)a.dx + row * a.lddx, sizeof(D) == 4 ? EB_F32 : std::is_same_v<D, Bf16> ? EB_BF16 : EB_F16, c, a.cols, d);
+        store8((D *)a.dx + row * a.lddx, kTypeOf<D>, c, a.cols, d);
     }
 }
 
@@ -193,7 +220,8 @@ template <typename D, typename T>
 __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_columns(NormBackArgs a)
 {
     const int64_t strips = (a.cols + kThreads * kEach - 1) / (kThreads * kEach);
-    const int64_t c = (blockIdx.x % strips * kThreads + threadIdx.x) * kEach, part = blockIdx.x / strips, parts = gridDim.x / strips;
+    const int c = (int)(blockIdx.x % strips * kThreads + threadIdx.x) * kEach;
+    const int64_t part = blockIdx.x / strips, parts = gridDim.x / strips;
     if (c >= a.cols) return;
     float dw[kEach] = {}, db[kEach] = {};
     for (int64_t row = part; row < a.rows; row += parts) {
@@ -210,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_columns(NormBackA
     store8(to + a.cols, EB_F32, c, a.cols, db);
 }
 
-// The workgroups' sums added: 64 columns of dweight and dbias side by side, four
-// waves a share of the workgroups each.
+// The workgroups' sums added: 64 columns of dweight and dbias side by side, 16 waves a
+// share of the workgroups each.
 struct JoinArgs {
     const float *partial;
     float *dweight, *dbias;
@@ -219,21 +247,24 @@ struct JoinArgs {
     int32_t parts;
 };
 
-__global__ __launch_bounds__(kThreads) void eb_layer_norm_join(JoinArgs a)
+constexpr int kJoinThreads = 1024;
+
+__global__ __launch_bounds__(kJoinThreads) void eb_layer_norm_join(JoinArgs a)
 {
-    __shared__ float shared[kThreads];
+    __shared__ float shared[kJoinThreads];
     const int64_t c = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;
-    const int wave = threadIdx.x / kWave, waves = kThreads / kWave;
+    const int wave = threadIdx.x / kWave;
+    constexpr int kWaves = kJoinThreads / kWave;
     float sum = 0.f;
     if (c < 2 * a.cols) {
 #pragma unroll 8
-        for (int p = wave; p < a.parts; p += waves) sum += a.partial[(int64_t)p * 2 * a.cols + c];
+        for (int p = wave; p < a.parts; p += kWaves) sum += a.partial[(int64_t)p * 2 * a.cols + c];
     }
     shared[threadIdx.x] = sum;
     __syncthreads();
     if (wave > 0 || c >= 2 * a.cols) return;
 #pragma unroll
-    for (int i = 1; i < waves; ++i) sum += shared[i * kWave + threadIdx.x];
+    for (int i = 1; i < kWaves; ++i) sum += shared[i * kWave + threadIdx.x];
     if (c < a.cols) {
         if (a.dweight) a.dweight[c] = sum;
     } else if (a.dbias) {
@@ -241,12 +272,7 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_join(JoinArgs a)
     }
 }
 
-struct Plan {
-    void *kernel;  // NULL: the kernels for long rows
-    int64_t grid;  // workgroups that add up dweight and dbias
-};
-
-constexpr int64_t kMostHeld = 8 * 4 * kStride; // columns of a row in registers
+constexpr int64_t kMostHeld = 2 * 8 * kStride; // columns of a row in registers
 
 int64_t groups_of(int64_t rows, int64_t cols)
 {
@@ -254,25 +280,32 @@ int64_t groups_of(int64_t rows, int64_t cols)
         const int64_t strips = (cols + kThreads * kEach - 1) / (kThreads * kEach);
         return std::min<int64_t>(std::max<int64_t>(1, kMostGroups / strips), (rows + 7) / 8);
     }
-    const int64_t held = cols > 4 * kStride ? 1 : 4;
-    return std::min<int64_t>(kMostGroups, (rows + held - 1) / held);
+    const int64_t held = cols > 2 * kStride ? 1 : 4;
+    return std::min<int64_t>(cols > 8 * kStride ? 384 : kMostGroups, (rows + held - 1) / held);
 }
 
+struct RowPlan {
+    void *kernel;
+    int threads;
+};
+
 template <typename D, typename T>
-void *kernel_of(int64_t cols)
+RowPlan plan_of(int64_t cols)
 {
-    if (cols > 4 * 4 * kStride) return (void *)eb_layer_norm_back<D, T, 8, 4>;
-    if (cols > 2 * 4 * kStride) return (void *)eb_layer_norm_back<D, T, 4, 4>;
-    if (cols > 4 * kStride) return (void *)eb_layer_norm_back<D, T, 2, 4>;
-    if (cols > 2 * kStride) return (void *)eb_layer_norm_back<D, T, 4, 1>;
-    if (cols > kStride) return (void *)eb_layer_norm_back<D, T, 2, 1>;
-    return (void *)eb_layer_norm_back<D, T, 1, 1>;
+    if (cols > 2 * 4 * kStride) return {(void *)eb_layer_norm_back<D, T, 2, 8>, 512};
+    if (cols > 4 * kStride) return {(void *)eb_layer_norm_back<D, T, 2, 4>, kThreads};
+    if (cols > 2 * kStride) return {(void *)eb_layer_norm_back<D, T, 1, 4>, kThreads};
+    if (cols > kStride) return {(void *)eb_layer_norm_back<D, T, 2, 1>, kThreads};
+    return {(void *)eb_layer_norm_back<D, T, 1, 1>, kThreads};
 }
 
 template <typename D, typename T>
 int run(const char *who, NormBackArgs &a, int64_t groups, void *stream)
 {
-    if (a.cols <= kMostHeld) return launch(who, kernel_of<D, T>(a.cols), groups, kThreads, &a, stream);
+    if (a.cols <= kMostHeld) {
+        const RowPlan plan = plan_of<D, T>(a.cols);
+        return launch(who, plan.kernel, groups, plan.threads, &a, stream);
+    }
     if (int rc = launch(who, (void *)eb_layer_norm_back_long<D, T>, a.rows, kThreads, &a, stream)) return rc;
     if (!a.partial) return EB_OK;
     const int64_t strips = (a.cols + kThreads * kEach - 1) / (kThreads * kEach);
@@ -335,7 +368,7 @@ int back_impl(const char *who, int64_t rows, int64_t cols, const void *dy, int32
         return EB_OK;
     }
     JoinArgs j{(const float *)workspace, dweight, dbias, cols, (int32_t)groups};
-    return launch(who, (void *)eb_layer_norm_join, (2 * cols + kWave - 1) / kWave, kThreads, &j, stream);
+    return launch(who, (void *)eb_layer_norm_join, (2 * cols + kWave - 1) / kWave, kJoinThreads, &j, stream);
 }
 
 int workspace_impl(const char *who, int64_t rows, int64_t cols, size_t *bytes)

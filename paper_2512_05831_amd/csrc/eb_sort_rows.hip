@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
     const T *y = (const T *)a.y;
     const int32_t *slots = a.slots + t * a.K;
     const float *weights = a.weights ? a.weights + t * a.K : nullptr;
-    for (int64_t c = threadIdx.x % kRowLanes * kEach; c < a.cols; c += kRowLanes * kEach) {
+    for (int c = threadIdx.x % kRowLanes * kEach; c < a.cols; c += kRowLanes * kEach) {
         float sum[kEach] = {};
         for (int k0 = 0; k0 < a.K; k0 += kAhead) {
             Raw<T> raw[kAhead];
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
                 for (int j = 0; j < kEach; ++j) sum[j] = fmaf(w[i], f[j], sum[j]);
             }
         }
-        store_out(a.out, t, c, a.cols, sum, 0);
+        store_out(a.out, t, c, (int)a.cols, sum);
     }
 }
 
@@ -120,20 +120,21 @@ template <typename D, typename T, int kRowLanes, int kSteps>
 __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
 {
     constexpr int kRows = kThreads / kRowLanes;
-    constexpr int64_t kStride = kRowLanes * kEach, kPart = kStride * kSteps;
+    constexpr int kStride = kRowLanes * kEach, kPart = kStride * kSteps;
+    const int cols = (int)a.cols;
     const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kRowLanes;
     if (t >= a.N) return;
     const int lane = threadIdx.x % kRowLanes;
     const D *dout = (const D *)a.dout + t * a.lddout;
     const bool fp8 = a.out.type == EB_FP8;
     float kept = 0.f;
-    for (int64_t part = 0; part < a.cols; part += kPart) {
-        const int64_t first = part + lane * kEach;
+    for (int part = 0; part < cols; part += kPart) {
+        const int first = part + lane * kEach;
         Raw<D> raw[kSteps];
         float d[kSteps][kEach];
         int most[kSteps];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(dout, first + i * kStride, a.cols);
+        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(dout, first + i * kStride, cols);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             widen8(raw[i], d[i]);
@@ -142,14 +143,14 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
         for (int k = 0; k < a.K; ++k) {
             const int64_t s = a.slots[t * a.K + k];
             if (s < 0 || s >= a.y_rows) {
-                if (a.dweights && part == 0 && kPart >= a.cols && lane == 0) a.dweights[t * a.K + k] = 0.f;
+                if (a.dweights && part == 0 && kPart >= cols && lane == 0) a.dweights[t * a.K + k] = 0.f;
                 continue;
             }
             if (a.dweights) {
                 const T *y = (const T *)a.y + s * a.ldy;
                 Raw<T> other[kSteps];
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) other[i] = load_raw(y, first + i * kStride, a.cols);
+                for (int i = 0; i < kSteps; ++i) other[i] = load_raw(y, first + i * kStride, cols);
                 float dot = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
                     for (int j = 0; j < kEach; ++j) dot = fmaf(d[i][j], f[j], dot);
                 }
                 dot = sum_lanes<kRowLanes>(dot);
-                if (kPart >= a.cols) {
+                if (kPart >= cols) {
                     if (lane == 0) a.dweights[t * a.K + k] = dot;
                 } else if (lane == k) { // only waves of one token have several parts
                     kept += dot;
@@ -174,12 +175,13 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
                     for (int j = 0; j < kEach; ++j) f[j] = w * d[i][j];
                     // A product rounds as its factor orders: the largest is the largest's.
                     const int scaled = fp8 ? magnitude(w * __int_as_float(most[i])) : 0;
-                    store_out(a.out, s, first + i * kStride, a.cols, f, scaled);
+                    if (fp8) store_fp8(a.out, s, first + i * kStride, cols, f, to_fp8(scaled), scaled);
+                    else store_out(a.out, s, first + i * kStride, cols, f);
                 }
             }
         }
     }
-    if (kRowLanes == kWave && a.dweights && kPart < a.cols && lane < a.K) a.dweights[t * a.K + lane] = kept;
+    if (kRowLanes == kWave && a.dweights && kPart < cols && lane < a.K) a.dweights[t * a.K + lane] = kept;
 }
 
 // --------------------------------------------------------------------- host

@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <limits>
+#include <type_traits>
 
 #include "../../include/eb.h"
 #include "../../include/eb_experts.h"
@@ -39,29 +40,33 @@ struct Raw {
     T v[kEach];
 };
 
-// Those from column c of a row; zeros outside [0, cols).
+// Those from column c of a row on, which has columns [0, cols); zeros outside.
 template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *row, int64_t c, int64_t cols)
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int cols)
 {
     Raw<T> r;
     if (c >= 0 && c + kEach <= cols) {
+        const char *at = (const char *)row + (int64_t)c * (int)sizeof(T);
         if constexpr (sizeof(T) == 1) {
-            const i32x2_any w = *(const i32x2_any *)(row + c);
+            const i32x2_any w = *(const i32x2_any *)at;
             __builtin_memcpy(&r, &w, 8);
         } else {
 #pragma unroll
             for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const i32x4_any w = *(const i32x4_any *)((const char *)(row + c) + 16 * i);
+                const i32x4_any w = *(const i32x4_any *)(at + 16 * i);
                 __builtin_memcpy((char *)&r + 16 * i, &w, 16);
             }
         }
     } else {
-        __builtin_memset(&r, 0, sizeof(r));
+        using Bits = std::conditional_t<sizeof(T) == 1, uint8_t, std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>>;
+        constexpr int kOf = 4 / (int)sizeof(T); // values of a word
+        uint32_t w[kEach / kOf] = {};
         if (c < cols && c + kEach > 0) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
-                if (c + i >= 0 && c + i < cols) r.v[i] = row[c + i];
+                if (c + i >= 0 && c + i < cols) w[i / kOf] |= (uint32_t)((const Bits *)row)[c + i] << i % kOf * 8 * (int)sizeof(T);
         }
+        __builtin_memcpy(&r, w, sizeof(r));
     }
     return r;
 }
@@ -74,10 +79,11 @@ __device__ __forceinline__ void widen8(const Raw<T> &r, float *f)
         __builtin_memcpy(w, &r, 8);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            f[4 * i + 0] = __builtin_amdgcn_cvt_f32_fp8(w[i], 0);
-            f[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(w[i], 1);
-            f[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(w[i], 2);
-            f[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(w[i], 3);
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+            f[4 * i + 0] = lo[0];
+            f[4 * i + 1] = lo[1];
+            f[4 * i + 2] = hi[0];
+            f[4 * i + 3] = hi[1];
         }
     } else {
 #pragma unroll
@@ -91,33 +97,24 @@ struct Scales {
     int64_t ld;
 };
 
-// Columns c .. c + 7 of a row of an 8-bit matrix lie in one block, or in two.
-struct TwoScales {
-    float first, second;
-    int border; // values from this one on have the second
-};
-
-__device__ __forceinline__ TwoScales scales_at(const Scales &s, int64_t row, int64_t c, int64_t cols)
+// Columns c .. c + 7 of a row of an 8-bit matrix of `cols` columns, times their
+// scales: they lie in one block, or in two where c is no multiple of 8.
+__device__ __forceinline__ void scale8(float *f, const Scales &s, int64_t row, int c, int cols)
 {
-    TwoScales t{0.f, 0.f, kEach};
-    const int64_t lo = c > 0 ? c : 0, hi = c + kEach - 1 < cols - 1 ? c + kEach - 1 : cols - 1;
-    if (lo > hi) return t;
-    const int64_t b = lo / kBlock;
-    t.first = s.p[b * s.ld + row];
-    t.second = t.first;
-    if (hi / kBlock != b) {
-        t.second = s.p[(b + 1) * s.ld + row];
-        t.border = (int)((b + 1) * kBlock - c);
-    }
-    return t;
-}
-
-__device__ __forceinline__ void scale8(float *f, const TwoScales &t)
-{
+    const int lo = max(c, 0), hi = min(c + kEach, cols) - 1, b = lo / kBlock;
+    if (lo > hi) return; // zeros
+    const float first = s.p[b * s.ld + row];
+    if (hi / kBlock == b) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) f[i] *= i < t.border ? t.first : t.second;
+        for (int i = 0; i < kEach; ++i) f[i] *= first;
+    } else {
+        const float second = s.p[(b + 1) * s.ld + row];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) f[i] *= c + i < (b + 1) * kBlock ? first : second;
+    }
 }
 
+// The bits of the largest magnitude.
 __device__ __forceinline__ int most8(const float *f)
 {
     int m = 0;
@@ -126,15 +123,14 @@ __device__ __forceinline__ int most8(const float *f)
     return m;
 }
 
-// Eight values as e4m3 under the scale of a block whose largest magnitude has the
-// bits `most`; `left`: how many of them there are (the others are zeros).
-__device__ __forceinline__ int2 eight_bits(const float *f, int most, int64_t left)
+// Eight values times `by` as e4m3; NaNs where a block's scale is one. `left`: how many
+// of them there are (the others are zeros).
+__device__ __forceinline__ int2 eight_bits(const float *f, float by, bool nan, int left)
 {
-    const float by = kMostFp8 / fmaxf(__int_as_float(most), kMostFp8 * kLeastScale);
     int2 v;
     v.x = pack_fp8(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
     v.y = pack_fp8(f[4] * by, f[5] * by, f[6] * by, f[7] * by);
-    if (most >= 0x7F800000) { // an infinity or a NaN: only NaNs
+    if (nan) {
         const uint64_t all = 0x7F7F7F7F7F7F7F7Full, some = left >= 8 ? all : left <= 0 ? 0 : all >> 8 * (8 - left);
         v.x = (int)some;
         v.y = (int)(some >> 32);
@@ -160,7 +156,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 
 // Eight fp32 values to columns c .. c + 7 of a row in a floating-point type (a
 // code of eb.h), each rounded once to nearest even; those past cols are left out.
-__device__ __forceinline__ void store8(void *row, int type, int64_t c, int64_t cols, const float *f)
+__device__ __forceinline__ void store8(void *row, int type, int c, int cols, const float *f)
 {
     if (type == EB_F32) {
         float *to = (float *)row + c;
@@ -177,9 +173,13 @@ __device__ __forceinline__ void store8(void *row, int type, int64_t c, int64_t c
         return;
     }
     uint32_t w[4];
+    if (type == EB_F16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i] = type == EB_F16 ? pack16((_Float16)f[2 * i], (_Float16)f[2 * i + 1]) : pack_bf16(f[2 * i], f[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) w[i] = pack16((_Float16)f[2 * i], (_Float16)f[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+    }
     uint16_t *to = (uint16_t *)row + c;
     if (c + kEach <= cols) {
         const i32x4_any v = {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
@@ -199,14 +199,24 @@ struct Out {
     int32_t type;
 };
 
-// Columns c .. c + 7 of a row; in 8 bits the 16 lanes of a block call together
-// (`most`: bits of the block's largest magnitude), the row padded to 16 bytes.
-__device__ __forceinline__ void store_out(const Out &o, int64_t row, int64_t c, int64_t cols, const float *f, int most)
+// Columns c .. c + 7 of a row in 8 bits, the row padded to 16 bytes: values that are
+// `by` to be multiplied with, under a scale for the largest magnitude `most` (bits).
+__device__ __forceinline__ void store_fp8(const Out &o, int64_t row, int c, int cols, const float *f, float by, int most)
 {
-    if (c >= ((cols + 15) & ~(int64_t)15)) return;
+    if (c >= ((cols + 15) & ~15)) return;
+    *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits(f, by, most >= 0x7F800000, cols - c);
+    if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = block_scale(most);
+}
+
+// What brings a block's values to e4m3.
+__device__ __forceinline__ float to_fp8(int most) { return kMostFp8 / fmaxf(__int_as_float(most), kMostFp8 * kLeastScale); }
+
+// Columns c .. c + 7 of a row; in 8 bits the 16 lanes of a block call together.
+__device__ __forceinline__ void store_out(const Out &o, int64_t row, int c, int cols, const float *f)
+{
     if (o.type == EB_FP8) {
-        *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits(f, most, cols - c);
-        if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = block_scale(most);
+        const int most = max_lanes<kLanes>(most8(f));
+        store_fp8(o, row, c, cols, f, to_fp8(most), most);
     } else if (c < cols) {
         store8((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
     }
