@@ -42,20 +42,20 @@ __device__ __forceinline__ float sigmoid(float g)
 }
 
 // Columns c .. c + 7 of v that lie in [lo, hi); zeros for the others.
-template <typename T>
+template <bool kRagged, typename T>
 __device__ __forceinline__ Raw<T> load_v(const ActArgs &a, int64_t row, int c, int lo, int hi)
 {
-    return load_raw((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
+    return load_raw<kRagged>((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
 }
 
-template <typename T>
+template <bool kRagged, typename T>
 __device__ __forceinline__ void widen_v(const ActArgs &a, int64_t row, int c, int hi, const Raw<T> &r, float *f)
 {
     widen8(r, f);
-    if constexpr (sizeof(T) == 1) scale8(f, a.v_scales, row, c, hi);
+    if constexpr (sizeof(T) == 1) scale8<kRagged>(f, a.v_scales, row, c, hi);
 }
 
-template <typename T>
+template <typename T, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_activate(ActArgs a)
 {
     const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
@@ -67,20 +67,20 @@ __global__ __launch_bounds__(kThreads) void eb_activate(ActArgs a)
         const int c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
         float g[kEach], h[kEach];
-        const Raw<T> first = load_v<T>(a, row, c, 0, cols);
+        const Raw<T> first = load_v<kRagged, T>(a, row, c, 0, cols);
         if (a.gate) {
-            const Raw<T> second = load_v<T>(a, row, cols + c, cols, width);
+            const Raw<T> second = load_v<kRagged, T>(a, row, cols + c, cols, width);
             float u[kEach];
-            widen_v(a, row, c, cols, first, g);
-            widen_v(a, row, cols + c, width, second, u);
+            widen_v<kRagged>(a, row, c, cols, first, g);
+            widen_v<kRagged>(a, row, cols + c, width, second, u);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
         } else {
-            widen_v(a, row, c, cols, first, g);
+            widen_v<kRagged>(a, row, c, cols, first, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] > 0.f ? g[i] : g[i] == g[i] ? 0.f : g[i];
         }
-        store_out(a.out, row, c, cols, h);
+        store_out<kRagged>(a.out, row, c, cols, h);
     }
 }
 
@@ -93,7 +93,7 @@ __device__ __forceinline__ float2 d_gate(float dh, float g, float u)
 
 // dg and du by the lane that has both g and u: floating-point outputs, and 8-bit
 // ones whose blocks do not lie across the border between dg and du.
-template <typename D, typename T>
+template <typename D, typename T, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
 {
     const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
@@ -105,21 +105,21 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         const int c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
         float dh[kEach], g[kEach], d[kEach];
-        const Raw<D> of_h = load_raw((const D *)a.dh + row * a.lddh, c, cols);
-        const Raw<T> first = load_v<T>(a, row, c, 0, cols);
+        const Raw<D> of_h = load_raw<kRagged>((const D *)a.dh + row * a.lddh, c, cols);
+        const Raw<T> first = load_v<kRagged, T>(a, row, c, 0, cols);
         if (!a.gate) {
             widen8(of_h, dh);
-            widen_v(a, row, c, cols, first, g);
+            widen_v<kRagged>(a, row, c, cols, first, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) d[i] = g[i] > 0.f ? dh[i] : 0.f;
-            store_out(a.out, row, c, cols, d);
+            store_out<kRagged>(a.out, row, c, cols, d);
             continue;
         }
-        const Raw<T> second = load_v<T>(a, row, cols + c, cols, width);
+        const Raw<T> second = load_v<kRagged, T>(a, row, cols + c, cols, width);
         float u[kEach], e[kEach];
         widen8(of_h, dh);
-        widen_v(a, row, c, cols, first, g);
-        widen_v(a, row, cols + c, width, second, u);
+        widen_v<kRagged>(a, row, c, cols, first, g);
+        widen_v<kRagged>(a, row, cols + c, width, second, u);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float2 v = d_gate(dh[i], g[i], u[i]);
@@ -133,8 +133,8 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         } else {
             of_u.p = (char *)a.out.p + cols * (int64_t)(a.out.type == EB_F32 ? 4 : 2);
         }
-        store_out(a.out, row, c, cols, d);
-        store_out(of_u, row, c, cols, e);
+        store_out<kRagged>(a.out, row, c, cols, d);
+        store_out<kRagged>(of_u, row, c, cols, e);
     }
 }
 
@@ -153,13 +153,13 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
         if (b0 + s >= a.blocks) return;
         float d[kEach] = {}, dh[kEach], g[kEach], u[kEach];
         auto take = [&](int c, bool first) { // columns c on of dg, or of du
-            const Raw<D> of_h = load_raw((const D *)a.dh + row * a.lddh, c, cols);
-            const Raw<T> of_g = load_v<T>(a, row, c, 0, cols), of_u = load_v<T>(a, row, cols + c, cols, width);
+            const Raw<D> of_h = load_raw<true>((const D *)a.dh + row * a.lddh, c, cols);
+            const Raw<T> of_g = load_v<true, T>(a, row, c, 0, cols), of_u = load_v<true, T>(a, row, cols + c, cols, width);
             widen8(of_h, dh);
-            widen_v(a, row, c, cols, of_g, g);
+            widen_v<true>(a, row, c, cols, of_g, g);
             // (Of du's first chunk some columns lie before u, and before dh and g: zeros.)
             widen8(of_u, u);
-            if (sizeof(T) == 1 && first) scale8(u, a.v_scales, row, cols + c, width);
+            if (sizeof(T) == 1 && first) scale8<true>(u, a.v_scales, row, cols + c, width);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 if (c + i < 0 || c + i >= cols) continue;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
         };
         if (at < cols) take(at, true);
         if (at + kEach > cols) take(at - cols, false);
-        store_out(a.out, row, at, width, d);
+        store_out<true>(a.out, row, at, width, d);
     }
 }
 
@@ -189,6 +189,12 @@ int launch_rows(const char *who, void *kernel, ActArgs &a, void *stream)
     return launch(who, kernel, lines > kMax32 / strips ? kMax32 : lines * strips, kThreads, &a, stream);
 }
 
+template <typename T>
+void *act_kernel(bool ragged)
+{
+    return ragged ? (void *)eb_activate<T, true> : (void *)eb_activate<T, false>;
+}
+
 int act_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const void *v, int32_t v_type, int64_t ldv, const float *v_scales,
              int64_t ldvs, int32_t out_type, void *h, int64_t ldh, float *h_scales, int64_t ldhs, void *stream)
 {
@@ -206,20 +212,28 @@ int act_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const voi
     a.cols = cols;
     a.ldv = ldv;
     a.blocks = (cols + kBlock - 1) / kBlock;
-    void *kernel = v_type == EB_F32   ? (void *)eb_activate<float>
-                   : v_type == EB_F16 ? (void *)eb_activate<_Float16>
-                   : v_type == EB_FP8 ? (void *)eb_activate<Fp8>
-                                      : (void *)eb_activate<Bf16>;
+    const bool ragged = cols % kEach != 0;
+    void *kernel = v_type == EB_F32   ? act_kernel<float>(ragged)
+                   : v_type == EB_F16 ? act_kernel<_Float16>(ragged)
+                   : v_type == EB_FP8 ? act_kernel<Fp8>(ragged)
+                                      : act_kernel<Bf16>(ragged);
     return launch_rows(who, kernel, a, stream);
 }
 
-template <typename D>
-void *back_kernel(int32_t v_type, bool across)
+template <typename D, typename T>
+void *back_kernel(bool across, bool ragged)
 {
-    if (v_type == EB_F32) return across ? (void *)eb_activate_back_across<D, float> : (void *)eb_activate_back<D, float>;
-    if (v_type == EB_F16) return across ? (void *)eb_activate_back_across<D, _Float16> : (void *)eb_activate_back<D, _Float16>;
-    if (v_type == EB_FP8) return across ? (void *)eb_activate_back_across<D, Fp8> : (void *)eb_activate_back<D, Fp8>;
-    return across ? (void *)eb_activate_back_across<D, Bf16> : (void *)eb_activate_back<D, Bf16>;
+    if (across) return (void *)eb_activate_back_across<D, T>;
+    return ragged ? (void *)eb_activate_back<D, T, true> : (void *)eb_activate_back<D, T, false>;
+}
+
+template <typename D>
+void *back_kernel(int32_t v_type, bool across, bool ragged)
+{
+    if (v_type == EB_F32) return back_kernel<D, float>(across, ragged);
+    if (v_type == EB_F16) return back_kernel<D, _Float16>(across, ragged);
+    if (v_type == EB_FP8) return back_kernel<D, Fp8>(across, ragged);
+    return back_kernel<D, Bf16>(across, ragged);
 }
 
 int back_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const void *dh, int32_t dh_type, int64_t lddh, const void *v,
@@ -245,9 +259,9 @@ int back_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const vo
     a.lddh = lddh;
     const bool across = a.gate && out_type == EB_FP8 && cols % kBlock != 0;
     a.blocks = ((across ? a.width : cols) + kBlock - 1) / kBlock;
-    void *kernel = dh_type == EB_F32   ? back_kernel<float>(v_type, across)
-                   : dh_type == EB_F16 ? back_kernel<_Float16>(v_type, across)
-                                       : back_kernel<Bf16>(v_type, across);
+    void *kernel = dh_type == EB_F32   ? back_kernel<float>(v_type, across, cols % kEach != 0)
+                   : dh_type == EB_F16 ? back_kernel<_Float16>(v_type, across, cols % kEach != 0)
+                                       : back_kernel<Bf16>(v_type, across, cols % kEach != 0);
     return launch_rows(who, kernel, a, stream);
 }
 

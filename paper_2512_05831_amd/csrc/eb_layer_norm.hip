@@ -44,13 +44,14 @@ __device__ __forceinline__ float sum_row(float v, float *shared, int wave)
 }
 
 // The outputs of columns c .. c + 7, of which d is x - mean (zeros past cols).
+template <bool kRagged>
 __device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, const float *d, float rstd)
 {
     const int cols = (int)a.cols;
     if (c >= ((cols + kBlock - 1) & ~(kBlock - 1))) return; // whole blocks: their 16 lanes stay together
     float n[kEach], y[kEach], w[kEach], b[kEach];
-    if (a.weight) widen8(load_raw(a.weight, c, cols), w);
-    if (a.bias) widen8(load_raw(a.bias, c, cols), b);
+    if (a.weight) widen8(load_raw<kRagged>(a.weight, c, cols), w);
+    if (a.bias) widen8(load_raw<kRagged>(a.bias, c, cols), b);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) n[i] = d[i] * rstd;
     if (a.kept.p) {
@@ -64,11 +65,11 @@ __device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, co
         y[i] = a.weight ? n[i] * w[i] : n[i];
         if (a.bias) y[i] += b[i];
     }
-    store_out(a.y, row, c, cols, y);
+    store_out<kRagged>(a.y, row, c, cols, y);
 }
 
 // kSteps * 512 columns a wave; kLoop: any number of them, read again for each sum.
-template <typename T, int kSteps, int kWaves, bool kLoop>
+template <typename T, int kSteps, int kWaves, bool kLoop, bool kRagged>
 __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_rows(NormArgs a)
 {
     __shared__ float shared[kWaves];
@@ -82,7 +83,10 @@ __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_r
     auto centred = [&](int c, float *f, float mean) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) f[i] -= mean;
-        if (c + kEach > cols) {
+        if (!kRagged) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) f[i] = c < cols ? f[i] : 0.f;
+        } else if (c + kEach > cols) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
                 if (c + i >= cols) f[i] = 0.f;
@@ -110,28 +114,28 @@ __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_r
         float f[kEach];
         const int blocks = (cols + kBlock - 1) & ~(kBlock - 1);
         for (int c = first; c < cols; c += kAll) {
-            widen8(load_raw(x, c, cols), f);
+            widen8(load_raw<kRagged>(x, c, cols), f);
             sum = add(f, sum);
         }
         const float mean = sum_row<kWaves>(sum, shared, wave) / of;
         for (int c = first; c < cols; c += kAll) {
-            widen8(load_raw(x, c, cols), f);
+            widen8(load_raw<kRagged>(x, c, cols), f);
             centred(c, f, mean);
             square = add_squares(f, square);
         }
         const float rstd = 1.f / sqrtf(sum_row<kWaves>(square, shared, wave) / of + a.eps);
         statistics(mean, rstd);
         for (int c = first; c < blocks; c += kAll) {
-            widen8(load_raw(x, c, cols), f);
+            widen8(load_raw<kRagged>(x, c, cols), f);
             centred(c, f, mean);
-            write8(a, row, c, f, rstd);
+            write8<kRagged>(a, row, c, f, rstd);
         }
     } else {
         float f[kSteps][kEach];
         {
             Raw<T> raw[kSteps];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(x, first + i * kAll, cols);
+            for (int i = 0; i < kSteps; ++i) raw[i] = load_raw<kRagged>(x, first + i * kAll, cols);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 widen8(raw[i], f[i]);
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_r
         statistics(mean, rstd);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            write8(a, row, first + i * kAll, f[i], rstd);
+            write8<kRagged>(a, row, first + i * kAll, f[i], rstd);
             __builtin_amdgcn_sched_barrier(0); // not all steps' weights at a time: registers
         }
     }
@@ -159,15 +163,22 @@ struct Plan {
     int rows; // of a workgroup
 };
 
+template <typename T, bool kRagged>
+Plan plan_of(int64_t rows, int64_t cols)
+{
+    if (cols > 8 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 1, 4, true, kRagged>, 1};
+    if (cols > 4 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 4, false, kRagged>, 1};
+    if (cols > 8 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 4, false, kRagged>, 1};
+    if (cols > 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 1, false, kRagged>, 4};
+    if (cols > 2 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 1, false, kRagged>, 4};
+    if (cols > kStride) return {(void *)eb_layer_norm_rows<T, 2, 1, false, kRagged>, 4};
+    return {(void *)eb_layer_norm_rows<T, 1, 1, false, kRagged>, 4};
+}
+
 template <typename T>
 Plan plan_of(int64_t rows, int64_t cols)
 {
-    if (cols > 8 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 1, 4, true>, 1};
-    if (cols > 8 * kStride) return {(void *)(cols > 4 * 4 * kStride ? eb_layer_norm_rows<T, 8, 4, false> : eb_layer_norm_rows<T, 4, 4, false>), 1};
-    if (cols > 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 1, false>, 4};
-    if (cols > 2 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 1, false>, 4};
-    if (cols > kStride) return {(void *)eb_layer_norm_rows<T, 2, 1, false>, 4};
-    return {(void *)eb_layer_norm_rows<T, 1, 1, false>, 4};
+    return cols % kEach ? plan_of<T, true>(rows, cols) : plan_of<T, false>(rows, cols);
 }
 
 int norm_impl(const char *who, int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx, const float *weight, const float *bias,

@@ -61,7 +61,7 @@ struct RawRow {
     float rstd, mean;
 };
 
-template <typename D, typename T, int kSteps, int kWaves>
+template <typename D, typename T, int kSteps, int kWaves, bool kRagged>
 __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_layer_norm_back(NormBackArgs a)
 {
     constexpr int kRows = kWaves > 4 ? 1 : kThreads / kWave / kWaves; // rows that a workgroup holds at a time
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
     float dw[kSteps][kEach] = {}, db[kSteps][kEach] = {}, w[kSteps][kEach];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        if (a.weight) widen8(load_raw(a.weight, first + i * kAll, cols), w[i]);
+        if (a.weight) widen8(load_raw<kRagged>(a.weight, first + i * kAll, cols), w[i]);
         else
 #pragma unroll
             for (int j = 0; j < kEach; ++j) w[i][j] = 1.f;
@@ -87,9 +87,9 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int c = first + i * kAll;
-            r.dy[i] = load_raw(dy, c, cols);
-            r.x[i] = load_raw(x, c, cols);
-            if constexpr (kFp8) r.scale[i] = c < cols ? a.x_scales.p[c / kBlock * a.x_scales.ld + row] : 0.f;
+            r.dy[i] = load_raw<kRagged>(dy, c, cols);
+            r.x[i] = load_raw<kRagged>(x, c, cols);
+            if constexpr (kFp8) r.scale[i] = a.x_scales.p[(c < cols ? c / kBlock : 0) * a.x_scales.ld + row];
         }
         r.rstd = a.rstd[row];
         r.mean = kFp8 ? 0.f : a.mean[row];
@@ -110,9 +110,13 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
             const int c = first + i * kAll;
             widen8(now.dy[i], g[i]);
             widen8(now.x[i], n[i]);
+            const float scale = kFp8 && c < cols ? now.scale[i] : 0.f;
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) n[i][j] = kFp8 ? n[i][j] * now.scale[i] : (n[i][j] - now.mean) * now.rstd;
-            if (!kFp8 && c + kEach > cols) {
+            for (int j = 0; j < kEach; ++j) n[i][j] = kFp8 ? n[i][j] * scale : (n[i][j] - now.mean) * now.rstd;
+            if (!kFp8 && !kRagged) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) n[i][j] = c < cols ? n[i][j] : 0.f;
+            } else if (!kFp8 && c + kEach > cols) {
 #pragma unroll
                 for (int j = 0; j < kEach; ++j)
                     if (c + j >= cols) n[i][j] = 0.f;
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
             float d[kEach];
 #pragma unroll
             for (int j = 0; j < kEach; ++j) d[j] = now.rstd * (g[i][j] - c1 - n[i][j] * c2);
-            store8((D *)a.dx + row * a.lddx, kTypeOf<D>, c, cols, d);
+            store8<kRagged>((D *)a.dx + row * a.lddx, kTypeOf<D>, c, cols, d);
         }
     }
     if (!a.partial) return;
@@ -168,8 +172,8 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
     for (int i = 0; i < kSteps; ++i) {
         const int c = first + i * kAll;
         if (c >= cols) break;
-        store8(to, EB_F32, c, cols, dw[i]);
-        store8(to + a.cols, EB_F32, c, cols, db[i]);
+        store8<kRagged>(to, EB_F32, c, cols, dw[i]);
+        store8<kRagged>(to + a.cols, EB_F32, c, cols, db[i]);
     }
 }
 
@@ -177,8 +181,8 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
 template <typename D, typename T>
 __device__ __forceinline__ void long_values(const NormBackArgs &a, int64_t row, int c, float r, float m, float *d, float *n)
 {
-    widen8(load_raw((const D *)a.dy + row * a.lddy, c, a.cols), d);
-    widen8(load_raw((const T *)a.x + row * a.ldx, c, a.cols), n);
+    widen8(load_raw<true>((const D *)a.dy + row * a.lddy, c, a.cols), d);
+    widen8(load_raw<true>((const T *)a.x + row * a.ldx, c, a.cols), n);
     const float s = sizeof(T) == 1 ? a.x_scales.p[c / kBlock * a.x_scales.ld + row] : 0.f;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) n[j] = sizeof(T) == 1 ? n[j] * s : c + j < a.cols ? (n[j] - m) * r : 0.f;
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_long(NormBackArgs
     float d[kEach], n[kEach], w[kEach];
     for (int c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
         long_values<D, T>(a, row, c, r, m, d, n);
-        if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
+        if (a.weight) widen8(load_raw<true>(a.weight, c, a.cols), w);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const float g = a.weight ? d[j] * w[j] : d[j];
@@ -207,10 +211,10 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_long(NormBackArgs
     const float c1 = sums.x / (float)a.cols, c2 = sums.y / (float)a.cols;
     for (int c = threadIdx.x * kEach; c < a.cols; c += kThreads * kEach) {
         long_values<D, T>(a, row, c, r, m, d, n);
-        if (a.weight) widen8(load_raw(a.weight, c, a.cols), w);
+        if (a.weight) widen8(load_raw<true>(a.weight, c, a.cols), w);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) d[j] = r * ((a.weight ? d[j] * w[j] : d[j]) - c1 - n[j] * c2);
-        store8((D *)a.dx + row * a.lddx, kTypeOf<D>, c, a.cols, d);
+        store8<true>((D *)a.dx + row * a.lddx, kTypeOf<D>, c, a.cols, d);
     }
 }
 
@@ -234,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void eb_layer_norm_back_columns(NormBackA
         }
     }
     float *to = a.partial + part * 2 * a.cols;
-    store8(to, EB_F32, c, a.cols, dw);
-    store8(to + a.cols, EB_F32, c, a.cols, db);
+    store8<true>(to, EB_F32, c, a.cols, dw);
+    store8<true>(to + a.cols, EB_F32, c, a.cols, db);
 }
 
 // The workgroups' sums added: 64 columns of dweight and dbias side by side, 16 waves a
@@ -292,11 +296,12 @@ struct RowPlan {
 template <typename D, typename T>
 RowPlan plan_of(int64_t cols)
 {
-    if (cols > 2 * 4 * kStride) return {(void *)eb_layer_norm_back<D, T, 2, 8>, 512};
-    if (cols > 4 * kStride) return {(void *)eb_layer_norm_back<D, T, 2, 4>, kThreads};
-    if (cols > 2 * kStride) return {(void *)eb_layer_norm_back<D, T, 1, 4>, kThreads};
-    if (cols > kStride) return {(void *)eb_layer_norm_back<D, T, 2, 1>, kThreads};
-    return {(void *)eb_layer_norm_back<D, T, 1, 1>, kThreads};
+    const bool ragged = cols % kEach != 0;
+    if (cols > 2 * 4 * kStride) return {ragged ? (void *)eb_layer_norm_back<D, T, 2, 8, true> : (void *)eb_layer_norm_back<D, T, 2, 8, false>, 512};
+    if (cols > 4 * kStride) return {ragged ? (void *)eb_layer_norm_back<D, T, 2, 4, true> : (void *)eb_layer_norm_back<D, T, 2, 4, false>, kThreads};
+    if (cols > 2 * kStride) return {ragged ? (void *)eb_layer_norm_back<D, T, 1, 4, true> : (void *)eb_layer_norm_back<D, T, 1, 4, false>, kThreads};
+    if (cols > kStride || ragged) return {ragged ? (void *)eb_layer_norm_back<D, T, 2, 1, true> : (void *)eb_layer_norm_back<D, T, 2, 1, false>, kThreads};
+    return {(void *)eb_layer_norm_back<D, T, 1, 1, false>, kThreads};
 }
 
 template <typename D, typename T>

@@ -74,7 +74,7 @@ struct CombineArgs {
     int32_t K;
 };
 
-template <typename T, int kRowLanes>
+template <typename T, int kRowLanes, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
 {
     constexpr int kRows = kThreads / kRowLanes;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
                 const int64_t s = k0 + i < a.K ? slots[k0 + i] : -1;
                 there[i] = s >= 0 && s < a.y_rows;
                 if (there[i]) {
-                    raw[i] = load_raw(y + s * a.ldy, c, a.cols);
+                    raw[i] = load_raw<kRagged>(y + s * a.ldy, c, a.cols);
                     w[i] = weights ? weights[k0 + i] : 1.f;
                 }
             }
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
                 for (int j = 0; j < kEach; ++j) sum[j] = fmaf(w[i], f[j], sum[j]);
             }
         }
-        store_out(a.out, t, c, (int)a.cols, sum);
+        store_out<kRagged>(a.out, t, c, (int)a.cols, sum);
     }
 }
 
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
 
 // A token's row of dout in registers, kSteps * kRowLanes * 8 columns at a time (a
 // part), for all its pairs; with several parts lane k keeps the sum for pair k.
-template <typename D, typename T, int kRowLanes, int kSteps>
+template <typename D, typename T, int kRowLanes, int kSteps, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
 {
     constexpr int kRows = kThreads / kRowLanes;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
         float d[kSteps][kEach];
         int most[kSteps];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw(dout, first + i * kStride, cols);
+        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw<kRagged>(dout, first + i * kStride, cols);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             widen8(raw[i], d[i]);
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
                 const T *y = (const T *)a.y + s * a.ldy;
                 Raw<T> other[kSteps];
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) other[i] = load_raw(y, first + i * kStride, cols);
+                for (int i = 0; i < kSteps; ++i) other[i] = load_raw<kRagged>(y, first + i * kStride, cols);
                 float dot = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
                     // A product rounds as its factor orders: the largest is the largest's.
                     const int scaled = fp8 ? magnitude(w * __int_as_float(most[i])) : 0;
                     if (fp8) store_fp8(a.out, s, first + i * kStride, cols, f, to_fp8(scaled), scaled);
-                    else store_out(a.out, s, first + i * kStride, cols, f);
+                    else store_out<kRagged>(a.out, s, first + i * kStride, cols, f);
                 }
             }
         }
@@ -227,10 +227,18 @@ int dispatch_impl(const char *who, int64_t M, int64_t cols, const void *x, int32
     return launch(who, kernel, (M + rows - 1) / rows, kThreads, &a, stream);
 }
 
-template <typename T>
+template <typename T, bool kRagged>
 void *combine_kernel(int lanes)
 {
-    return lanes == 64 ? (void *)eb_combine_rows<T, 64> : lanes == 16 ? (void *)eb_combine_rows<T, 16> : (void *)eb_combine_rows<T, 4>;
+    return lanes == 64   ? (void *)eb_combine_rows<T, 64, kRagged>
+           : lanes == 16 ? (void *)eb_combine_rows<T, 16, kRagged>
+                         : (void *)eb_combine_rows<T, 4, kRagged>;
+}
+
+template <typename T>
+void *combine_kernel(int lanes, bool ragged)
+{
+    return ragged ? combine_kernel<T, true>(lanes) : combine_kernel<T, false>(lanes);
 }
 
 int check_combine(const char *who, int64_t N, int32_t K, int64_t cols, int64_t y_rows, const int32_t *slots)
@@ -262,9 +270,10 @@ int combine_impl(const char *who, int64_t N, int32_t K, int64_t cols, const void
     a.K = K;
     const int64_t pieces = (cols + kEach - 1) / kEach;
     const int lanes = pieces > 16 ? 64 : pieces > 4 ? 16 : 4, rows = kThreads / lanes;
-    void *kernel = y_type == EB_F32   ? combine_kernel<float>(lanes)
-                   : y_type == EB_F16 ? combine_kernel<_Float16>(lanes)
-                                      : combine_kernel<Bf16>(lanes);
+    const bool ragged = cols % kEach != 0;
+    void *kernel = y_type == EB_F32   ? combine_kernel<float>(lanes, ragged)
+                   : y_type == EB_F16 ? combine_kernel<_Float16>(lanes, ragged)
+                                      : combine_kernel<Bf16>(lanes, ragged);
     return launch(who, kernel, (N + rows - 1) / rows, kThreads, &a, stream);
 }
 
@@ -272,10 +281,11 @@ template <typename D, typename T>
 void *back_kernel(int64_t cols, int *rows)
 {
     *rows = cols <= 128 ? kThreads / 16 : kThreads / kWave;
-    if (cols <= 128) return (void *)eb_combine_back<D, T, 16, 1>;
-    if (cols <= 512) return (void *)eb_combine_back<D, T, 64, 1>;
-    if (cols <= 1024) return (void *)eb_combine_back<D, T, 64, 2>;
-    return (void *)eb_combine_back<D, T, 64, 4>;
+    if (cols % kEach) return cols <= 128 ? (void *)eb_combine_back<D, T, 16, 1, true> : (void *)eb_combine_back<D, T, 64, 2, true>;
+    if (cols <= 128) return (void *)eb_combine_back<D, T, 16, 1, false>;
+    if (cols <= 512) return (void *)eb_combine_back<D, T, 64, 1, false>;
+    if (cols <= 1024) return (void *)eb_combine_back<D, T, 64, 2, false>;
+    return (void *)eb_combine_back<D, T, 64, 4, false>;
 }
 
 template <typename D>

@@ -41,19 +41,24 @@ struct Raw {
 };
 
 // Those from column c of a row on, which has columns [0, cols); zeros outside.
-template <typename T>
+// kRagged: cols may be any, and c below 0; else cols is a multiple of 8, as c is, and
+// no branch is taken: loads of several chunks then go out together.
+template <bool kRagged, typename T>
 __device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int cols)
 {
     Raw<T> r;
-    if (c >= 0 && c + kEach <= cols) {
-        const char *at = (const char *)row + (int64_t)c * (int)sizeof(T);
+    const bool whole = !kRagged || (c >= 0 && c + kEach <= cols), there = kRagged || c < cols;
+    if (whole) {
+        const char *at = (const char *)row + (int64_t)(there ? c : 0) * (int)sizeof(T);
         if constexpr (sizeof(T) == 1) {
-            const i32x2_any w = *(const i32x2_any *)at;
+            i32x2_any w = *(const i32x2_any *)at;
+            if (!there) w = 0;
             __builtin_memcpy(&r, &w, 8);
         } else {
 #pragma unroll
             for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const i32x4_any w = *(const i32x4_any *)(at + 16 * i);
+                i32x4_any w = *(const i32x4_any *)(at + 16 * i);
+                if (!there) w = 0;
                 __builtin_memcpy((char *)&r + 16 * i, &w, 16);
             }
         }
@@ -98,13 +103,14 @@ struct Scales {
 };
 
 // Columns c .. c + 7 of a row of an 8-bit matrix of `cols` columns, times their
-// scales: they lie in one block, or in two where c is no multiple of 8.
+// scales: they lie in one block, or, where c is no multiple of 8, in two.
+template <bool kRagged>
 __device__ __forceinline__ void scale8(float *f, const Scales &s, int64_t row, int c, int cols)
 {
     const int lo = max(c, 0), hi = min(c + kEach, cols) - 1, b = lo / kBlock;
-    if (lo > hi) return; // zeros
-    const float first = s.p[b * s.ld + row];
-    if (hi / kBlock == b) {
+    const bool none = lo > hi; // zeros, whatever the scales
+    const float any = s.p[(none ? 0 : b) * s.ld + row], first = none ? 0.f : any;
+    if (!kRagged || none || hi / kBlock == b) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) f[i] *= first;
     } else {
@@ -155,12 +161,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 }
 
 // Eight fp32 values to columns c .. c + 7 of a row in a floating-point type (a
-// code of eb.h), each rounded once to nearest even; those past cols are left out.
+// code of eb.h), each rounded once to nearest even; of the last chunk of a ragged row
+// those past cols are left out.
+template <bool kRagged>
 __device__ __forceinline__ void store8(void *row, int type, int c, int cols, const float *f)
 {
     if (type == EB_F32) {
         float *to = (float *)row + c;
-        if (c + kEach <= cols) {
+        if (!kRagged || c + kEach <= cols) {
             const i32x4_any lo = {__float_as_int(f[0]), __float_as_int(f[1]), __float_as_int(f[2]), __float_as_int(f[3])};
             const i32x4_any hi = {__float_as_int(f[4]), __float_as_int(f[5]), __float_as_int(f[6]), __float_as_int(f[7])};
             *(i32x4_any *)to = lo;
@@ -181,7 +189,7 @@ __device__ __forceinline__ void store8(void *row, int type, int c, int cols, con
         for (int i = 0; i < 4; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
     }
     uint16_t *to = (uint16_t *)row + c;
-    if (c + kEach <= cols) {
+    if (!kRagged || c + kEach <= cols) {
         const i32x4_any v = {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
         *(i32x4_any *)to = v;
     } else {
@@ -212,13 +220,14 @@ __device__ __forceinline__ void store_fp8(const Out &o, int64_t row, int c, int 
 __device__ __forceinline__ float to_fp8(int most) { return kMostFp8 / fmaxf(__int_as_float(most), kMostFp8 * kLeastScale); }
 
 // Columns c .. c + 7 of a row; in 8 bits the 16 lanes of a block call together.
+template <bool kRagged>
 __device__ __forceinline__ void store_out(const Out &o, int64_t row, int c, int cols, const float *f)
 {
     if (o.type == EB_FP8) {
         const int most = max_lanes<kLanes>(most8(f));
         store_fp8(o, row, c, cols, f, to_fp8(most), most);
     } else if (c < cols) {
-        store8((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
+        store8<kRagged>((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
     }
 }
 
