@@ -32,13 +32,14 @@ struct ActArgs {
 };
 
 // 1 / (1 + exp(-g)): the exponential with the rounding of its argument put right.
+// Beyond 87 it is 1 or below 2^-125.
 __device__ __forceinline__ float sigmoid(float g)
 {
     constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f; // together log2(e) to 2^-50
+    g = __builtin_amdgcn_fmed3f(g, -87.f, 87.f);
     const float h = g * -kLog2e, l = fmaf(g, -kRest, fmaf(g, -kLog2e, -h));
     const float e = __builtin_amdgcn_exp2f(h);
-    // (l is 0 or a NaN where h is infinite or far below: then e stands.)
-    return __builtin_amdgcn_rcpf(1.f + (fabsf(h) < 126.f ? fmaf(e, l * 0.693147182f, e) : e));
+    return __builtin_amdgcn_rcpf(1.f + fmaf(e, l * 0.693147182f, e));
 }
 
 // Columns c .. c + 7 of v that lie in [lo, hi); zeros for the others.
@@ -119,7 +120,9 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         float u[kEach], e[kEach];
         widen8(of_h, dh);
         widen_v<kRagged>(a, row, c, cols, first, g);
-        widen_v<kRagged>(a, row, cols + c, width, second, u);
+        const bool fp8 = a.out.type == EB_FP8; // whole blocks
+        if (sizeof(T) == 1 && fp8) widen8(second, u);
+        else widen_v<kRagged>(a, row, cols + c, width, second, u);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float2 v = d_gate(dh[i], g[i], u[i]);
@@ -127,13 +130,28 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
             e[i] = v.y;
         }
         Out of_u = a.out;
-        if (a.out.type == EB_FP8) { // whole blocks
-            of_u.p = (char *)a.out.p + cols;
-            of_u.scales = a.out.scales + cols / kBlock * a.out.lds;
-        } else {
+        if (!fp8) {
             of_u.p = (char *)a.out.p + cols * (int64_t)(a.out.type == EB_F32 ? 4 : 2);
+            store8_of<kRagged>(a.out, row, c, cols, d);
+            store8_of<kRagged>(of_u, row, c, cols, e);
+            continue;
         }
-        store_out<kRagged>(a.out, row, c, cols, d);
+        of_u.p = (char *)a.out.p + cols;
+        of_u.scales = a.out.scales + cols / kBlock * a.out.lds;
+        if constexpr (sizeof(T) == 1) {
+            // u's block is dg's: its scale is a factor of dg's scale, and of none of its values.
+            const float su = a.v_scales.p[(c < cols ? (cols + c) / kBlock : 0) * a.v_scales.ld + row];
+            const int most = max_lanes<kLanes>(most8(d)), scaled = magnitude(__int_as_float(most) * su);
+            if (__int_as_float(scaled) <= kMostFp8 * kLeastScale) { // the least scale: the values count
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) d[i] *= su;
+                store_fp8(a.out, row, c, cols, d, 1.f / kLeastScale, scaled);
+            } else {
+                store_fp8(a.out, row, c, cols, d, to_fp8(most), scaled);
+            }
+        } else {
+            store_out<kRagged>(a.out, row, c, cols, d);
+        }
         store_out<kRagged>(of_u, row, c, cols, e);
     }
 }

@@ -58,7 +58,7 @@ __device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, co
         // n / scale is d times one factor: as exact as d.
         const int most_d = max_lanes<kLanes>(most8(d)), most = magnitude(__int_as_float(most_d) * rstd);
         if (__int_as_float(most) <= kMostFp8 * kLeastScale) store_fp8(a.kept, row, c, cols, n, 1.f / kLeastScale, most);
-        else store_fp8(a.kept, row, c, cols, d, kMostFp8 / __int_as_float(most_d), most);
+        else store_fp8(a.kept, row, c, cols, d, to_fp8(most_d), most);
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {

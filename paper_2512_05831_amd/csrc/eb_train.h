@@ -207,17 +207,39 @@ struct Out {
     int32_t type;
 };
 
+// The scale of a block whose largest magnitude has these bits: its 448th, rounded once
+// (the quotient by a product, then what that leaves of the dividend), 2^-126 and more.
+__device__ __forceinline__ float scale_of(int most)
+{
+    constexpr float kPart = 1.f / kMostFp8;
+    const float m = __int_as_float(most), q = m * kPart;
+    const float s = fmaxf(fmaf(fmaf(-kMostFp8, q, m), kPart, q), kLeastScale);
+    return most >= 0x7F800000 ? __int_as_float(0x7FC00000) : s;
+}
+
+// What brings such a block's values to e4m3: 448 / largest, within an ulp (the
+// reciprocal instruction's, and one step of Newton's method).
+__device__ __forceinline__ float to_fp8(int most)
+{
+    const float m = fmaxf(__int_as_float(most), kMostFp8 * kLeastScale) * 0x1p-4f, r = __builtin_amdgcn_rcpf(m); // both normal
+    return fmaf(fmaf(-m, r, 1.f), r, r) * (kMostFp8 * 0x1p-4f);
+}
+
 // Columns c .. c + 7 of a row in 8 bits, the row padded to 16 bytes: values that are
 // `by` to be multiplied with, under a scale for the largest magnitude `most` (bits).
 __device__ __forceinline__ void store_fp8(const Out &o, int64_t row, int c, int cols, const float *f, float by, int most)
 {
     if (c >= ((cols + 15) & ~15)) return;
     *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits(f, by, most >= 0x7F800000, cols - c);
-    if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = block_scale(most);
+    if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = scale_of(most);
 }
 
-// What brings a block's values to e4m3.
-__device__ __forceinline__ float to_fp8(int most) { return kMostFp8 / fmaxf(__int_as_float(most), kMostFp8 * kLeastScale); }
+// Columns c .. c + 7 of a row in floating point.
+template <bool kRagged>
+__device__ __forceinline__ void store8_of(const Out &o, int64_t row, int c, int cols, const float *f)
+{
+    if (c < cols) store8<kRagged>((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
+}
 
 // Columns c .. c + 7 of a row; in 8 bits the 16 lanes of a block call together.
 template <bool kRagged>
@@ -226,8 +248,8 @@ __device__ __forceinline__ void store_out(const Out &o, int64_t row, int c, int 
     if (o.type == EB_FP8) {
         const int most = max_lanes<kLanes>(most8(f));
         store_fp8(o, row, c, cols, f, to_fp8(most), most);
-    } else if (c < cols) {
-        store8<kRagged>((char *)o.p + row * o.ld * (o.type == EB_F32 ? 4 : 2), o.type, c, cols, f);
+    } else {
+        store8_of<kRagged>(o, row, c, cols, f);
     }
 }
 
