@@ -44,14 +44,19 @@ __device__ __forceinline__ float sum_row(float v, float *shared, int wave)
 }
 
 // The outputs of columns c .. c + 7, of which d is x - mean (zeros past cols).
-template <bool kRagged>
-__device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, const float *d, float rstd)
+template <bool kRagged, bool kHeld>
+__device__ __forceinline__ void write8(const NormArgs &a, const float *held, int64_t row, int c, const float *d, float rstd)
 {
     const int cols = (int)a.cols;
     if (c >= ((cols + kBlock - 1) & ~(kBlock - 1))) return; // whole blocks: their 16 lanes stay together
     float n[kEach], y[kEach], w[kEach], b[kEach];
-    if (a.weight) widen8(load_raw<kRagged>(a.weight, c, cols), w);
-    if (a.bias) widen8(load_raw<kRagged>(a.bias, c, cols), b);
+    if constexpr (kHeld) {
+        __builtin_memcpy(w, held + 2 * c, sizeof(w)); // a chunk's weights, then its biases
+        __builtin_memcpy(b, held + 2 * c + kEach, sizeof(b));
+    } else {
+        if (a.weight) widen8(load_raw<kRagged>(a.weight, c, cols), w);
+        if (a.bias) widen8(load_raw<kRagged>(a.bias, c, cols), b);
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) n[i] = d[i] * rstd;
     if (a.kept.p) {
@@ -62,15 +67,15 @@ __device__ __forceinline__ void write8(const NormArgs &a, int64_t row, int c, co
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        y[i] = a.weight ? n[i] * w[i] : n[i];
-        if (a.bias) y[i] += b[i];
+        y[i] = kHeld || a.weight ? n[i] * w[i] : n[i];
+        if (kHeld || a.bias) y[i] += b[i];
     }
     store_out<kRagged>(a.y, row, c, cols, y);
 }
 
 // kSteps * 512 columns a wave; kLoop: any number of them, read again for each sum.
 template <typename T, int kSteps, int kWaves, bool kLoop, bool kRagged>
-__global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_rows(NormArgs a)
+__global__ __launch_bounds__(kThreads, kSteps > 4 ? 4 : 6) void eb_layer_norm_rows(NormArgs a)
 {
     __shared__ float shared[kWaves];
     constexpr int kRows = kThreads / kWave / kWaves;
@@ -128,7 +133,7 @@ __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_r
         for (int c = first; c < blocks; c += kAll) {
             widen8(load_raw<kRagged>(x, c, cols), f);
             centred(c, f, mean);
-            write8<kRagged>(a, row, c, f, rstd);
+            write8<kRagged, false>(a, nullptr, row, c, f, rstd);
         }
     } else {
         float f[kSteps][kEach];
@@ -152,33 +157,113 @@ __global__ __launch_bounds__(kThreads, kSteps == 8 ? 4 : 6) void eb_layer_norm_r
         statistics(mean, rstd);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            write8<kRagged>(a, row, first + i * kAll, f[i], rstd);
+            write8<kRagged, false>(a, nullptr, row, first + i * kAll, f[i], rstd);
             __builtin_amdgcn_sched_barrier(0); // not all steps' weights at a time: registers
         }
     }
 }
 
-struct Plan {
-    void *kernel;
-    int rows; // of a workgroup
-};
+// Many rows of up to 4096 columns with weights: a workgroup reads those once for its
+// eight rows, a wave each, into LDS while the rows are on their way (else every row
+// waits for its weights, step after step: 16384 x 3328 fp32 90 us, so 78.5, 4.9 TB/s).
+constexpr int kHeldRows = 8;
+
+template <typename T, int kSteps>
+__global__ __launch_bounds__(kHeldRows * kWave, 4) void eb_layer_norm_held(NormArgs a)
+{
+    __shared__ alignas(16) float held[kSteps * kStride * 2];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), cols = (int)a.cols, first = threadIdx.x % kWave * kEach;
+    const int64_t row = min((int64_t)blockIdx.x * kHeldRows + wave, a.rows - 1); // past the end: the last one again
+    const T *x = (const T *)a.x + row * a.ldx;
+    Raw<T> raw[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) raw[i] = load_raw<false>(x, first + i * kStride, cols);
+    // The chunks of weights are the waves' in turn.
+#pragma unroll
+    for (int i = 0; i < (kSteps + kHeldRows - 1) / kHeldRows; ++i) {
+        const int c = (i * kHeldRows + wave) * kStride + first;
+        if (i * kHeldRows + wave >= kSteps) break;
+        float w[kEach], b[kEach] = {};
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) w[j] = 1.f;
+        if (a.weight) widen8(load_raw<false>(a.weight, c, cols), w);
+        if (a.bias) widen8(load_raw<false>(a.bias, c, cols), b);
+        __builtin_memcpy(held + 2 * c, w, sizeof(w));
+        __builtin_memcpy(held + 2 * c + kEach, b, sizeof(b));
+    }
+    float f[kSteps][kEach], sum = 0.f, square = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        widen8(raw[i], f[i]);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) sum += f[i][j];
+    }
+    const float mean = sum_lanes<kWave>(sum) / (float)cols;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const bool there = first + i * kStride < cols;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            f[i][j] = there ? f[i][j] - mean : 0.f;
+            square = fmaf(f[i][j], f[i][j], square);
+        }
+    }
+    const float rstd = 1.f / sqrtf(sum_lanes<kWave>(square) / (float)cols + a.eps);
+    if (threadIdx.x % kWave == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        write8<false, true>(a, held, row, first + i * kStride, f[i], rstd);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 template <typename T, bool kRagged>
-Plan plan_of(int64_t rows, int64_t cols)
+void *rows_kernel(int64_t cols, int *rows)
 {
-    if (cols > 8 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 1, 4, true, kRagged>, 1};
-    if (cols > 4 * 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 4, false, kRagged>, 1};
-    if (cols > 8 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 4, false, kRagged>, 1};
-    if (cols > 4 * kStride) return {(void *)eb_layer_norm_rows<T, 8, 1, false, kRagged>, 4};
-    if (cols > 2 * kStride) return {(void *)eb_layer_norm_rows<T, 4, 1, false, kRagged>, 4};
-    if (cols > kStride) return {(void *)eb_layer_norm_rows<T, 2, 1, false, kRagged>, 4};
-    return {(void *)eb_layer_norm_rows<T, 1, 1, false, kRagged>, 4};
+    *rows = cols > 8 * kStride ? 1 : 4;
+    if (cols > 8 * 4 * kStride) return (void *)eb_layer_norm_rows<T, 1, 4, true, kRagged>;
+    if (cols > 4 * 4 * kStride) return (void *)eb_layer_norm_rows<T, 8, 4, false, kRagged>;
+    if (cols > 8 * kStride) return (void *)eb_layer_norm_rows<T, 4, 4, false, kRagged>;
+    if (cols > 4 * kStride) return (void *)eb_layer_norm_rows<T, 8, 1, false, kRagged>;
+    if (cols > 2 * kStride) return (void *)eb_layer_norm_rows<T, 4, 1, false, kRagged>;
+    if (cols > kStride) return (void *)eb_layer_norm_rows<T, 2, 1, false, kRagged>;
+    return (void *)eb_layer_norm_rows<T, 1, 1, false, kRagged>;
 }
 
 template <typename T>
-Plan plan_of(int64_t rows, int64_t cols)
+void *held_kernel(int64_t cols)
 {
-    return cols % kEach ? plan_of<T, true>(rows, cols) : plan_of<T, false>(rows, cols);
+    switch ((cols + kStride - 1) / kStride) {
+    case 1: return (void *)eb_layer_norm_held<T, 1>;
+    case 2: return (void *)eb_layer_norm_held<T, 2>;
+    case 3: return (void *)eb_layer_norm_held<T, 3>;
+    case 4: return (void *)eb_layer_norm_held<T, 4>;
+    case 5: return (void *)eb_layer_norm_held<T, 5>;
+    case 6: return (void *)eb_layer_norm_held<T, 6>;
+    case 7: return (void *)eb_layer_norm_held<T, 7>;
+    default: return (void *)eb_layer_norm_held<T, 8>;
+    }
+}
+
+struct Plan {
+    void *kernel;
+    int64_t grid;
+    int threads;
+};
+
+template <typename T>
+Plan plan_of(int64_t rows, int64_t cols, bool affine)
+{
+    constexpr int64_t kMany = 2048;
+    if (affine && cols % kEach == 0 && cols <= 8 * kStride && rows >= kMany)
+        return {held_kernel<T>(cols), rows / kHeldRows + (rows % kHeldRows != 0), kHeldRows * kWave};
+    int each = 1;
+    void *kernel = cols % kEach ? rows_kernel<T, true>(cols, &each) : rows_kernel<T, false>(cols, &each);
+    return {kernel, rows / each + (rows % each != 0), kThreads};
 }
 
 int norm_impl(const char *who, int64_t rows, int64_t cols, const void *x, int32_t dtype, int64_t ldx, const float *weight, const float *bias,
@@ -206,10 +291,11 @@ int norm_impl(const char *who, int64_t rows, int64_t cols, const void *x, int32_
     a.cols = cols;
     a.ldx = ldx;
     a.eps = eps;
-    const Plan plan = dtype == EB_F32   ? plan_of<float>(rows, cols)
-                      : dtype == EB_F16 ? plan_of<_Float16>(rows, cols)
-                                        : plan_of<Bf16>(rows, cols);
-    return launch(who, plan.kernel, rows / plan.rows + (rows % plan.rows != 0), kThreads, &a, stream);
+    const bool affine = weight || bias;
+    const Plan plan = dtype == EB_F32   ? plan_of<float>(rows, cols, affine)
+                      : dtype == EB_F16 ? plan_of<_Float16>(rows, cols, affine)
+                                        : plan_of<Bf16>(rows, cols, affine);
+    return launch(who, plan.kernel, plan.grid, plan.threads, &a, stream);
 }
 
 } // namespace

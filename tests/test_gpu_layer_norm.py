@@ -81,6 +81,16 @@ def test_forward_many_rows(cols, device):
 
 
 @pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("rows,cols", [(2048, 8), (2051, 512), (2050, 520), (4099, 200), (2049, 1512), (2055, 2048), (2100, 2568), (2101, 3080), (2500, 4096)])
+def test_forward_weights_held(rows, cols, dtype, device):
+    """Rows that share their weights by eight; the last ones fewer."""
+    x, w, b = inputs(rows, cols, dtype, device)
+    check_forward(x, w, b, 1e-5, dtype, checkpoint=True)
+    check_forward(x, w, None, 1e-5, FP8, statistics=True)
+    check_forward(x, None, b, 1e-5, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", WIDE)
 def test_forward_strided(dtype, device):
     x, w, b = inputs(40, 900, dtype, device)
     for view in (x[3:, 5:777], x[::3, 1:130], x[1:2, 7:]):
