@@ -121,8 +121,7 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         widen8(of_h, dh);
         widen_v<kRagged>(a, row, c, cols, first, g);
         const bool fp8 = a.out.type == EB_FP8; // whole blocks
-        if (sizeof(T) == 1 && fp8) widen8(second, u);
-        else widen_v<kRagged>(a, row, cols + c, width, second, u);
+        widen_v<kRagged>(a, row, cols + c, width, second, u);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float2 v = d_gate(dh[i], g[i], u[i]);
@@ -138,21 +137,64 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         }
         of_u.p = (char *)a.out.p + cols;
         of_u.scales = a.out.scales + cols / kBlock * a.out.lds;
-        if constexpr (sizeof(T) == 1) {
-            // u's block is dg's: its scale is a factor of dg's scale, and of none of its values.
-            const float su = a.v_scales.p[(c < cols ? (cols + c) / kBlock : 0) * a.v_scales.ld + row];
-            const int most = max_lanes<kLanes>(most8(d)), scaled = magnitude(__int_as_float(most) * su);
-            if (__int_as_float(scaled) <= kMostFp8 * kLeastScale) { // the least scale: the values count
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) d[i] *= su;
-                store_fp8(a.out, row, c, cols, d, 1.f / kLeastScale, scaled);
-            } else {
-                store_fp8(a.out, row, c, cols, d, to_fp8(most), scaled);
-            }
-        } else {
-            store_out<kRagged>(a.out, row, c, cols, d);
-        }
+        store_out<kRagged>(a.out, row, c, cols, d);
         store_out<kRagged>(of_u, row, c, cols, e);
+    }
+}
+
+// The same from 8 bits to 8 bits, gated, columns a multiple of 128: bound by the vector
+// unit as much as by memory (65536 x 1024 from bf16 dh: BLOCKS_US us, at 5.2 TB/s 79), so
+// nothing is made twice: a block's place is the workgroup's, and u's scale is left to
+// dg's, whose block is u's.
+template <typename D>
+__global__ __launch_bounds__(kThreads) void eb_activate_back_blocks(ActArgs a)
+{
+    const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
+    const int64_t row = (int64_t)(blockIdx.x / strips) * kRows + threadIdx.x / kLanes;
+    const int b0 = blockIdx.x % strips * kSteps, cols = (int)a.cols, blocks = (int)a.blocks;
+    if (row >= a.rows) return;
+    const int at = threadIdx.x % kLanes * kEach;
+    const D *dh_row = (const D *)a.dh + row * a.lddh + at;
+    const Fp8 *v_row = (const Fp8 *)a.v + row * a.ldv + at;
+    char *out_row = (char *)a.out.p + row * a.out.ld + at;
+    Raw<D> of_h[kSteps];
+    Raw<Fp8> of_g[kSteps], of_u[kSteps];
+    float sg[kSteps], su[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) { // a step past the last block takes that again, and writes it again
+        const int b = min(b0 + s, blocks - 1), c = b * kBlock;
+        of_h[s] = load_raw<false>(dh_row + c, 0, kEach);
+        of_g[s] = load_raw<false>(v_row + c, 0, kEach);
+        of_u[s] = load_raw<false>(v_row + cols + c, 0, kEach);
+        sg[s] = (a.v_scales.p + (int64_t)b * a.v_scales.ld)[row];
+        su[s] = (a.v_scales.p + (int64_t)(blocks + b) * a.v_scales.ld)[row];
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int b = min(b0 + s, blocks - 1), c = b * kBlock;
+        float d[kEach], e[kEach], g[kEach], u[kEach];
+        widen8(of_h[s], d);
+        widen8(of_g[s], g);
+        widen8(of_u[s], u);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const float2 v = d_gate(d[i], g[i] * sg[s], u[i]);
+            d[i] = v.x;
+            e[i] = v.y;
+        }
+        const int most_d = most_of_block(most8(d)), scaled = magnitude(__int_as_float(most_d) * su[s]), most_e = most_of_block(most8(e));
+        Factor of_d = to_fp8(most_d);
+        if (__int_as_float(scaled) <= kMostFp8 * kLeastScale) { // the least scale: the values count
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) d[i] *= su[s];
+            of_d = kToLeast;
+        }
+        *(int2 *)(out_row + c) = eight_bits<false>(d, of_d, scaled >= 0x7F800000, kEach);
+        *(int2 *)(out_row + cols + c) = eight_bits<false>(e, to_fp8(most_e), most_e >= 0x7F800000, kEach);
+        if (threadIdx.x % kLanes == 0) {
+            (a.out.scales + (int64_t)b * a.out.lds)[row] = scale_of(scaled);
+            (a.out.scales + (int64_t)(blocks + b) * a.out.lds)[row] = scale_of(most_e);
+        }
     }
 }
 
@@ -277,6 +319,12 @@ int back_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const vo
     a.lddh = lddh;
     const bool across = a.gate && out_type == EB_FP8 && cols % kBlock != 0;
     a.blocks = ((across ? a.width : cols) + kBlock - 1) / kBlock;
+    if (a.gate && v_type == EB_FP8 && out_type == EB_FP8 && !across) {
+        void *kernel = dh_type == EB_F32   ? (void *)eb_activate_back_blocks<float>
+                       : dh_type == EB_F16 ? (void *)eb_activate_back_blocks<_Float16>
+                                           : (void *)eb_activate_back_blocks<Bf16>;
+        return launch_rows(who, kernel, a, stream);
+    }
     void *kernel = dh_type == EB_F32   ? back_kernel<float>(v_type, across, cols % kEach != 0)
                    : dh_type == EB_F16 ? back_kernel<_Float16>(v_type, across, cols % kEach != 0)
                                        : back_kernel<Bf16>(v_type, across, cols % kEach != 0);

@@ -61,8 +61,8 @@ __device__ __forceinline__ void write8(const NormArgs &a, const float *held, int
     for (int i = 0; i < kEach; ++i) n[i] = d[i] * rstd;
     if (a.kept.p) {
         // n / scale is d times one factor: as exact as d.
-        const int most_d = max_lanes<kLanes>(most8(d)), most = magnitude(__int_as_float(most_d) * rstd);
-        if (__int_as_float(most) <= kMostFp8 * kLeastScale) store_fp8(a.kept, row, c, cols, n, 1.f / kLeastScale, most);
+        const int most_d = most_of_block(most8(d)), most = magnitude(__int_as_float(most_d) * rstd);
+        if (__int_as_float(most) <= kMostFp8 * kLeastScale) store_fp8(a.kept, row, c, cols, n, kToLeast, most);
         else store_fp8(a.kept, row, c, cols, d, to_fp8(most_d), most);
     }
 #pragma unroll

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             widen8(raw[i], d[i]);
-            if (fp8) most[i] = max_lanes<kLanes>(most8(d[i]));
+            if (fp8) most[i] = most_of_block(most8(d[i]));
         }
         for (int k = 0; k < a.K; ++k) {
             const int64_t s = a.slots[t * a.K + k];

@@ -129,13 +129,34 @@ __device__ __forceinline__ int most8(const float *f)
     return m;
 }
 
-// Eight values times `by` as e4m3; NaNs where a block's scale is one. `left`: how many
-// of them there are (the others are zeros).
-__device__ __forceinline__ int2 eight_bits(const float *f, float by, bool nan, int left)
+// The largest over the 16 lanes of a block, all of them there, in every lane.
+__device__ __forceinline__ int most_of_block(int v)
 {
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true)); // rotated by 8
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x124, 0xF, 0xF, true));
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x122, 0xF, 0xF, true));
+    return max(v, __builtin_amdgcn_mov_dpp(v, 0x121, 0xF, 0xF, true));
+}
+
+// What brings a block's values to e4m3: 448 / largest, and what its rounding left.
+struct Factor {
+    float by, rest;
+};
+
+// Eight values times that as e4m3; NaNs where a block's scale is one. `left`: how many
+// of them there are (the others are zeros).  The product is the quotient rounded once
+// to fp32 (but for one in 2^20): values that lie in the middle of two e4m3 numbers
+// stay there.
+// kOnce false: rounded twice, where the values have roundings of their own behind them.
+template <bool kOnce>
+__device__ __forceinline__ int2 eight_bits(const float *f, Factor k, bool nan, int left)
+{
+    float p[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) p[i] = kOnce ? fmaf(f[i], k.by, f[i] * k.rest) : f[i] * k.by;
     int2 v;
-    v.x = pack_fp8(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
-    v.y = pack_fp8(f[4] * by, f[5] * by, f[6] * by, f[7] * by);
+    v.x = pack_fp8(p[0], p[1], p[2], p[3]);
+    v.y = pack_fp8(p[4], p[5], p[6], p[7]);
     if (nan) {
         const uint64_t all = 0x7F7F7F7F7F7F7F7Full, some = left >= 8 ? all : left <= 0 ? 0 : all >> 8 * (8 - left);
         v.x = (int)some;
@@ -217,20 +238,23 @@ __device__ __forceinline__ float scale_of(int most)
     return most >= 0x7F800000 ? __int_as_float(0x7FC00000) : s;
 }
 
-// What brings such a block's values to e4m3: 448 / largest, within an ulp (the
-// reciprocal instruction's, and one step of Newton's method).
-__device__ __forceinline__ float to_fp8(int most)
+// The factor of such a block (the reciprocal instruction's, and steps of Newton's method).
+__device__ __forceinline__ Factor to_fp8(int most)
 {
     const float m = fmaxf(__int_as_float(most), kMostFp8 * kLeastScale) * 0x1p-4f, r = __builtin_amdgcn_rcpf(m); // both normal
-    return fmaf(fmaf(-m, r, 1.f), r, r) * (kMostFp8 * 0x1p-4f);
+    const float by = fmaf(fmaf(-m, r, 1.f), r, r) * (kMostFp8 * 0x1p-4f);
+    return {by, fmaf(-m, by, kMostFp8 * 0x1p-4f) * r};
 }
+
+constexpr Factor kToLeast = {1.f / kLeastScale, 0.f}; // under the least scale
 
 // Columns c .. c + 7 of a row in 8 bits, the row padded to 16 bytes: values that are
 // `by` to be multiplied with, under a scale for the largest magnitude `most` (bits).
-__device__ __forceinline__ void store_fp8(const Out &o, int64_t row, int c, int cols, const float *f, float by, int most)
+template <bool kOnce = true>
+__device__ __forceinline__ void store_fp8(const Out &o, int64_t row, int c, int cols, const float *f, Factor by, int most)
 {
     if (c >= ((cols + 15) & ~15)) return;
-    *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits(f, by, most >= 0x7F800000, cols - c);
+    *(int2 *)((char *)o.p + row * o.ld + c) = eight_bits<kOnce>(f, by, most >= 0x7F800000, cols - c);
     if (c % kBlock == 0) o.scales[c / kBlock * o.lds + row] = scale_of(most);
 }
 
@@ -246,7 +270,7 @@ template <bool kRagged>
 __device__ __forceinline__ void store_out(const Out &o, int64_t row, int c, int cols, const float *f)
 {
     if (o.type == EB_FP8) {
-        const int most = max_lanes<kLanes>(most8(f));
+        const int most = most_of_block(most8(f));
         store_fp8(o, row, c, cols, f, to_fp8(most), most);
     } else {
         store8_of<kRagged>(o, row, c, cols, f);
