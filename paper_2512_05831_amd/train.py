@@ -16,9 +16,11 @@ import ctypes
 import functools
 from typing import NamedTuple
 
+import torch
+
 from . import eb, experts as ex
 from .eb import EB_BF16, EB_F16, EB_F32, _check
-from .experts import BLOCK, EB_ACT_RELU, EB_ACT_SILU_GATE, EB_FP8, _code, _gpu, _place, _raw_stream, _same_device
+from .experts import BLOCK, EB_ACT_SILU_GATE, EB_FP8, _place
 
 _lib = None
 
@@ -128,44 +130,61 @@ def eb_weight_gradient(M: int, E: int, N: int, K: int, dy_ptr: int | None, dy_ty
 # --------------------------------------------------------------------------- torch
 
 
+_F32, _I32, _BF16, _FP8 = torch.float32, torch.int32, torch.bfloat16, torch.float8_e4m3fn
+_CODES = {_F32: EB_F32, torch.float16: EB_F16, _BF16: EB_BF16, _FP8: EB_FP8}
+
+
+def _code(dtype) -> int:
+    code = _CODES.get(dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {dtype}")
+    return code
+
+
 def _placed(f):
     """The call under its ``stream``, or on its first tensor's GPU: at once where that is current."""
     @functools.wraps(f)
     def call(x, *args, stream=None, **kw):
-        if stream is None and -1 < x.get_device() == _gpu():
+        if stream is None and -1 < x.get_device() == ex._gpu():
             return f(x, *args, **kw)
         if not x.is_cuda:
             raise ValueError("expected device tensors")
-        import torch
-
         with _place(torch, x, stream):
             return f(x, *args, stream=stream, **kw)
     return call
 
 
 def _stream(x, stream):
-    return _raw_stream(x.get_device()) if stream is None else stream.cuda_stream
+    return ex._raw_stream(x.get_device()) if stream is None else stream.cuda_stream
 
 
-def _matrix(x, what: str, scales=None, cols: int | None = None):
-    """(pointer, code, pitch, scales' pointer, scales' pitch, what has to live on) of a 2-D
+def _floating(x, what: str):
+    """(pointer, code, pitch) of a 2-D tensor of fp32, fp16 or bf16 with unit column stride."""
+    code = _CODES.get(x.dtype)
+    if code is None or code == EB_FP8 or x.dim() != 2:
+        raise ValueError(f"{what} must be 2-D, fp32, fp16 or bf16")
+    return x.data_ptr(), code, ex._pitch(x, what)
+
+
+def _matrix(x, what: str, scales):
+    """(pointer, code, pitch, scales' pointer, scales' pitch, the scales in use) of a 2-D
     tensor with unit column stride, in 8 bits with its scales."""
-    if x.dim() != 2:
-        raise ValueError(f"{what} must be 2-D")
-    code = _code(x.dtype, fp8=True)
-    rows, n = x.shape
-    if cols is not None and n != cols:
-        raise ValueError(f"{what} must have {cols} columns")
+    code = _CODES.get(x.dtype)
+    if code is None or x.dim() != 2:
+        raise ValueError(f"{what} must be 2-D, fp32, fp16, bf16 or float8_e4m3fn")
     ld = ex._pitch(x, what)
     if code != EB_FP8:
         if scales is not None:
             raise ValueError(f"{what} is not in 8 bits: it takes no scales")
-        return x.data_ptr(), code, ld, None, 0, x
+        return x.data_ptr(), code, ld, None, 0, None
+    rows, n = x.shape
     if rows == 1 and ld % 16:
         ld = ld + 15 & -16  # a single row has no next one
     blocks = (n + BLOCK - 1) // BLOCK
-    if scales is None or str(scales.dtype) != "torch.float32" or scales.shape != (rows, blocks):
+    if scales is None or scales.dtype != _F32 or scales.shape != (rows, blocks):
         raise ValueError(f"{what} in 8 bits needs its scales, fp32 [rows, ceil(columns/128)]")
+    if scales.get_device() != x.get_device():
+        raise ValueError(f"the scales of {what} are on {scales.device}, expected {x.device}")
     by_row, by_block = scales.stride()
     if rows > 1 and by_row != 1 or blocks > 1 and by_block < rows:
         scales = scales.t().contiguous().t()
@@ -174,42 +193,25 @@ def _matrix(x, what: str, scales=None, cols: int | None = None):
 
 
 def _new(like, rows: int, cols: int, dtype):
-    """An output matrix of rows x cols beside ``like``: (tensor, code, pitch, scales or None)."""
-    import torch
-
-    code = _code(dtype, fp8=True)
+    """An output matrix beside ``like``: (tensor, code, pitch, scales or None, their pointer)."""
+    code = _code(dtype)
     if code != EB_FP8:
-        return like.new_empty((rows, cols), dtype=dtype), code, cols, None
+        return like.new_empty((rows, cols), dtype=dtype), code, cols, None, None
     ld = cols + 15 & -16
     q = like.new_empty((rows, ld), dtype=dtype)
-    scales = like.new_empty_strided((rows, (cols + BLOCK - 1) // BLOCK), (1, rows), dtype=torch.float32)
-    return (q if ld == cols else q[:, :cols]), code, ld, scales
+    scales = like.new_empty_strided((rows, (cols + BLOCK - 1) // BLOCK), (1, rows), dtype=_F32)
+    return (q if ld == cols else q[:, :cols]), code, ld, scales, scales.data_ptr()
 
 
-def _floats(x, what: str, dev, *shape):
-    """The address of a contiguous fp32 tensor of a shape on a GPU; None of None."""
+def _vector(x, what: str, dtype, dev, *shape):
+    """The address of a contiguous tensor of a type and shape on a GPU; None of None."""
     if x is None:
         return None
-    if str(x.dtype) != "torch.float32" or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous fp32 {list(shape)}")
-    _same_device(dev, x)
+    if x.dtype != dtype or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {list(shape)}")
+    if x.get_device() != dev:
+        raise ValueError(f"{what} is on {x.device}, expected GPU {dev}")
     return x.data_ptr()
-
-
-def _ints(x, what: str, dev, *shape):
-    """The same for int32."""
-    if x is None:
-        return None
-    if str(x.dtype) != "torch.int32" or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous int32 {list(shape)}")
-    _same_device(dev, x)
-    return x.data_ptr()
-
-
-def _bf16():
-    import torch
-
-    return torch.bfloat16
 
 
 class Norm(NamedTuple):
@@ -230,26 +232,24 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out_dtype=None, sta
     ``out_dtype``: y's type (bfloat16), float8_e4m3fn for 8 bits with scales.  For the
     backward pass ``statistics`` gives mean and rstd (the caller keeps x), ``checkpoint``
     rstd and the normalised values in 8 bits."""
-    import torch
-
-    ptr, code, ldx, *_ = _matrix(x, "x")
-    if code == EB_FP8:
-        raise ValueError("x must be fp32, fp16 or bf16")
-    (rows, cols), dev = x.shape, x.device
-    y, out_type, ldy, y_scales = _new(x, rows, cols, out_dtype or torch.bfloat16)
+    ptr, code, ldx = _floating(x, "x")
+    (rows, cols), dev = x.shape, x.get_device()
+    y, out_type, ldy, y_scales, ys_ptr = _new(x, rows, cols, out_dtype or _BF16)
     mean = rstd = kept = kept_scales = None
+    mean_ptr = rstd_ptr = kept_ptr = ks_ptr = None
     ldk = 0
     if statistics:
-        mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+        mean, rstd = x.new_empty((2, rows), dtype=_F32).unbind(0)
+        mean_ptr, rstd_ptr = mean.data_ptr(), rstd.data_ptr()
     elif checkpoint:
-        rstd = x.new_empty((rows,), dtype=torch.float32)
+        rstd = x.new_empty((rows,), dtype=_F32)
+        rstd_ptr = rstd.data_ptr()
     if checkpoint:
-        kept, _, ldk, kept_scales = _new(x, rows, cols, torch.float8_e4m3fn)
+        kept, _, ldk, kept_scales, ks_ptr = _new(x, rows, cols, _FP8)
+        kept_ptr = kept.data_ptr()
     rc = (_lib or library()).eb_layer_norm(
-        rows, cols, ptr, code, ldx, _floats(weight, "weight", dev, cols), _floats(bias, "bias", dev, cols), eps, out_type, y.data_ptr(), ldy,
-        None if y_scales is None else y_scales.data_ptr(), rows, None if kept is None else kept.data_ptr(), ldk,
-        None if kept is None else kept_scales.data_ptr(), rows, None if mean is None else mean.data_ptr(),
-        None if rstd is None else rstd.data_ptr(), _stream(x, stream))
+        rows, cols, ptr, code, ldx, _vector(weight, "weight", _F32, dev, cols), _vector(bias, "bias", _F32, dev, cols), eps, out_type,
+        y.data_ptr(), ldy, ys_ptr, rows, kept_ptr, ldk, ks_ptr, rows, mean_ptr, rstd_ptr, _stream(x, stream))
     if rc:
         _check(rc)
     return Norm(y, y_scales, mean, rstd, kept, kept_scales)
@@ -266,29 +266,26 @@ def layer_norm_backward(dy, x, rstd, mean=None, x_scales=None, weight=None, para
     fp16 or bf16; ``x`` with ``mean``: forward's input; or ``x`` (8 bits) with ``x_scales``:
     what it kept; ``weight``: forward's.  Returns (dx of dy's type, dweight, dbias), the
     last two fp32 [cols], or None without ``parameters``."""
-    import torch
-
-    dy_ptr, dy_type, lddy, *_ = _matrix(dy, "dy")
-    if dy_type == EB_FP8:
-        raise ValueError("dy must be fp32, fp16 or bf16")
-    (rows, cols), dev = dy.shape, dy.device
-    if x.shape != dy.shape:
-        raise ValueError("x must have dy's shape")
+    dy_ptr, dy_type, lddy = _floating(dy, "dy")
+    (rows, cols), dev = dy.shape, dy.get_device()
+    if x.shape != dy.shape or x.get_device() != dev:
+        raise ValueError("x must have dy's shape, on its GPU")
     x_ptr, x_type, ldx, xs_ptr, ldxs, held = _matrix(x, "x", x_scales)
-    _same_device(dev, x, x_scales)
     if (x_type == EB_FP8) != (mean is None):
         raise ValueError("mean goes with an x in floating point, and only with that")
     dx = dy.new_empty((rows, cols))
     dweight = dbias = work = None
+    dw_ptr = db_ptr = work_ptr = None
     nbytes = 0
     if parameters:
-        dweight, dbias = dy.new_empty((2, cols), dtype=torch.float32).unbind(0)
         nbytes = _norm_workspace(rows, cols)
-        work = dy.new_empty((nbytes // 4,), dtype=torch.float32)
+        dweight, dbias = dy.new_empty((2, cols), dtype=_F32).unbind(0)
+        work = dy.new_empty((nbytes // 4,), dtype=_F32)
+        dw_ptr, db_ptr, work_ptr = dweight.data_ptr(), dbias.data_ptr(), work.data_ptr()
     rc = (_lib or library()).eb_layer_norm_backward(
-        rows, cols, dy_ptr, dy_type, lddy, x_ptr, x_type, ldx, xs_ptr, ldxs, _floats(mean, "mean", dev, rows), _floats(rstd, "rstd", dev, rows),
-        _floats(weight, "weight", dev, cols), dx.data_ptr(), cols, None if work is None else dweight.data_ptr(),
-        None if work is None else dbias.data_ptr(), None if work is None else work.data_ptr(), nbytes, _stream(dy, stream))
+        rows, cols, dy_ptr, dy_type, lddy, x_ptr, x_type, ldx, xs_ptr, ldxs, _vector(mean, "mean", _F32, dev, rows),
+        _vector(rstd, "rstd", _F32, dev, rows), _vector(weight, "weight", _F32, dev, cols), dx.data_ptr(), cols, dw_ptr, db_ptr, work_ptr,
+        nbytes, _stream(dy, stream))
     if rc:
         _check(rc)
     return dx, dweight, dbias
@@ -307,11 +304,10 @@ def activation(v, v_scales=None, act: int = EB_ACT_SILU_GATE, out_dtype=None, st
     ``out_dtype`` (bfloat16), or for float8_e4m3fn (h, scales)."""
     cols = _width_of_v(v, act)
     ptr, code, ldv, vs_ptr, ldvs, held = _matrix(v, "v", v_scales)
-    _same_device(v.device, v_scales)
     rows = v.shape[0]
-    h, out_type, ldh, scales = _new(v, rows, cols, out_dtype or _bf16())
-    rc = (_lib or library()).eb_activation(rows, cols, act, ptr, code, ldv, vs_ptr, ldvs, out_type, h.data_ptr(), ldh,
-                                           None if scales is None else scales.data_ptr(), rows, _stream(v, stream))
+    h, out_type, ldh, scales, hs_ptr = _new(v, rows, cols, out_dtype or _BF16)
+    rc = (_lib or library()).eb_activation(rows, cols, act, ptr, code, ldv, vs_ptr, ldvs, out_type, h.data_ptr(), ldh, hs_ptr, rows,
+                                           _stream(v, stream))
     if rc:
         _check(rc)
     return h if scales is None else (h, scales)
@@ -323,18 +319,14 @@ def activation_backward(dh, v, v_scales=None, act: int = EB_ACT_SILU_GATE, out_d
     fp16 or bf16; ``v``, ``v_scales``, ``act``: forward's.  Returns dv, of v's shape and of
     ``out_dtype`` (bfloat16), or for float8_e4m3fn (dv, scales)."""
     cols = _width_of_v(v, act)
-    dh_ptr, dh_type, lddh, *_ = _matrix(dh, "dh", cols=cols)
-    if dh_type == EB_FP8:
-        raise ValueError("dh must be fp32, fp16 or bf16")
+    dh_ptr, dh_type, lddh = _floating(dh, "dh")
     rows = dh.shape[0]
-    if v.shape[0] != rows:
-        raise ValueError("v must have dh's rows")
+    if dh.shape[1] != cols or v.shape[0] != rows or v.get_device() != dh.get_device():
+        raise ValueError("dh must be of h's shape, v on its GPU")
     ptr, code, ldv, vs_ptr, ldvs, held = _matrix(v, "v", v_scales)
-    _same_device(dh.device, v, v_scales)
-    dv, out_type, lddv, scales = _new(dh, rows, v.shape[1], out_dtype or _bf16())
+    dv, out_type, lddv, scales, dvs_ptr = _new(dh, rows, v.shape[1], out_dtype or _BF16)
     rc = (_lib or library()).eb_activation_backward(rows, cols, act, dh_ptr, dh_type, lddh, ptr, code, ldv, vs_ptr, ldvs, out_type,
-                                                    dv.data_ptr(), lddv, None if scales is None else scales.data_ptr(), rows,
-                                                    _stream(dh, stream))
+                                                    dv.data_ptr(), lddv, dvs_ptr, rows, _stream(dh, stream))
     if rc:
         _check(rc)
     return dv if scales is None else (dv, scales)
@@ -347,20 +339,19 @@ def dispatch(x, tokens, x_scales=None, out=None, stream=None):
     Returns [slots, cols] of x's type, in 8 bits (rows, scales); rows of slots without a
     token are not written.  ``out``: the floating-point output, with unit column stride."""
     ptr, code, ldx, xs_ptr, ldxs, held = _matrix(x, "x", x_scales)
-    (rows, cols), M = x.shape, tokens.numel()
-    tokens_ptr = _ints(tokens, "tokens", x.device, M)
-    _same_device(x.device, x_scales, out)
-    scales = None
+    (rows, cols), M, dev = x.shape, tokens.numel(), x.get_device()
+    tokens_ptr = _vector(tokens, "tokens", _I32, dev, M)
+    scales = os_ptr = None
     if out is None:
-        out, _, ldo, scales = _new(x, M, cols, x.dtype)
+        out, _, ldo, scales, os_ptr = _new(x, M, cols, x.dtype)
     else:
         if code == EB_FP8:
             raise ValueError("out is for floating-point rows")
-        if out.dtype != x.dtype or out.shape != (M, cols):
-            raise ValueError("out must be [slots, cols] of x's type")
+        if out.dtype != x.dtype or out.shape != (M, cols) or out.get_device() != dev:
+            raise ValueError("out must be [slots, cols] of x's type, on its GPU")
         ldo = ex._pitch(out, "out")
-    rc = (_lib or library()).eb_dispatch(M, cols, ptr, code, ldx, rows, xs_ptr, ldxs, tokens_ptr, out.data_ptr(), ldo,
-                                         None if scales is None else scales.data_ptr(), M, _stream(x, stream))
+    rc = (_lib or library()).eb_dispatch(M, cols, ptr, code, ldx, rows, xs_ptr, ldxs, tokens_ptr, out.data_ptr(), ldo, os_ptr, M,
+                                         _stream(x, stream))
     if rc:
         _check(rc)
     return out if scales is None else (out, scales)
@@ -371,13 +362,16 @@ def combine(y, slots, weights=None, out_dtype=None, stream=None):
     """Torch convenience for eb_combine.  ``y``: device [rows, cols] of fp32, fp16 or bf16;
     ``slots``: int32 [tokens, K] as ``experts.route`` gives them; ``weights``: fp32
     [tokens, K] or None.  Returns [tokens, cols] of ``out_dtype`` (y's type)."""
-    ptr, code, ldy, *_ = _matrix(y, "y")
-    if code == EB_FP8 or slots.dim() != 2:
-        raise ValueError("y must be fp32, fp16 or bf16, slots 2-D")
-    (rows, cols), (N, K), dev = y.shape, slots.shape, y.device
-    slots_ptr, weights_ptr = _ints(slots, "slots", dev, N, K), _floats(weights, "weights", dev, N, K)
+    ptr, code, ldy = _floating(y, "y")
+    if slots.dim() != 2:
+        raise ValueError("slots must be 2-D")
+    (rows, cols), (N, K), dev = y.shape, slots.shape, y.get_device()
+    slots_ptr, weights_ptr = _vector(slots, "slots", _I32, dev, N, K), _vector(weights, "weights", _F32, dev, N, K)
+    out_type = code if out_dtype is None else _code(out_dtype)
+    if out_type == EB_FP8:
+        raise ValueError("out_dtype must be fp32, fp16 or bf16")
     out = y.new_empty((N, cols), dtype=out_dtype or y.dtype)
-    rc = (_lib or library()).eb_combine(N, K, cols, ptr, code, ldy, rows, slots_ptr, weights_ptr, _code(out.dtype), out.data_ptr(), cols,
+    rc = (_lib or library()).eb_combine(N, K, cols, ptr, code, ldy, rows, slots_ptr, weights_ptr, out_type, out.data_ptr(), cols,
                                         _stream(y, stream))
     if rc:
         _check(rc)
@@ -397,20 +391,17 @@ def combine_backward(dout, y, slots, weights=None, out_dtype=None, stream=None) 
     fp16 or bf16; ``y``, ``slots``, ``weights``: forward's, no slot twice.  dy is of y's
     shape and ``out_dtype`` (y's type; float8_e4m3fn: 8 bits with scales); its rows that are
     no pair's slot are not written."""
-    import torch
-
-    dout_ptr, dout_type, lddo, *_ = _matrix(dout, "dout")
-    ptr, code, ldy, *_ = _matrix(y, "y", cols=dout.shape[1])
-    if EB_FP8 in (code, dout_type) or slots.dim() != 2 or slots.shape[0] != dout.shape[0]:
-        raise ValueError("dout and y must be fp32, fp16 or bf16, slots [tokens, K]")
-    (N, K), (rows, cols), dev = slots.shape, y.shape, dout.device
-    _same_device(dev, y)
-    slots_ptr, weights_ptr = _ints(slots, "slots", dev, N, K), _floats(weights, "weights", dev, N, K)
-    dy, dy_type, lddy, scales = _new(dout, rows, cols, out_dtype or y.dtype)
-    dweights = dout.new_empty((N, K), dtype=torch.float32)
+    dout_ptr, dout_type, lddo = _floating(dout, "dout")
+    ptr, code, ldy = _floating(y, "y")
+    dev, (rows, cols) = dout.get_device(), y.shape
+    if slots.dim() != 2 or dout.shape != (slots.shape[0], cols) or y.get_device() != dev:
+        raise ValueError("dout must be [tokens, columns of y], slots [tokens, K], y on dout's GPU")
+    N, K = slots.shape
+    slots_ptr, weights_ptr = _vector(slots, "slots", _I32, dev, N, K), _vector(weights, "weights", _F32, dev, N, K)
+    dy, dy_type, lddy, scales, dys_ptr = _new(dout, rows, cols, out_dtype or y.dtype)
+    dweights = dout.new_empty((N, K), dtype=_F32)
     rc = (_lib or library()).eb_combine_backward(N, K, cols, dout_ptr, dout_type, lddo, ptr, code, ldy, rows, slots_ptr, weights_ptr, dy_type,
-                                                 dy.data_ptr(), lddy, None if scales is None else scales.data_ptr(), rows,
-                                                 dweights.data_ptr(), _stream(dout, stream))
+                                                 dy.data_ptr(), lddy, dys_ptr, rows, dweights.data_ptr(), _stream(dout, stream))
     if rc:
         _check(rc)
     return CombineGradient(dy, scales, dweights)
@@ -429,23 +420,23 @@ def weight_gradient(dy, x, offsets=None, tokens=None, dy_scales=None, x_scales=N
     ``tokens``: int32 [slots], or None, as ``experts.route`` gives them.  Returns [E, N, K],
     without offsets [N, K], of ``out_dtype`` (float32).  ``out``: the output, contiguous or
     with rows further apart; ``accumulate`` adds to it."""
-    import torch
-
-    if dy.dim() != 2 or x.dim() != 2:
-        raise ValueError("dy and x must be 2-D")
-    (M, N), (rows, K), dev = dy.shape, x.shape, dy.device
     dy_ptr, dy_type, lddy, dys_ptr, lddys, held = _matrix(dy, "dy", dy_scales)
     x_ptr, x_type, ldx, xs_ptr, ldxs, held_too = _matrix(x, "x", x_scales)
-    _same_device(dev, x, dy_scales, x_scales, out)
-    if offsets is not None and (offsets.dim() != 1 or offsets.numel() < 2):
-        raise ValueError("offsets must be int32 [E + 1]")
-    E = 1 if offsets is None else offsets.numel() - 1
-    offsets_ptr, tokens_ptr = _ints(offsets, "offsets", dev, E + 1), _ints(tokens, "tokens", dev, M)
-    shape = (N, K) if offsets is None else (E, N, K)
+    (M, N), (rows, K), dev = dy.shape, x.shape, dy.get_device()
+    if x.get_device() != dev or (out is not None and out.get_device() != dev):
+        raise ValueError("x and out must be on dy's GPU")
+    if offsets is None:
+        E, shape = 1, (N, K)
+    else:
+        E = offsets.numel() - 1
+        if E < 1:
+            raise ValueError("offsets must be int32 [E + 1]")
+        shape = (E, N, K)
+    offsets_ptr, tokens_ptr = _vector(offsets, "offsets", _I32, dev, E + 1), _vector(tokens, "tokens", _I32, dev, M)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs an out")
-        out, ld = dy.new_empty(shape, dtype=out_dtype or torch.float32), K
+        out, ld = dy.new_empty(shape, dtype=out_dtype or _F32), K
     else:
         if out.shape != shape or (out_dtype is not None and out.dtype != out_dtype):
             raise ValueError("out must be [E, N, K], without offsets [N, K], of out_dtype")
@@ -454,11 +445,138 @@ def weight_gradient(dy, x, offsets=None, tokens=None, dy_scales=None, x_scales=N
             ld = out.stride(0)
         elif E > 1 and out.stride(0) != N * ld:
             raise ValueError("out's matrices must be stacked row after row")
+    out_type = _code(out.dtype)
+    if out_type == EB_FP8:
+        raise ValueError("the output is fp32, fp16 or bf16")
     nbytes = _gradient_workspace(M, E, N, K)
-    work = dy.new_empty((nbytes // 4,), dtype=torch.float32) if nbytes else None
+    work = dy.new_empty((nbytes // 4,), dtype=_F32) if nbytes else None
     rc = (_lib or library()).eb_weight_gradient(
-        M, E, N, K, dy_ptr, dy_type, lddy, dys_ptr, lddys, x_ptr, x_type, ldx, rows, xs_ptr, ldxs, tokens_ptr, offsets_ptr, _code(out.dtype),
+        M, E, N, K, dy_ptr, dy_type, lddy, dys_ptr, lddys, x_ptr, x_type, ldx, rows, xs_ptr, ldxs, tokens_ptr, offsets_ptr, out_type,
         int(accumulate), out.data_ptr(), ld, work.data_ptr() if nbytes else None, nbytes, _stream(dy, stream))
     if rc:
         _check(rc)
     return out
+
+
+class Saved(NamedTuple):
+    """What ``ExpertTraining.forward`` leaves for ``backward``: values in 8 bits with their scales,
+    but the experts' rows and what goes by token."""
+    route: object      # experts.Route
+    scores: object     # fp32 [B, experts]
+    x: object          # (values, scales): what the experts and the router read
+    kept: object       # (values, scales) and rstd of the layer norm, or None
+    rstd: object
+    v: object          # (values, scales) before the activation
+    rows: object       # [slots, D] in row_dtype, before they are joined
+
+
+class ExpertGradients(NamedTuple):
+    """What ``ExpertTraining.backward`` returns; of a layer without norm the last two are None."""
+    x: object
+    w_up: object        # fp32, as are the others
+    w_down: object
+    router: object
+    norm_weight: object
+    norm_bias: object
+
+
+class ExpertTraining:
+    """A mixture of experts in training: ``experts.ExpertLayer``'s two layers behind a layer
+    norm, and the gradients of all their weights, from values that wait in 8 bits.
+
+    ``w_up``: [E, N, K], ``w_down``: [E, D, N] (gated [E, D, N / 2]), ``router``: [experts, K]
+    fp32 and ``norm_weight``, ``norm_bias``: fp32 [K] (both None: no norm) are the caller's and
+    stay so: after a change of ``w_up`` or ``w_down`` call ``refresh``, which makes the 8-bit
+    forms that the products take, of each matrix and of its transpose.  ``top``, ``act`` (a
+    ReLU or a gated SiLU), ``mode``, ``bias``, ``groups``, ``top_groups``, ``scale``, ``shard_lo``
+    and ``row_dtype`` are ``ExpertLayer``'s; of several GPUs' experts a GPU's output, and its
+    gradients of x and the router, are shares to be added over the GPUs (and the norm's
+    gradients with that of x: where all GPUs hold the same tokens pass the summed dx on)."""
+
+    def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = ex.EB_SOFTMAX | ex.EB_RENORMALIZE,
+                 norm_weight=None, norm_bias=None, eps: float = 1e-5, bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0,
+                 shard_lo: int = 0, row_dtype=None):
+        if w_up.dim() != 3 or w_down.dim() != 3 or router.dim() != 2:
+            raise ValueError("w_up and w_down must be 3-D, router 2-D")
+        E, N, K = w_up.shape
+        gate = act == EB_ACT_SILU_GATE
+        if act not in (EB_ACT_SILU_GATE, ex.EB_ACT_RELU):
+            raise ValueError("act must be EB_ACT_RELU or EB_ACT_SILU_GATE")
+        if gate and N % 2 or tuple(w_down.shape[::2]) != (E, N // 2 if gate else N) or router.shape[1] != K:
+            raise ValueError("w_up [E, N, K], w_down [E, D, N or N / 2] and router [experts, K] do not fit")
+        if (norm_weight is None) != (norm_bias is None):
+            raise ValueError("norm_weight and norm_bias go together")
+        self.w_up, self.w_down, self.router, self.norm_weight, self.norm_bias = w_up, w_down, router, norm_weight, norm_bias
+        self.E, self.K, self.D, self.top, self.act, self.mode, self.eps = E, K, int(w_down.shape[1]), top, act, mode, eps
+        self.bias, self.groups, self.top_groups, self.scale, self.shard_lo = bias, groups, top_groups, scale, shard_lo
+        self.row_dtype = row_dtype or _BF16
+        self.refresh()
+
+    def refresh(self) -> None:
+        """The weights' 8-bit forms again, from ``w_up`` and ``w_down`` as they are now."""
+        with torch.cuda.device(self.w_up.device):
+            self._up = ex.quantize_fp8(self.w_up.contiguous(), block_rows=BLOCK)
+            self._down = ex.quantize_fp8(self.w_down.contiguous(), block_rows=BLOCK)
+            self._up_t = ex.quantize_fp8(self.w_up.transpose(1, 2).contiguous(), block_rows=BLOCK)
+            self._down_t = ex.quantize_fp8(self.w_down.transpose(1, 2).contiguous(), block_rows=BLOCK)
+
+    def forward(self, x, out_dtype=None):
+        """``x``: device [B, K] of fp32, fp16 or bf16.  Returns (out [B, D] of ``out_dtype``
+        (float32), Saved)."""
+        if x.dim() != 2 or x.shape[1] != self.K or not x.is_cuda:
+            raise ValueError("x must be [B, K] on the GPU")
+        with torch.cuda.device(x.device):
+            kept = rstd = None
+            if self.norm_weight is not None:
+                n = layer_norm(x, self.norm_weight, self.norm_bias, self.eps, out_dtype=x.dtype, checkpoint=True)
+                x, kept, rstd = n.y, (n.kept, n.kept_scales), n.rstd
+            scores = x.float() @ self.router.t()
+            r = ex.route(scores, self.top, self.mode, self.bias, self.groups, self.top_groups, self.scale, self.shard_lo, self.shard_lo + self.E)
+            q = ex.quantize_fp8(x)
+            v = ex.product(*q, *self._up, r.offsets, r.tokens, out_dtype=_FP8)
+            h = activation(*v, act=self.act, out_dtype=_FP8)
+            rows = ex.product(*h, *self._down, r.offsets, out_dtype=self.row_dtype)
+            out = combine(rows, r.slots, r.weights, out_dtype=out_dtype or _F32)
+        return out, Saved(r, scores, q, kept, rstd, v, rows)
+
+    def backward(self, saved: Saved, dout) -> ExpertGradients:
+        """``dout``: [B, D] of fp32, fp16 or bf16, the gradient of forward's output.  dx is of
+        bf16 behind a norm, else fp32."""
+        return self._backward(saved, dout)[0]
+
+    def _backward(self, saved, dout):
+        r = saved.route
+        with torch.cuda.device(dout.device):
+            g = combine_backward(dout, saved.rows, r.slots, r.weights, out_dtype=_FP8)
+            dz = (g.dy, g.dy_scales)
+            dh = ex.product(*dz, *self._down_t, r.offsets, out_dtype=_BF16)
+            dv = activation_backward(dh, *saved.v, act=self.act, out_dtype=_FP8)
+            h = activation(*saved.v, act=self.act, out_dtype=_FP8)  # forward's, made again
+            w_down = weight_gradient(dz[0], h[0], r.offsets, dy_scales=dz[1], x_scales=h[1])
+            w_up = weight_gradient(dv[0], saved.x[0], r.offsets, r.tokens, dy_scales=dv[1], x_scales=saved.x[1])
+            dslots = ex.product(*dv, *self._up_t, r.offsets, out_dtype=_BF16)
+            dscores = self._dscores(saved, g.dweights)
+            dx = combine(dslots, r.slots, out_dtype=_F32) + dscores @ self.router
+            router = weight_gradient(dscores.to(_BF16), saved.x[0], x_scales=saved.x[1])
+            norm_weight = norm_bias = None
+            if self.norm_weight is not None:
+                dx, norm_weight, norm_bias = layer_norm_backward(dx.to(_BF16), saved.kept[0], saved.rstd, x_scales=saved.kept[1],
+                                                                 weight=self.norm_weight)
+        return ExpertGradients(dx, w_up, w_down, router, norm_weight, norm_bias), dict(dz=dz, dh=dh, dv=dv, h=h, dslots=dslots, dweights=g.dweights, dscores=dscores)
+
+    def _dscores(self, saved, dweights):
+        """The router's outputs' gradient from that of the chosen pairs' weights (0 for other GPUs' pairs)."""
+        ids = saved.route.ids
+        at, there = ids.clamp(min=0).long(), ids >= 0
+        sigmoid = self.mode & 0xFF == ex.EB_SIGMOID
+        p = torch.sigmoid(saved.scores) if sigmoid else torch.softmax(saved.scores, 1)
+        chosen = torch.where(there, p.gather(1, at), 0.0)
+        d = dweights * self.scale
+        if self.mode & ex.EB_RENORMALIZE:
+            total = chosen.sum(1, keepdim=True)
+            total = torch.where(total > 0, total, 1.0)
+            d = (d - (d * chosen).sum(1, keepdim=True) / total) / total
+        dp = torch.zeros_like(p).scatter_add_(1, at, torch.where(there, d, 0.0))
+        if sigmoid:
+            return dp * p * (1 - p)
+        return p * (dp - (dp * p).sum(1, keepdim=True))
