@@ -21,7 +21,7 @@
  * the transposed weights.  An "8-bit matrix" is what eb_quantize_fp8 writes with
  * block_rows 1: e4m3 values, 16-byte aligned, rows a multiple of 16 bytes apart,
  * and fp32 scales [ceil(columns/128)][lds], the scale of row r's block b at
- * b * lds + r.  Where a call writes one, the quotients are rounded to fp32
+ * b * lds + r.  A row is read up to the next multiple of 16 columns.  Where a call writes one, the quotients are rounded to fp32
  * before they are to e4m3, and the bytes of a row past its columns are
  * zero up to the next multiple of 16.
  *
@@ -138,9 +138,10 @@ int eb_activation(int64_t rows, int64_t cols, int32_t act, const void *v, int32_
  *                rows (blocks of 128 columns from g's first to u's last).
  *
  *   EB_ACT_RELU: dv = dh where v > 0, else 0.  EB_ACT_SILU_GATE, with
- *   p = 1 / (1 + exp(-g)):  dg = dh * u * p * (1 + g * (1 - p)),  du = dh * g * p
+ *   p = 1 / (1 + exp(-g)):  dg = dh * p * u * (1 + g * (1 - p)),  du = dh * p * g
  *
- * In fp32, rounded once.  Errors as eb_activation.
+ * In fp32, rounded once; p as in eb_activation.  What of dh * p lies below 2^-126 may be
+ * lost.  Errors as eb_activation.
  */
 int eb_activation_backward(int64_t rows, int64_t cols, int32_t act, const void *dh, int32_t dh_type, int64_t lddh,
                            const void *v, int32_t v_type, int64_t ldv, const float *v_scales, int64_t ldvs,
@@ -159,7 +160,8 @@ int eb_activation_backward(int64_t rows, int64_t cols, int32_t act, const void *
  *                >= M, for EB_FP8.
  *
  * Its gradient is eb_combine without weights.  Errors: EB_ERR_INVALID for an
- * argument outside the above, EB_ERR_UNSUPPORTED for sizes past the above,
+ * argument outside the above, EB_ERR_UNSUPPORTED for sizes past the above or past one
+ * launch (2^26 rows of more than 256 bytes or 128 columns, more of shorter ones),
  * EB_ERR_HIP when a launch fails.
  */
 int eb_dispatch(int64_t M, int64_t cols, const void *x, int32_t dtype, int64_t ldx, int64_t x_rows, const float *x_scales,

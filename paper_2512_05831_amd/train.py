@@ -178,8 +178,6 @@ def _matrix(x, what: str, scales):
             raise ValueError(f"{what} is not in 8 bits: it takes no scales")
         return x.data_ptr(), code, ld, None, 0, None
     rows, n = x.shape
-    if rows == 1 and ld % 16:
-        ld = ld + 15 & -16  # a single row has no next one
     blocks = (n + BLOCK - 1) // BLOCK
     if scales is None or scales.dtype != _F32 or scales.shape != (rows, blocks):
         raise ValueError(f"{what} in 8 bits needs its scales, fp32 [rows, ceil(columns/128)]")

@@ -101,6 +101,17 @@ def test_extremes(device):
     assert nan.isnan().tolist() == [[False, True, False, False, False, True, False]]
 
 
+def test_large_gradients_and_small_scales(device):
+    """dh u beyond fp32's range before u's scale, and far below it: the values between are finite."""
+    g = generator(device, 7)
+    for size, scale in ((1e37, 1e-30), (1e-30, 1e-10), (1e-20, 1e18)):
+        v = torch.randn(5, 256, generator=g, device=device)
+        v[:, 128:] *= scale
+        q, s = ex.quantize_fp8(v)
+        dh = torch.randn(5, 128, generator=g, device=device) * size
+        check8(*train.activation_backward(dh, q, s, out_dtype=FP8), *backward(dh.double(), q.double() * s.double().repeat_interleave(128, 1), GATE))
+
+
 def test_backward_is_the_slope(device):
     """Against differences of the definition, in 64 bits."""
     v = torch.randn(4, 300, generator=generator(device, 1), device=device)
