@@ -244,23 +244,9 @@ __device__ __forceinline__ void write_out(T *to, bool accumulate, float v)
     *to = (T)(accumulate ? (float)*to + v : v);
 }
 
-// Four neighbouring outputs of row n from column k on, `left` of them there.
-__device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial, int e, int n, int k, const float *v)
+// Four neighbouring outputs from `place` of dw on, `left` of them there.
+__device__ __forceinline__ void write_values(const GradientArgs &a, int64_t place, int left, const float *v)
 {
-    const int left = a.K - k;
-    if (partial) {
-        float *to = partial + (int64_t)n * a.K + k;
-        if (left >= kQuad) {
-            const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
-            *(i32x4_any *)to = w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < kQuad; ++j)
-                if (j < left) to[j] = v[j];
-        }
-        return;
-    }
-    const int64_t place = ((int64_t)e * a.N + n) * a.lddw + k;
     if (left >= kQuad && !a.accumulate) {
         if (a.out_type == EB_F32) {
             const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
@@ -279,6 +265,22 @@ __device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial
         if (a.out_type == EB_F32) write_out((float *)a.dw + place + j, a.accumulate, v[j]);
         else if (a.out_type == EB_F16) write_out((_Float16 *)a.dw + place + j, a.accumulate, v[j]);
         else write_out((__bf16 *)a.dw + place + j, a.accumulate, v[j]);
+    }
+}
+
+// Those of row n from column k on, or a split's share of them.
+__device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial, int e, int n, int k, const float *v)
+{
+    const int left = a.K - k;
+    if (!partial) return write_values(a, ((int64_t)e * a.N + n) * a.lddw + k, left, v);
+    float *to = partial + (int64_t)n * a.K + k;
+    if (left >= kQuad) {
+        const i32x4_any w = {__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+        *(i32x4_any *)to = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < kQuad; ++j)
+            if (j < left) to[j] = v[j];
     }
 }
 

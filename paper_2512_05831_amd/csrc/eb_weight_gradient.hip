@@ -12,18 +12,34 @@ using namespace eb_gradient;
 
 constexpr int64_t kMostSize = (int64_t)1 << 30;
 
-// The splits' sums added in order.
+// The splits' sums added in order, four neighbours a thread: a workgroup takes rows of
+// dw, or, where those follow each other, all of it as one (2048 x 1000 x 1512 in 4 parts
+// 6.0 us; with a division for every value 7.7).
 __global__ __launch_bounds__(kThreads) void eb_gradient_join(GradientArgs a)
 {
     const int64_t all = (int64_t)a.E * a.N * a.K;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s) v += a.partial[s * all + i];
-        const int64_t place = i / a.K * a.lddw + i % a.K;
-        if (a.out_type == EB_F32) write_out((float *)a.dw + place, a.accumulate, v);
-        else if (a.out_type == EB_F16) write_out((_Float16 *)a.dw + place, a.accumulate, v);
-        else write_out((__bf16 *)a.dw + place, a.accumulate, v);
-    }
+    const bool one = a.lddw == a.K;
+    const int64_t rows = one ? 1 : (int64_t)a.E * a.N, cols = one ? all : a.K;
+    const int64_t parts = one ? gridDim.x : 1, part = one ? blockIdx.x : 0;
+    for (int64_t row = one ? 0 : blockIdx.x; row < rows; row += one ? 1 : gridDim.x)
+        for (int64_t c = (part * kThreads + threadIdx.x) * kQuad; c < cols; c += parts * kThreads * kQuad) {
+            const float *from = a.partial + row * a.K + c;
+            const int left = (int)min(cols - c, (int64_t)kQuad);
+            float v[kQuad] = {};
+#pragma unroll 4
+            for (int s = 0; s < a.splits; ++s, from += all) {
+                if (left == kQuad) {
+                    const i32x4_any w = *(const i32x4_any *)from;
+#pragma unroll
+                    for (int j = 0; j < kQuad; ++j) v[j] += __int_as_float(w[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kQuad; ++j)
+                        if (j < left) v[j] += from[j];
+                }
+            }
+            write_values(a, row * a.lddw + c, left, v);
+        }
 }
 
 int check_sizes(const char *who, int64_t M, int32_t E, int64_t N, int64_t K)
@@ -133,8 +149,8 @@ int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, c
     const int64_t grid = square > kMax32 / E / a.splits ? kMax32 : square * E * a.splits;
     if (int rc = launch(who, choice.kernel, grid, kThreads, &a, stream)) return rc;
     if (need == 0) return EB_OK;
-    const int64_t all = E * N * K;
-    return launch(who, (void *)eb_gradient_join, std::min<int64_t>((all + kThreads - 1) / kThreads, 8192), kThreads, &a, stream);
+    const int64_t groups = lddw == K ? (E * N * K + kThreads * kQuad - 1) / (kThreads * kQuad) : E * N;
+    return launch(who, (void *)eb_gradient_join, std::min<int64_t>(groups, 8192), kThreads, &a, stream);
 }
 
 int workspace_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, size_t *bytes)
