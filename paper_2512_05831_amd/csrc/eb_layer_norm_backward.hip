@@ -284,8 +284,10 @@ int64_t groups_of(int64_t rows, int64_t cols)
         const int64_t strips = (cols + kThreads * kEach - 1) / (kThreads * kEach);
         return std::min<int64_t>(std::max<int64_t>(1, kMostGroups / strips), (rows + 7) / 8);
     }
-    const int64_t held = cols > 2 * kStride ? 1 : 4;
-    return std::min<int64_t>(cols > 8 * kStride ? 384 : kMostGroups, (rows + held - 1) / held);
+    // Every workgroup leaves sums of all columns: as many as fill the GPU, then one for
+    // each eight rows (2048 x 1512 fp16: 256 workgroups 15.2 us with the joining, 768 16.4).
+    const int64_t held = cols > 2 * kStride ? 1 : 4, most = cols > 8 * kStride ? 384 : kMostGroups;
+    return std::min({most, std::max<int64_t>(256, rows / 8), (rows + held - 1) / held});
 }
 
 struct RowPlan {

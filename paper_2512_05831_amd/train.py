@@ -553,6 +553,8 @@ class ExpertTraining:
             w_down = weight_gradient(dz[0], h[0], r.offsets, dy_scales=dz[1], x_scales=h[1])
             w_up = weight_gradient(dv[0], saved.x[0], r.offsets, r.tokens, dy_scales=dv[1], x_scales=saved.x[1])
             dslots = ex.product(*dv, *self._up_t, r.offsets, out_dtype=_BF16)
+            # In bf16, whose range is fp32's: the rows' gradients before and after they are joined
+            # (each comes of 4-bit values), and what the router's gradient and the norm's take.
             dscores = self._dscores(saved, g.dweights)
             dx = combine(dslots, r.slots, out_dtype=_F32) + dscores @ self.router
             router = weight_gradient(dscores.to(_BF16), saved.x[0], x_scales=saved.x[1])
