@@ -135,14 +135,24 @@ struct Panel {
 
 __device__ const i32x4 kZeros = {0, 0, 0, 0};
 
-// 16 bytes of a row that may have any alignment; zeros past `left` bytes.
-__device__ __forceinline__ i32x4 load_any(const char *at, int64_t left)
+// The first `left` bytes (below 16) at an address of any alignment, zeros behind them.
+__device__ __forceinline__ i32x4 load_some(const char *at, uint32_t left)
 {
-    if (left >= 16) return *(const i32x4_any *)at;
     uint32_t w[4] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (uint32_t i = 0; i < 8; ++i)
         if (2 * i < left) w[i / 2] |= (uint32_t)((const uint16_t *)at)[i] << i % 2 * 16;
+    return i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+
+// 16 bytes without the first `n` (even, below 16), zeros behind the others.
+__device__ __forceinline__ i32x4 drop_bytes(i32x4 v, uint32_t n)
+{
+    uint32_t w[5] = {(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3], 0};
+    if (n & 8) w[0] = w[2], w[1] = w[3], w[2] = 0, w[3] = 0;
+    if (n & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], n & 2);
     return i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
@@ -285,7 +295,9 @@ __device__ __forceinline__ void write_quad(const GradientArgs &a, float *partial
 }
 
 // kDirect: 16-bit operands lie so that 16 bytes can be copied to LDS at a time (8-bit
-// ones always do); else they go through registers.
+// ones always do); else they go through registers, in narrow tiles, whose sums leave
+// room for them (12000 slots by 2047 x 2047, fp16 by 8 bits: 537 us in wide ones, 249 in
+// narrow ones; bf16 270 and 293; by 2048 x 2048, copied, 191 and 133).
 template <typename D, typename X, bool kExact, bool kDirect, int kSharedTile>
 __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) void eb_gradient_tile(GradientArgs a)
 {
@@ -367,7 +379,9 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
     // dy's rows follow each other: where the thread's first one is from a step's start on.
     constexpr uint32_t kRowsOfDy = S::kOwnX ? SharedPanel::kRows : OwnPanel::kRows;
     const int64_t dy_ld = S::kOwnX ? a.shared_ld : a.own_ld, of_dy = thread / (kThreads / kRowsOfDy) * dy_ld;
-    auto copy = [&](auto &panel, auto direct, auto of_x, i32x4 *raw, const char *base, uint32_t left, int64_t m, int of) {
+    // Bytes before a piece that are read with it, where it ends past its row.
+    auto back_of = [](uint32_t byte, uint32_t left) { return byte < left && byte + 16 > left ? byte + 16 - left : 0; };
+    auto copy = [&](auto &panel, auto direct, auto of_x, i32x4 *raw, const char *base, uint32_t left, int64_t m, int of, bool few) {
         using P = std::remove_reference_t<decltype(panel)>;
         const char *dy = base + m * dy_ld;
 #pragma unroll
@@ -381,26 +395,35 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                                  (__attribute__((address_space(3))) void *)(panel.bytes + (p * kThreads + wave * kWave) * 16), 16, 0, 0);
             } else {
-                raw[p] = load_any(from, x < 0 ? 0 : (int64_t)left - byte);
+                // Whole 16 bytes in any case, so that no load waits for another: a row's last
+                // ones together with what is before them, which is dropped when they are stored.
+                const bool there = x >= 0 && byte < left;
+                if (few) raw[p] = load_some(there ? from : zeros, there ? left - byte : 0);
+                else raw[p] = *(const i32x4_any *)(there ? from - back_of(byte, left) : zeros);
             }
         }
     };
     auto left_of = [](int cols, int first, int width, int size) { return (uint32_t)(min(cols - first, width) * size); };
     const uint32_t own_left = left_of(a.own_cols, own0, kOwnTile, sizeof(Own)), shared_left = left_of(a.shared_cols, shared0, kSharedTile, sizeof(Shared));
+    const bool own_few = a.own_cols < 8, shared_few = a.shared_cols < 8; // rows of less than 16 bytes
     auto copy_step = [&](auto &own, auto &shared, int64_t m, int of) {
-        copy(own, std::bool_constant<kOwnDirect>(), std::bool_constant<S::kOwnX>(), own_raw, a.own + (int64_t)own0 * sizeof(Own), own_left, m, of);
+        copy(own, std::bool_constant<kOwnDirect>(), std::bool_constant<S::kOwnX>(), own_raw, a.own + (int64_t)own0 * sizeof(Own), own_left, m, of, own_few);
         copy(shared, std::bool_constant<kSharedDirect>(), std::bool_constant<!S::kOwnX>(), shared_raw, a.shared + (int64_t)shared0 * sizeof(Shared),
-             shared_left, m, of);
+             shared_left, m, of, shared_few);
+    };
+    auto store = [&](auto &panel, const i32x4 *raw, uint32_t left, bool few) {
+        using P = std::remove_reference_t<decltype(panel)>;
+#pragma unroll
+        for (int p = 0; p < P::kCopies; ++p) {
+            const uint32_t row = p * P::kRows + thread / P::kPieces, back = few ? 0 : back_of(P::piece_of(row, thread % P::kPieces) * 16, left);
+            i32x4 v = raw[p];
+            if (__any(back != 0)) v = drop_bytes(v, back);
+            *(i32x4 *)(panel.bytes + (p * kThreads + thread) * 16) = v;
+        }
     };
     auto store_step = [&](auto &own, auto &shared) { // what went through registers
-        if constexpr (!kOwnDirect) {
-#pragma unroll
-            for (int p = 0; p < OwnPanel::kCopies; ++p) *(i32x4 *)(own.bytes + (p * kThreads + t) * 16) = own_raw[p];
-        }
-        if constexpr (!kSharedDirect) {
-#pragma unroll
-            for (int p = 0; p < SharedPanel::kCopies; ++p) *(i32x4 *)(shared.bytes + (p * kThreads + t) * 16) = shared_raw[p];
-        }
+        if constexpr (!kOwnDirect) store(own, own_raw, own_left, own_few);
+        if constexpr (!kSharedDirect) store(shared, shared_raw, shared_left, shared_few);
     };
 
     // x's columns are the rows of the unit's result, of which a lane has four neighbours.
@@ -519,7 +542,7 @@ Choice choice_of(bool exact, bool direct)
     if (direct && exact) return {(void *)eb_gradient_tile<D, X, true, true, kSharedTile>, S::kOwnX};
     if constexpr (!S::kAsItIs || S::kScaled)
         if (direct) return {(void *)eb_gradient_tile<D, X, false, true, kSharedTile>, S::kOwnX};
-    if constexpr (sizeof(D) == 2 || sizeof(X) == 2) {
+    if constexpr (kSharedTile == 64 && (sizeof(D) == 2 || sizeof(X) == 2)) {
         if (exact) return {(void *)eb_gradient_tile<D, X, true, false, kSharedTile>, S::kOwnX};
         if constexpr (!S::kAsItIs || S::kScaled) return {(void *)eb_gradient_tile<D, X, false, false, kSharedTile>, S::kOwnX};
     }
@@ -533,9 +556,9 @@ Choice choice_of(int32_t x_type, bool exact, bool direct, bool narrow)
         return x_type == EB_FP8   ? choice_of<D, Fp8, 64>(exact, direct)
                : x_type == EB_F16 ? choice_of<D, _Float16, 64>(exact, direct)
                                   : choice_of<D, Bf16, 64>(exact, direct);
-    return x_type == EB_FP8   ? choice_of<D, Fp8, 128>(exact, direct)
-           : x_type == EB_F16 ? choice_of<D, _Float16, 128>(exact, direct)
-                              : choice_of<D, Bf16, 128>(exact, direct);
+    return x_type == EB_FP8   ? choice_of<D, Fp8, 128>(exact, true)
+           : x_type == EB_F16 ? choice_of<D, _Float16, 128>(exact, true)
+                              : choice_of<D, Bf16, 128>(exact, true);
 }
 
 // By dy's type, each in a source of its own.

@@ -111,7 +111,8 @@ int gradient_impl(const char *who, int64_t M, int32_t E, int64_t N, int64_t K, c
         return type == EB_FP8 || ((uintptr_t)p % 16 == 0 && cols % 8 == 0 && ld % 8 == 0);
     };
     const bool direct = whole(dy, dy_type, N, lddy) && whole(x, x_type, K, ldx);
-    const auto [narrow, splits] = cut_of(M, E, N, K);
+    const auto [few, splits] = cut_of(M, E, N, K);
+    const bool narrow = few || !direct;
     const Choice choice = dy_type == EB_FP8   ? choice_fp8(x_type, exact, direct, narrow)
                           : dy_type == EB_F16 ? choice_f16(x_type, exact, direct, narrow)
                                               : choice_bf16(x_type, exact, direct, narrow);
