@@ -42,18 +42,27 @@ __device__ __forceinline__ float sigmoid(float g)
     return __builtin_amdgcn_rcpf(1.f + fmaf(e, l * 0.693147182f, e));
 }
 
-// Columns c .. c + 7 of v that lie in [lo, hi); zeros for the others.
+// Columns c .. c + 7 of v that lie in [lo, hi), to be settled where they are used.
 template <bool kRagged, typename T>
 __device__ __forceinline__ Raw<T> load_v(const ActArgs &a, int64_t row, int c, int lo, int hi)
 {
-    return load_raw<kRagged>((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
+    return fetch_raw<kRagged>((const T *)a.v + row * a.ldv + lo, c - lo, hi - lo);
 }
 
-template <bool kRagged, typename T>
-__device__ __forceinline__ void widen_v(const ActArgs &a, int64_t row, int c, int hi, const Raw<T> &r, float *f)
+// The scales of those, and their values.
+template <bool kAcross, typename T>
+__device__ __forceinline__ TwoScales scales_v(const ActArgs &a, int64_t row, int c, int hi)
 {
-    widen8(r, f);
-    if constexpr (sizeof(T) == 1) scale8<kRagged>(f, a.v_scales, row, c, hi);
+    if constexpr (sizeof(T) == 1) return load_scales<kAcross>(a.v_scales, row, c, hi);
+    else return {};
+}
+
+// (c and cols within the part.)
+template <bool kRagged, bool kAcross, bool kBelow = false, typename T>
+__device__ __forceinline__ void widen_v(const Raw<T> &r, const TwoScales &t, int c, int cols, float *f)
+{
+    widen8(settle_raw<kRagged, kBelow>(r, c, cols), f);
+    if constexpr (sizeof(T) == 1) scale8<kAcross>(f, t);
 }
 
 template <typename T, bool kRagged>
@@ -69,15 +78,17 @@ __global__ __launch_bounds__(kThreads) void eb_activate(ActArgs a)
         if (b0 + s >= a.blocks) return;
         float g[kEach], h[kEach];
         const Raw<T> first = load_v<kRagged, T>(a, row, c, 0, cols);
+        const TwoScales of_g = scales_v<false, T>(a, row, c, cols);
         if (a.gate) {
             const Raw<T> second = load_v<kRagged, T>(a, row, cols + c, cols, width);
+            const TwoScales of_u = scales_v<kRagged, T>(a, row, cols + c, width);
             float u[kEach];
-            widen_v<kRagged>(a, row, c, cols, first, g);
-            widen_v<kRagged>(a, row, cols + c, width, second, u);
+            widen_v<kRagged, false>(first, of_g, c, cols, g);
+            widen_v<kRagged, kRagged>(second, of_u, c, cols, u);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
         } else {
-            widen_v<kRagged>(a, row, c, cols, first, g);
+            widen_v<kRagged, false>(first, of_g, c, cols, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) h[i] = g[i] > 0.f ? g[i] : g[i] == g[i] ? 0.f : g[i];
         }
@@ -106,22 +117,24 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back(ActArgs a)
         const int c = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
         float dh[kEach], g[kEach], d[kEach];
-        const Raw<D> of_h = load_raw<kRagged>((const D *)a.dh + row * a.lddh, c, cols);
+        const Raw<D> of_h = fetch_raw<kRagged>((const D *)a.dh + row * a.lddh, c, cols);
         const Raw<T> first = load_v<kRagged, T>(a, row, c, 0, cols);
+        const TwoScales scales_g = scales_v<false, T>(a, row, c, cols);
         if (!a.gate) {
-            widen8(of_h, dh);
-            widen_v<kRagged>(a, row, c, cols, first, g);
+            widen8(settle_raw<kRagged>(of_h, c, cols), dh);
+            widen_v<kRagged, false>(first, scales_g, c, cols, g);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) d[i] = g[i] > 0.f ? dh[i] : 0.f;
             store_out<kRagged>(a.out, row, c, cols, d);
             continue;
         }
         const Raw<T> second = load_v<kRagged, T>(a, row, cols + c, cols, width);
+        const TwoScales scales_u = scales_v<kRagged, T>(a, row, cols + c, width);
         float u[kEach], e[kEach];
-        widen8(of_h, dh);
-        widen_v<kRagged>(a, row, c, cols, first, g);
+        widen8(settle_raw<kRagged>(of_h, c, cols), dh);
+        widen_v<kRagged, false>(first, scales_g, c, cols, g);
         const bool fp8 = a.out.type == EB_FP8; // whole blocks
-        widen_v<kRagged>(a, row, cols + c, width, second, u);
+        widen_v<kRagged, kRagged>(second, scales_u, c, cols, u);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float2 v = d_gate(dh[i], g[i], u[i]);
@@ -210,8 +223,8 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_blocks(ActArgs a)
 }
 
 // A lane of a block of dv, which may lie across the border, takes dg where its
-// columns are g's, du where they are u's; dh, g and u are read for each.
-template <typename D, typename T>
+// columns are g's, du where they are u's; dh and g are read for each.
+template <typename D, typename T, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
 {
     const uint32_t strips = (a.blocks + kSteps - 1) / kSteps;
@@ -222,25 +235,32 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
     for (int s = 0; s < kSteps; ++s) {
         const int at = (b0 + s) * kBlock + threadIdx.x % kLanes * kEach;
         if (b0 + s >= a.blocks) return;
-        float d[kEach] = {}, dh[kEach], g[kEach], u[kEach];
-        auto take = [&](int c, bool first) { // columns c on of dg, or of du
-            const Raw<D> of_h = load_raw<true>((const D *)a.dh + row * a.lddh, c, cols);
-            const Raw<T> of_g = load_v<true, T>(a, row, c, 0, cols), of_u = load_v<true, T>(a, row, cols + c, cols, width);
-            widen8(of_h, dh);
-            widen_v<true>(a, row, c, cols, of_g, g);
-            // (Of du's first chunk some columns lie before u, and before dh and g: zeros.)
-            widen8(of_u, u);
-            if (sizeof(T) == 1 && first) scale8<true>(u, a.v_scales, row, cols + c, width);
+        float d[kEach] = {};
+        // Columns c on of dg, or of du; those outside [0, cols) are another's, or padding.
+        auto take = [&](int c, bool first, auto aligned) {
+            constexpr bool kAcross = kRagged && !decltype(aligned)::value;
+            const Raw<D> of_h = fetch_raw<kRagged>((const D *)a.dh + row * a.lddh, c, cols);
+            const Raw<T> of_g = load_v<kRagged, T>(a, row, c, 0, cols), of_u = load_v<kRagged, T>(a, row, cols + c, cols, width);
+            const TwoScales scales_g = scales_v<kAcross, T>(a, row, c, cols), scales_u = scales_v<kRagged, T>(a, row, cols + c, width);
+            float dh[kEach], g[kEach], u[kEach];
+            widen8(settle_raw<kRagged, kAcross>(of_h, c, cols), dh);
+            widen_v<kRagged, kAcross, kAcross>(of_g, scales_g, c, cols, g);
+            widen_v<kRagged, kRagged, kAcross>(of_u, scales_u, c, cols, u);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                if (c + i < 0 || c + i >= cols) continue;
                 const float2 v = d_gate(dh[i], g[i], u[i]);
-                d[i] = first ? v.x : v.y;
+                const float one = first ? v.x : v.y;
+                if (!kRagged) d[i] = one; // of columns past the last zero
+                else if (c + i >= 0 && c + i < cols) d[i] = one;
             }
         };
-        if (at < cols) take(at, true);
-        if (at + kEach > cols) take(at - cols, false);
-        store_out<true>(a.out, row, at, width, d);
+        if constexpr (!kRagged) {
+            take(at < cols ? at : at - cols, at < cols, std::true_type());
+        } else {
+            if (at < cols) take(at, true, std::true_type());
+            if (at + kEach > cols) take(at - cols, false, std::false_type()); // both, where the border lies within
+        }
+        store_out<kRagged>(a.out, row, at, width, d);
     }
 }
 
@@ -294,7 +314,7 @@ int act_impl(const char *who, int64_t rows, int64_t cols, int32_t act, const voi
 template <typename D, typename T>
 void *back_kernel(bool across, bool ragged)
 {
-    if (across) return (void *)eb_activate_back_across<D, T>;
+    if (across) return ragged ? (void *)eb_activate_back_across<D, T, true> : (void *)eb_activate_back_across<D, T, false>;
     return ragged ? (void *)eb_activate_back<D, T, true> : (void *)eb_activate_back<D, T, false>;
 }
 

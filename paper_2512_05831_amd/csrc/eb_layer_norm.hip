@@ -140,10 +140,10 @@ __global__ __launch_bounds__(kThreads, kSteps > 4 ? 4 : 6) void eb_layer_norm_ro
         {
             Raw<T> raw[kSteps];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) raw[i] = load_raw<kRagged>(x, first + i * kAll, cols);
+            for (int i = 0; i < kSteps; ++i) raw[i] = fetch_raw<kRagged>(x, first + i * kAll, cols);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                widen8(raw[i], f[i]);
+                widen8(settle_raw<kRagged>(raw[i], first + i * kAll, cols), f[i]);
                 sum = add(f[i], sum);
             }
         }

@@ -87,8 +87,8 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int c = first + i * kAll;
-            r.dy[i] = load_raw<kRagged>(dy, c, cols);
-            r.x[i] = load_raw<kRagged>(x, c, cols);
+            r.dy[i] = fetch_raw<kRagged>(dy, c, cols);
+            r.x[i] = fetch_raw<kRagged>(x, c, cols);
             if constexpr (kFp8) r.scale[i] = a.x_scales.p[(c < cols ? c / kBlock : 0) * a.x_scales.ld + row];
         }
         r.rstd = a.rstd[row];
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(kWaves > 4 ? kWaves * kWave : kThreads) void eb_lay
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int c = first + i * kAll;
-            widen8(now.dy[i], g[i]);
-            widen8(now.x[i], n[i]);
+            widen8(settle_raw<kRagged>(now.dy[i], c, cols), g[i]);
+            widen8(settle_raw<kRagged>(now.x[i], c, cols), n[i]);
             const float scale = kFp8 && c < cols ? now.scale[i] : 0.f;
 #pragma unroll
             for (int j = 0; j < kEach; ++j) n[i][j] = kFp8 ? n[i][j] * scale : (n[i][j] - now.mean) * now.rstd;

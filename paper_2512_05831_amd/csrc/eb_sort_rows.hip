@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
                 const int64_t s = k0 + i < a.K ? slots[k0 + i] : -1;
                 there[i] = s >= 0 && s < a.y_rows;
                 if (there[i]) {
-                    raw[i] = load_raw<kRagged>(y + s * a.ldy, c, a.cols);
+                    raw[i] = fetch_raw<kRagged>(y + s * a.ldy, c, a.cols);
                     w[i] = weights ? weights[k0 + i] : 1.f;
                 }
             }
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void eb_combine_rows(CombineArgs a)
             for (int i = 0; i < kAhead; ++i) {
                 if (!there[i]) continue;
                 float f[kEach];
-                widen8(raw[i], f);
+                widen8(settle_raw<kRagged>(raw[i], c, a.cols), f);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) sum[j] = fmaf(w[i], f[j], sum[j]);
             }
@@ -134,10 +134,10 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
         float d[kSteps][kEach];
         int most[kSteps];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) raw[i] = load_raw<kRagged>(dout, first + i * kStride, cols);
+        for (int i = 0; i < kSteps; ++i) raw[i] = fetch_raw<kRagged>(dout, first + i * kStride, cols);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            widen8(raw[i], d[i]);
+            widen8(settle_raw<kRagged>(raw[i], first + i * kStride, cols), d[i]);
             if (fp8) most[i] = most_of_block(most8(d[i]));
         }
         for (int k = 0; k < a.K; ++k) {
@@ -150,12 +150,12 @@ __global__ __launch_bounds__(kThreads) void eb_combine_back(CombineArgs a)
                 const T *y = (const T *)a.y + s * a.ldy;
                 Raw<T> other[kSteps];
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) other[i] = load_raw<kRagged>(y, first + i * kStride, cols);
+                for (int i = 0; i < kSteps; ++i) other[i] = fetch_raw<kRagged>(y, first + i * kStride, cols);
                 float dot = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
                     float f[kEach];
-                    widen8(other[i], f);
+                    widen8(settle_raw<kRagged>(other[i], first + i * kStride, cols), f);
 #pragma unroll
                     for (int j = 0; j < kEach; ++j) dot = fmaf(d[i][j], f[j], dot);
                 }

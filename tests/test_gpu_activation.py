@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import eb, experts as ex, train
-from train_util import FP8, U, WIDE, as_type, check, check8, generator
+from train_util import EVERY_REMAINDER, FP8, U, WIDE, among_nans, as_type, check, check8, generator
 
 pytestmark = pytest.mark.gpu
 GATE, RELU = ex.EB_ACT_SILU_GATE, ex.EB_ACT_RELU
@@ -158,3 +158,15 @@ def test_no_rows_and_refusals(device):
         with pytest.raises(eb.EbError) as e:
             train.activation(v, act=act)
         assert e.value.code == eb.EB_ERR_INVALID
+
+
+@pytest.mark.parametrize("cols", EVERY_REMAINDER)
+@pytest.mark.parametrize("act", [GATE, RELU])
+def test_every_remainder(cols, act, device):
+    """Rows that end anywhere in a chunk of 8, with NaN before and behind them."""
+    for v_type in (FP8, torch.float32, torch.bfloat16):
+        v, s, values, dh = inputs(19, cols, act, v_type, device)
+        v = v if v_type == FP8 else among_nans(v)
+        for out in (FP8, torch.float16):
+            for of_h in (torch.float32, torch.float16):
+                check_both(v, s, values, among_nans(dh.to(of_h)), act, out)

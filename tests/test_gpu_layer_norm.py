@@ -12,7 +12,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import eb, experts as ex, train
-from train_util import FP8, U, WIDE, as_type, check, check8, generator
+from train_util import EVERY_REMAINDER, FP8, U, WIDE, among_nans, as_type, check, check8, generator
 
 pytestmark = pytest.mark.gpu
 SIZES = [(1, 1), (1, 128), (3, 7), (5, 511), (4, 512), (7, 513), (9, 1000), (17, 1024), (33, 1512), (6, 2049), (40, 3328), (3, 4096), (2, 4097),
@@ -265,3 +265,15 @@ def test_refusals(device):
         with pytest.raises(eb.EbError) as e:
             train.layer_norm(x, eps=eps)
         assert e.value.code == eb.EB_ERR_INVALID
+
+
+@pytest.mark.parametrize("cols", EVERY_REMAINDER)
+@pytest.mark.parametrize("dtype", WIDE)
+def test_every_remainder(cols, dtype, device):
+    """Rows that end anywhere in a chunk of 8, with NaN before and behind them."""
+    x, w, b = inputs(19, cols, dtype, device)
+    x = among_nans(x)
+    dy = among_nans((torch.randn(19, cols, generator=generator(device, cols), device=device) * 0.1).to(dtype))
+    r = check_forward(x, w, b, 1e-5, FP8, statistics=True, checkpoint=True)
+    check_backward(dy, r.kept, r.kept_scales, None, r.rstd, w)
+    check_backward(dy, x, None, r.mean, r.rstd, w)

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2512_05831_amd import eb, experts as ex, train
-from train_util import FP8, U, WIDE, as_type, check, check8, generator, route_of
+from train_util import EVERY_REMAINDER, FP8, U, WIDE, among_nans, as_type, check, check8, generator, route_of
 
 pytestmark = pytest.mark.gpu
 WIDTHS = [1, 3, 8, 16, 31, 64, 100, 128, 129, 512, 513, 1000, 1024, 1512, 2048, 2100, 4096, 5000]
@@ -186,3 +186,16 @@ def test_refusals(device):
     with pytest.raises(eb.EbError) as e:
         train.combine(x, torch.zeros(2, 65, dtype=torch.int32, device=device))
     assert e.value.code == eb.EB_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("cols", EVERY_REMAINDER)
+@pytest.mark.parametrize("dtype", WIDE)
+def test_every_remainder(cols, dtype, device):
+    """Rows that end anywhere in a chunk of 8, with NaN before and behind them."""
+    r = route_of(13, 6, 3, device, cols)
+    g = generator(device, cols)
+    y = among_nans(torch.randn(39, cols, generator=g, device=device).to(dtype))
+    dout = among_nans(torch.randn(13, cols, generator=g, device=device).to(dtype))
+    check(train.combine(y, r.slots, r.weights, out_dtype=dtype), *joined(y, r.slots, r.weights), dtype)
+    for out in (FP8, dtype):
+        check_gradients(dout, y, r.slots, r.weights, out)
