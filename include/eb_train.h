@@ -21,9 +21,9 @@
  * the transposed weights.  An "8-bit matrix" is what eb_quantize_fp8 writes with
  * block_rows 1: e4m3 values, 16-byte aligned, rows a multiple of 16 bytes apart,
  * and fp32 scales [ceil(columns/128)][lds], the scale of row r's block b at
- * b * lds + r.  A row is read up to the next multiple of 16 columns.  Where a call writes one, the quotients are rounded to fp32
- * before they are to e4m3, and the bytes of a row past its columns are
- * zero up to the next multiple of 16.
+ * b * lds + r.  A row is read up to the next multiple of 16 columns.  Where a
+ * call writes one, the quotients are rounded to fp32 before they are to e4m3,
+ * and the bytes of a row past its columns are zero up to the next multiple of 16.
  *
  * The conventions of include/eb.h hold: return codes, eb_last_error, no
  * exceptions, no allocation, no host synchronisation, borrowed device buffers,

@@ -489,7 +489,8 @@ class ExpertTraining:
     ReLU or a gated SiLU), ``mode``, ``bias``, ``groups``, ``top_groups``, ``scale``, ``shard_lo``
     and ``row_dtype`` are ``ExpertLayer``'s; of several GPUs' experts a GPU's output, and its
     gradients of x and the router, are shares to be added over the GPUs (and the norm's
-    gradients with that of x: where all GPUs hold the same tokens pass the summed dx on)."""
+    gradients with that of x: where all GPUs hold the same tokens pass the summed dx on).
+    Torch records nothing of the calls, also where weights or inputs require gradients."""
 
     def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = ex.EB_SOFTMAX | ex.EB_RENORMALIZE,
                  norm_weight=None, norm_bias=None, eps: float = 1e-5, bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0,
@@ -508,16 +509,26 @@ class ExpertTraining:
         self.E, self.K, self.D, self.top, self.act, self.mode, self.eps = E, K, int(w_down.shape[1]), top, act, mode, eps
         self.bias, self.groups, self.top_groups, self.scale, self.shard_lo = bias, groups, top_groups, scale, shard_lo
         self.row_dtype = row_dtype or _BF16
-        self.refresh()
+        with torch.no_grad(), torch.cuda.device(w_up.device):
+            self._up, self._down, self._up_t, self._down_t = (ex.quantize_fp8(w.contiguous(), block_rows=BLOCK) for w in self._forms())
 
+    def _forms(self):
+        return self.w_up, self.w_down, self.w_up.transpose(1, 2), self.w_down.transpose(1, 2)
+
+    @torch.no_grad()
     def refresh(self) -> None:
-        """The weights' 8-bit forms again, from ``w_up`` and ``w_down`` as they are now."""
+        """The weights' 8-bit forms again, from ``w_up`` and ``w_down`` as they are now: in place,
+        so that a captured graph reads the new ones, and may hold the call."""
         with torch.cuda.device(self.w_up.device):
-            self._up = ex.quantize_fp8(self.w_up.contiguous(), block_rows=BLOCK)
-            self._down = ex.quantize_fp8(self.w_down.contiguous(), block_rows=BLOCK)
-            self._up_t = ex.quantize_fp8(self.w_up.transpose(1, 2).contiguous(), block_rows=BLOCK)
-            self._down_t = ex.quantize_fp8(self.w_down.transpose(1, 2).contiguous(), block_rows=BLOCK)
+            for w, (q, scales) in zip(self._forms(), (self._up, self._down, self._up_t, self._down_t)):
+                if w.shape != q.shape or w.device != q.device:
+                    raise ValueError("w_up and w_down must keep their shapes and GPU")
+                w = w.contiguous()
+                E, rows, cols = w.shape
+                ex.eb_quantize_fp8(E, rows, cols, w.data_ptr(), _code(w.dtype), cols, BLOCK, q.data_ptr(), cols + 15 & -16,
+                                   scales.data_ptr(), 0, _stream(w, None))
 
+    @torch.no_grad()
     def forward(self, x, out_dtype=None):
         """``x``: device [B, K] of fp32, fp16 or bf16.  Returns (out [B, D] of ``out_dtype``
         (float32), Saved)."""
@@ -542,6 +553,7 @@ class ExpertTraining:
         bf16 behind a norm, else fp32."""
         return self._backward(saved, dout)[0]
 
+    @torch.no_grad()
     def _backward(self, saved, dout):
         r = saved.route
         with torch.cuda.device(dout.device):

@@ -172,6 +172,60 @@ def test_refresh(device):
     assert torch.equal(layer.forward(x)[0], 2 * before)
 
 
+def test_refresh_and_a_captured_graph(device):
+    """A graph captured before weights changed reads their new forms; one that holds refresh makes them."""
+    layer = layer_of(4, 200, 72, 64, 2, device)
+    x = torch.randn(20, 200, generator=generator(device, 2), device=device)
+    side = torch.cuda.Stream(device)
+    side.wait_stream(torch.cuda.current_stream(device))
+    with torch.cuda.stream(side):
+        layer.forward(x)
+        layer.refresh()
+    torch.cuda.synchronize()
+    graph, both = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out, _ = layer.forward(x)
+    with torch.cuda.graph(both, stream=side):
+        layer.refresh()
+        fresh, _ = layer.forward(x)
+    for replay in range(3):
+        layer.w_up += 0.01 * torch.randn(layer.w_up.shape, generator=generator(device, 5 + replay), device=device)
+        layer.w_down *= 1.5
+        layer.refresh()
+        other = train.ExpertTraining(layer.w_up, layer.w_down, layer.router, 2, norm_weight=layer.norm_weight, norm_bias=layer.norm_bias)
+        want = other.forward(x)[0]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layer.forward(x)[0], want) and torch.equal(out, want), replay
+        layer.w_down *= 0.5
+        want = train.ExpertTraining(layer.w_up, layer.w_down, layer.router, 2, norm_weight=layer.norm_weight,
+                                    norm_bias=layer.norm_bias).forward(x)[0]
+        torch.cuda.synchronize()
+        both.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(fresh, want), replay
+    layer.w_up = layer.w_up[:, :, :128]
+    with pytest.raises(ValueError):
+        layer.refresh()
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_weights_that_require_gradients(norm, device):
+    """Torch records nothing: what is returned and kept holds no graph."""
+    plain, layer = (layer_of(8, 256, 128, 64, 2, device, norm=norm) for _ in range(2))
+    for w in (layer.w_up, layer.w_down, layer.router, *((layer.norm_weight, layer.norm_bias) if norm else ())):
+        w.requires_grad_(True)
+    x, dout = torch.randn(50, 256, generator=generator(device, 2), device=device), torch.randn(50, 64, generator=generator(device, 3), device=device)
+    layer.refresh()
+    out, s = layer.forward(x.clone().requires_grad_(True))
+    grads = layer.backward(s, dout.clone().requires_grad_(True))
+    want_out, want_s = plain.forward(x)
+    for got, want in zip((out, s.scores, *s.x, *s.v, s.rows, *grads), (want_out, want_s.scores, *want_s.x, *want_s.v, want_s.rows,
+                                                                     *plain.backward(want_s, dout))):
+        assert (got is None and want is None) or (not got.requires_grad and torch.equal(got.float(), want.float()))
+
+
 def test_no_tokens(device):
     layer = layer_of(4, 128, 128, 64, 2, device)
     out, s = layer.forward(torch.empty(0, 128, device=device))
