@@ -7,7 +7,8 @@
 // Element by element but for the scales: bound by memory.  Eight neighbours a lane,
 // 16 lanes a block of 128 that shares a scale; a workgroup takes 16 rows and up to
 // kSteps blocks along them, so that scales that are neighbours in memory are read and
-// written together.
+// written together.  32768 x 1024, gated, 8 bits in and out 28 us (3.7 TB/s);
+// ReLU's gradient 24, 16-bit gated gradients 62 (5.4 TB/s).
 
 #include <type_traits>
 
@@ -223,7 +224,8 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_blocks(ActArgs a)
 }
 
 // A lane of a block of dv, which may lie across the border, takes dg where its
-// columns are g's, du where they are u's; dh and g are read for each.
+// columns are g's, du where they are u's; dh and g are read for each. 32768 x 1016
+// 75 us, 1023 columns 83 (1024, without a border inside a block, 41).
 template <typename D, typename T, bool kRagged>
 __global__ __launch_bounds__(kThreads) void eb_activate_back_across(ActArgs a)
 {
