@@ -32,15 +32,17 @@ struct ActArgs {
     bool gate;
 };
 
-// 1 / (1 + exp(-g)): the exponential with the rounding of its argument put right.
-// Beyond 87 it is 1 or below 2^-125.
+// p = 1 / (1 + exp(-g)): the exponential with the rounding of its argument put right, by
+// a factor c.  From g = 87 on p is 1.  Below -88.7 the exponential is infinite and p, as
+// g p then, a zero of either sign (c means little there, but is neither 0 nor NaN; for
+// -infinity it is NaN, and so is p).  A p below 2^-126 may be 0.
 __device__ __forceinline__ float sigmoid(float g)
 {
     constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f; // together log2(e) to 2^-50
-    g = __builtin_amdgcn_fmed3f(g, -87.f, 87.f);
+    g = fminf(g, 87.f); // NaN: 87, whose p leaves the NaN of g p
     const float h = g * -kLog2e, l = fmaf(g, -kRest, fmaf(g, -kLog2e, -h));
-    const float e = __builtin_amdgcn_exp2f(h);
-    return __builtin_amdgcn_rcpf(1.f + fmaf(e, l * 0.693147182f, e));
+    const float e = __builtin_amdgcn_exp2f(h), c = fmaf(l, 0.693147182f, 1.f);
+    return __builtin_amdgcn_rcpf(fmaf(e, c, 1.f));
 }
 
 // Columns c .. c + 7 of v that lie in [lo, hi), to be settled where they are used.
