@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 from typing import NamedTuple
 
 import torch
@@ -577,18 +578,32 @@ class ExpertTraining:
         return ExpertGradients(dx, w_up, w_down, router, norm_weight, norm_bias), dict(dz=dz, dh=dh, dv=dv, h=h, dslots=dslots, dweights=g.dweights, dscores=dscores)
 
     def _dscores(self, saved, dweights):
-        """The router's outputs' gradient from that of the chosen pairs' weights (0 for other GPUs' pairs)."""
-        ids = saved.route.ids
+        """The router's outputs' gradient from that of the chosen pairs' weights (0 for other GPUs' pairs).
+
+        With EB_RENORMALIZE a token's weights w are its own chosen experts' alone, whose scores may lie
+        far below others' that a bias or a group keeps out: no sum over those is divided by.
+        softmax: w (d - sum of w d); sigmoid: that times 1 - p.  Scores are what the route takes them
+        as: an infinity the largest float, NaN minus infinity."""
+        scores, ids = saved.scores.nan_to_num(-math.inf, torch.finfo(_F32).max, -math.inf), saved.route.ids
         at, there = ids.clamp(min=0).long(), ids >= 0
         sigmoid = self.mode & 0xFF == ex.EB_SIGMOID
-        p = torch.sigmoid(saved.scores) if sigmoid else torch.softmax(saved.scores, 1)
-        chosen = torch.where(there, p.gather(1, at), 0.0)
-        d = dweights * self.scale
+        d = torch.where(there, dweights * self.scale, 0.0)
+        x = scores.gather(1, at)
         if self.mode & ex.EB_RENORMALIZE:
-            total = chosen.sum(1, keepdim=True)
-            total = torch.where(total > 0, total, 1.0)
-            d = (d - (d * chosen).sum(1, keepdim=True) / total) / total
-        dp = torch.zeros_like(p).scatter_add_(1, at, torch.where(there, d, 0.0))
-        if sigmoid:
-            return dp * p * (1 - p)
-        return p * (dp - (dp * p).sum(1, keepdim=True))
+            most = torch.where(there, x, torch.finfo(_F32).min).amax(1, keepdim=True)
+            if sigmoid:  # e^-m / (1 + e^-x): no underflow where all x are low
+                m = most.clamp(max=0)
+                w = torch.where(there, 1 / (torch.exp(m) + torch.exp(m - x)), 0.0)
+            else:
+                w = torch.where(there, torch.exp(x - most), 0.0)
+            w = w / torch.where(there.any(1, keepdim=True), w.sum(1, keepdim=True), 1.0)
+            d = w * (d - (w * d).sum(1, keepdim=True))
+            if sigmoid:
+                d = d * torch.sigmoid(-x)
+        elif sigmoid:
+            d = d * torch.sigmoid(x) * torch.sigmoid(-x)
+        ds = torch.zeros_like(scores).scatter_add_(1, at, d)
+        if sigmoid or self.mode & ex.EB_RENORMALIZE:
+            return ds
+        p = torch.softmax(scores, 1).nan_to_num(0.0)  # without an expert to choose none has a share
+        return p * (ds - (ds * p).sum(1, keepdim=True))
