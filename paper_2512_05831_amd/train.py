@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 import math
 from typing import NamedTuple
 
@@ -144,14 +145,20 @@ def _code(dtype) -> int:
 
 def _placed(f):
     """The call under its ``stream``, or on its first tensor's GPU: at once where that is current."""
+    first, last = f.__code__.co_varnames[0], f.__code__.co_argcount - 1  # the last one is the stream
+
     @functools.wraps(f)
-    def call(x, *args, stream=None, **kw):
-        if stream is None and -1 < x.get_device() == ex._gpu():
-            return f(x, *args, **kw)
-        if not x.is_cuda:
+    def call(*args, stream=None, **kw):
+        if len(args) == last + 1 and stream is None:
+            args, stream = args[:last], args[last]
+        x = args[0] if args else kw.get(first)
+        if stream is None and x is not None and -1 < x.get_device() == ex._gpu():
+            return f(*args, **kw)
+        if x is None or not x.is_cuda:
+            inspect.signature(f).bind(*args, **kw)
             raise ValueError("expected device tensors")
         with _place(torch, x, stream):
-            return f(x, *args, stream=stream, **kw)
+            return f(*args, stream=stream, **kw)
     return call
 
 
