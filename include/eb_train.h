@@ -242,11 +242,10 @@ int eb_weight_gradient_workspace(int64_t M, int32_t E, int64_t N, int64_t K, siz
  *   dw[e][n, k] = sum over e's slots m of dy[m, n] * x[tokens[m], k]
  *
  * Sums are fp32, in an order that depends on the sizes and offsets alone, rounded
- * once (with accumulate after dw is added).  fp32 and fp16 outputs: products within
- * 2^-20 of exact; where neither operand is bfloat16 and one has scales, also within
- * 2^-34 of the largest that the scales of the expert's slots allow.  bfloat16 outputs:
- * of the operands the one that takes the scales is rounded to 16 bits first, and so is
- * an fp16 one beside bfloat16: products within 2^-8.  An infinite operand gives
+ * once (with accumulate after dw is added).  Products are within 2^-20 of exact; where
+ * neither operand is bfloat16 and one has scales, also within 2^-34 of the largest that
+ * the scales of the expert's slots allow; for a bfloat16 output of a bfloat16 operand and
+ * one with scales within 2^-16.  An infinite operand gives
  * infinities or NaNs.  Errors: EB_ERR_INVALID for an argument outside the
  * above, EB_ERR_UNSUPPORTED for sizes past the above or past one launch (2^24
  * tiles of 128 x 128), EB_ERR_HIP when a launch fails.

@@ -13,12 +13,14 @@
 //   A slot's scales (of dy and of x) go into the own operand as their product S, one
 // number for a slot and 128 own columns; so that the shared one, e4m3 or 16 bits,
 // enters exactly, and where dy and x both have scales a workgroup's shared columns are
-// one block of them.  Scaled values have up to 28 bits and take several 16-bit parts
-// where sums have to be exact, each multiplied with the shared operand:
+// one block of them.  Scaled values have up to 28 bits and take several 16-bit parts,
+// each multiplied with the shared operand:
 //   beside e4m3 or fp16, two parts in fp16 (22 bits).  Their range is short, so S is
 //     divided by a power of two, kept above the largest S so far; where that grows the
 //     sums are brought to the new one (exactly), and the outputs multiplied by the last;
-//   beside bfloat16, three parts in that (24 bits).
+//   beside bfloat16, three parts in that (24 bits), for bfloat16 outputs two (16 bits, a
+//     512th of those outputs' own rounding; 8192 slots by 32 experts of 512 x 1024 take 40 us,
+//     in one part, whose error is that rounding's size again, 33).
 //   In LDS the 16-byte pieces of a row are permuted with its number (what a lane copies
 // goes where its number says, so it is the global addresses that are permuted): the
 // rows that an instruction reads at a time then lie in different banks.
@@ -72,7 +74,7 @@ struct Shape {
     static constexpr bool kBoth = kScaled && std::is_same_v<Shared, Fp8>;
     static constexpr bool kShift = kScaled && kHalf;
     static constexpr bool kAsItIs = std::is_same_v<Own, Unit>;
-    static constexpr int kParts = !kExact || kAsItIs ? 1 : kHalf || !kScaled ? 2 : 3;
+    static constexpr int kParts = kAsItIs ? 1 : kHalf || !kScaled || !kExact ? 2 : 3; // (fp16 values are exact in two of bfloat16)
     using OwnPiece = std::conditional_t<kScaled, Bytes, Piece>;
     static constexpr int kSlots = kScaled ? 64 : 32; // of a step
 };
@@ -201,13 +203,12 @@ __device__ __forceinline__ void each_part(const typename S::OwnPiece &piece, con
                                   : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], 1.f, false);
             const f16x2 v = q * scale.first[i];
             first.w[i] = __builtin_bit_cast(uint32_t, v);
-            if constexpr (S::kParts == 2) { // what v's rounding left of q * first (exactly), and q * rest, rounded once
-                const f16x2 left = __builtin_elementwise_fma(q, scale.first[i], -v);
-                rest.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, scale.rest[i], left));
-            }
+            // What v's rounding left of q * first (exactly), and q * rest, rounded once.
+            const f16x2 left = __builtin_elementwise_fma(q, scale.first[i], -v);
+            rest.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, scale.rest[i], left));
         }
         take(first);
-        if constexpr (S::kParts == 2) take(rest);
+        take(rest);
     } else {
         float f[kEach];
         if constexpr (S::kScaled) {
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
                 s = ldexpf(s, -next_shift);
                 const _Float16 first = (_Float16)s;
                 first_of[of][half][slot] = first;
-                if constexpr (kExact) rest_of[of][half][slot] = (_Float16)(s - (float)first);
+                rest_of[of][half][slot] = (_Float16)(s - (float)first);
             } else {
                 first_of[of][half][slot] = s;
             }
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
             const int c = s + lane / 16 * 8;
             if constexpr (S::kShift) {
                 __builtin_memcpy(scale.first, &first_of[of][own_half][c], 16);
-                if constexpr (kExact) __builtin_memcpy(scale.rest, &rest_of[of][own_half][c], 16);
+                __builtin_memcpy(scale.rest, &rest_of[of][own_half][c], 16);
             } else if constexpr (S::kScaled) {
                 __builtin_memcpy(scale.s, &first_of[of][own_half][c], 32);
             }
@@ -537,14 +538,15 @@ template <typename D, typename X, int kSharedTile>
 Choice choice_of(bool exact, bool direct)
 {
     using S = Shape<D, X, true>;
-    if constexpr (S::kAsItIs && !S::kScaled) exact = true; // the same
+    constexpr bool kTwoForms = S::kParts == 3; // else both are the same
+    if constexpr (!kTwoForms) exact = true;
     if constexpr (sizeof(D) == 1 && sizeof(X) == 1) direct = true;
     if (direct && exact) return {(void *)eb_gradient_tile<D, X, true, true, kSharedTile>, S::kOwnX};
-    if constexpr (!S::kAsItIs || S::kScaled)
+    if constexpr (kTwoForms)
         if (direct) return {(void *)eb_gradient_tile<D, X, false, true, kSharedTile>, S::kOwnX};
     if constexpr (kSharedTile == 64 && (sizeof(D) == 2 || sizeof(X) == 2)) {
         if (exact) return {(void *)eb_gradient_tile<D, X, true, false, kSharedTile>, S::kOwnX};
-        if constexpr (!S::kAsItIs || S::kScaled) return {(void *)eb_gradient_tile<D, X, false, false, kSharedTile>, S::kOwnX};
+        if constexpr (kTwoForms) return {(void *)eb_gradient_tile<D, X, false, false, kSharedTile>, S::kOwnX};
     }
     return {};
 }
