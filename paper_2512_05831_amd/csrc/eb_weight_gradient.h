@@ -15,9 +15,12 @@
 // enters exactly, and where dy and x both have scales a workgroup's shared columns are
 // one block of them.  Scaled values have up to 28 bits and take several 16-bit parts,
 // each multiplied with the shared operand:
-//   beside e4m3 or fp16, two parts in fp16 (22 bits).  Their range is short, so S is
-//     divided by a power of two, kept above the largest S so far; where that grows the
-//     sums are brought to the new one (exactly), and the outputs multiplied by the last;
+//   beside e4m3 or fp16, two parts in fp16 (22 bits).  Their range is short, so S (in two
+//     parts too) is divided by a power of two that keeps the largest S so far in [2^11,
+//     2^14), and the e4m3 value by 2^8 (exactly: it is 2^-17 and more).  What fp16, whose
+//     numbers lie 2^-24 apart and more, cannot hold of S and of the products is then below
+//     2^-34 of the largest product.  Where the power grows the sums are brought to the new one
+//     (exactly), and the outputs multiplied by the last;
 //   beside bfloat16, three parts in that (24 bits), for bfloat16 outputs two (16 bits, a
 //     512th of those outputs' own rounding; 8192 slots by 32 experts of 512 x 1024 take 40 us,
 //     in one part, whose error is that rounding's size again, 33).
@@ -177,6 +180,10 @@ __device__ __forceinline__ f32x4 multiply(const Piece &a, const Piece &b, f32x4 
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// An e4m3 value beside fp16 scales counts these, and its scale as many times more.
+constexpr int kOwnShift = 8;
+constexpr float kOwnUnit = 1.f / (1 << kOwnShift);
+
 // Scales of the eight slots of a lane, as the own operand's parts are made with them.
 template <bool kHalf>
 struct EightScales;
@@ -199,11 +206,11 @@ __device__ __forceinline__ void each_part(const typename S::OwnPiece &piece, con
         Piece first, rest;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const f16x2 q = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], 1.f, true)
-                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], 1.f, false);
+            const f16x2 q = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], kOwnUnit, true)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(piece.w[i / 2], kOwnUnit, false);
             const f16x2 v = q * scale.first[i];
             first.w[i] = __builtin_bit_cast(uint32_t, v);
-            // What v's rounding left of q * first (exactly), and q * rest, rounded once.
+            // What v's rounding left of q * first (exactly, or to 2^-25), and q * rest, rounded once.
             const f16x2 left = __builtin_elementwise_fma(q, scale.first[i], -v);
             rest.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, scale.rest[i], left));
         }
@@ -356,8 +363,9 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
         if constexpr (S::kScaled) {
             float s = row < 0 ? 0.f : own_scale * shared_scale;
             if constexpr (S::kShift) {
-                // 448 S / 2^shift stays below 2^15; a new shift leaves room for S to grow 4 times.
-                constexpr int kMostLeft = 5, kRoom = 2;
+                // S / 2^shift stays below 2^14, and 448 kOwnUnit times that below 2^15; a new
+                // shift leaves room for S to grow 4 times.
+                constexpr int kMostLeft = 5 + kOwnShift, kRoom = 2;
                 static_assert(kSlots == kWave, "a wave has a step's scales of a block");
                 const int bits = magnitude(s), most = max_lanes<kWave>(bits < 0x7F800000 ? bits >> 23 : 0) - 127;
                 if (most - next_shift > kMostLeft) next_shift = most - kMostLeft + kRoom;
@@ -524,7 +532,7 @@ __global__ __launch_bounds__(kThreads, kSharedTile == 64 && kDirect ? 3 : 2) voi
             if (n >= a.N || k >= a.K) continue;
             float v[kQuad];
 #pragma unroll
-            for (int r = 0; r < kQuad; ++r) v[r] = S::kShift ? ldexpf(sum[i][j][r], shift) : sum[i][j][r];
+            for (int r = 0; r < kQuad; ++r) v[r] = S::kShift ? ldexpf(sum[i][j][r], shift + kOwnShift) : sum[i][j][r];
             write_quad(a, partial, e, n, k, v);
         }
 }
