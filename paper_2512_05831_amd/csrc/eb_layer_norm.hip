@@ -60,9 +60,11 @@ __device__ __forceinline__ void write8(const NormArgs &a, const float *held, int
 #pragma unroll
     for (int i = 0; i < kEach; ++i) n[i] = d[i] * rstd;
     if (a.kept.p) {
-        // n / scale is d times one factor: as exact as d.
+        // n / scale is d times one factor, as exact as d: where that can be made of d's largest
+        // (not below the floor of what a factor is made of, which rstd may lift n over).
         const int most_d = most_of_block(most8(d)), most = magnitude(__int_as_float(most_d) * rstd);
-        if (__int_as_float(most) <= kMostFp8 * kLeastScale) store_fp8(a.kept, row, c, cols, n, kToLeast, most);
+        const bool least = __int_as_float(most) <= kMostFp8 * kLeastScale, small = __int_as_float(most_d) <= kMostFp8 * kLeastScale;
+        if (least || small) store_fp8(a.kept, row, c, cols, n, least ? kToLeast : to_fp8(most), most);
         else store_fp8(a.kept, row, c, cols, d, to_fp8(most_d), most);
     }
 #pragma unroll
