@@ -202,7 +202,9 @@ __global__ __launch_bounds__(kThreads) void eb_activate_back_blocks(ActArgs a)
         const int most_d = most_of_block(most8(d));
         int scaled = magnitude(__int_as_float(most_d) * su[s]);
         Factor of_d = to_fp8(most_d);
-        if (most_d >= 0x7F800000) { // with its scale it may be finite
+        // Beyond fp32's range before u's scale it may be finite with it, and below the floor of
+        // what a factor is made of it may lie above that: made again of the scaled u.
+        if (most_d >= 0x7F800000 || (most_d != 0 && __int_as_float(most_d) <= kMostFp8 * kLeastScale)) {
             float dh[kEach];
             widen8(of_h[s], dh);
             widen8(of_g[s], g);
