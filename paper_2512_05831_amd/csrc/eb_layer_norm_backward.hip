@@ -257,23 +257,26 @@ constexpr int kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void eb_layer_norm_join(JoinArgs a)
 {
     __shared__ float shared[kJoinThreads];
-    const int64_t c = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;
-    const int wave = threadIdx.x / kWave;
     constexpr int kWaves = kJoinThreads / kWave;
-    float sum = 0.f;
-    if (c < 2 * a.cols) {
+    const int wave = threadIdx.x / kWave;
+    for (int64_t first = (int64_t)blockIdx.x * kWave; first < 2 * a.cols; first += (int64_t)gridDim.x * kWave) {
+        const int64_t c = first + threadIdx.x % kWave;
+        float sum = 0.f;
+        if (c < 2 * a.cols) {
 #pragma unroll 8
-        for (int p = wave; p < a.parts; p += kWaves) sum += a.partial[(int64_t)p * 2 * a.cols + c];
-    }
-    shared[threadIdx.x] = sum;
-    __syncthreads();
-    if (wave > 0 || c >= 2 * a.cols) return;
+            for (int p = wave; p < a.parts; p += kWaves) sum += a.partial[(int64_t)p * 2 * a.cols + c];
+        }
+        __syncthreads(); // the last columns' have been read
+        shared[threadIdx.x] = sum;
+        __syncthreads();
+        if (wave > 0 || c >= 2 * a.cols) continue;
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) sum += shared[i * kWave + threadIdx.x];
-    if (c < a.cols) {
-        if (a.dweight) a.dweight[c] = sum;
-    } else if (a.dbias) {
-        a.dbias[c - a.cols] = sum;
+        for (int i = 1; i < kWaves; ++i) sum += shared[i * kWave + threadIdx.x];
+        if (c < a.cols) {
+            if (a.dweight) a.dweight[c] = sum;
+        } else if (a.dbias) {
+            a.dbias[c - a.cols] = sum;
+        }
     }
 }
 
@@ -376,7 +379,9 @@ int back_impl(const char *who, int64_t rows, int64_t cols, const void *dy, int32
         return EB_OK;
     }
     JoinArgs j{(const float *)workspace, dweight, dbias, cols, (int32_t)groups};
-    return launch(who, (void *)eb_layer_norm_join, (2 * cols + kWave - 1) / kWave, kJoinThreads, &j, stream);
+    // In turns where they are more than a launch's threads hold: its work is under way by now.
+    constexpr int64_t kMostJoins = 1 << 16;
+    return launch(who, (void *)eb_layer_norm_join, std::min((2 * cols + kWave - 1) / kWave, kMostJoins), kJoinThreads, &j, stream);
 }
 
 int workspace_impl(const char *who, int64_t rows, int64_t cols, size_t *bytes)
