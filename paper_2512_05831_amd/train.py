@@ -469,11 +469,12 @@ class Saved(NamedTuple):
     but the experts' rows and what goes by token."""
     route: object      # experts.Route
     scores: object     # fp32 [B, experts]
-    x: object          # (values, scales): what the experts and the router read
+    x: object          # (values, scales): what the experts read, and the router before it was rounded to 8 bits
     kept: object       # (values, scales) and rstd of the layer norm, or None
     rstd: object
     v: object          # (values, scales) before the activation
     rows: object       # [slots, D] in row_dtype, before they are joined
+    read: object = None  # [B, K]: what the router read, under ``exact_router``
 
 
 class ExpertGradients(NamedTuple):
@@ -498,11 +499,14 @@ class ExpertTraining:
     and ``row_dtype`` are ``ExpertLayer``'s; of several GPUs' experts a GPU's output, and its
     gradients of x and the router, are shares to be added over the GPUs (and the norm's
     gradients with that of x: where all GPUs hold the same tokens pass the summed dx on).
+    The router reads x (behind the norm) unrounded.  Its own gradient is made of x in 8 bits, as the
+    experts' are, and of its outputs' gradients in bf16; ``exact_router``: of both as they are, in fp32,
+    for which x waits too (a norm's output, else the caller's tensor, to be left as it is until ``backward``).
     Torch records nothing of the calls, also where weights or inputs require gradients."""
 
     def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = ex.EB_SOFTMAX | ex.EB_RENORMALIZE,
                  norm_weight=None, norm_bias=None, eps: float = 1e-5, bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0,
-                 shard_lo: int = 0, row_dtype=None):
+                 shard_lo: int = 0, row_dtype=None, exact_router: bool = False):
         if w_up.dim() != 3 or w_down.dim() != 3 or router.dim() != 2:
             raise ValueError("w_up and w_down must be 3-D, router 2-D")
         E, N, K = w_up.shape
@@ -516,7 +520,7 @@ class ExpertTraining:
         self.w_up, self.w_down, self.router, self.norm_weight, self.norm_bias = w_up, w_down, router, norm_weight, norm_bias
         self.E, self.K, self.D, self.top, self.act, self.mode, self.eps = E, K, int(w_down.shape[1]), top, act, mode, eps
         self.bias, self.groups, self.top_groups, self.scale, self.shard_lo = bias, groups, top_groups, scale, shard_lo
-        self.row_dtype = row_dtype or _BF16
+        self.row_dtype, self.exact_router = row_dtype or _BF16, exact_router
         with torch.no_grad(), torch.cuda.device(w_up.device):
             self._up, self._down, self._up_t, self._down_t = (ex.quantize_fp8(w.contiguous(), block_rows=BLOCK) for w in self._forms())
 
@@ -554,7 +558,7 @@ class ExpertTraining:
             h = activation(*v, act=self.act, out_dtype=_FP8)
             rows = ex.product(*h, *self._down, r.offsets, out_dtype=self.row_dtype)
             out = combine(rows, r.slots, r.weights, out_dtype=out_dtype or _F32)
-        return out, Saved(r, scores, q, kept, rstd, v, rows)
+        return out, Saved(r, scores, q, kept, rstd, v, rows, x if self.exact_router else None)
 
     def backward(self, saved: Saved, dout) -> ExpertGradients:
         """``dout``: [B, D] of fp32, fp16 or bf16, the gradient of forward's output.  dx is of
@@ -577,7 +581,10 @@ class ExpertTraining:
             # (each comes of 4-bit values), and what the router's gradient and the norm's take.
             dscores = self._dscores(saved, g.dweights)
             dx = combine(dslots, r.slots, out_dtype=_F32) + dscores @ self.router
-            router = weight_gradient(dscores.to(_BF16), saved.x[0], x_scales=saved.x[1])
+            if saved.read is not None:
+                router = dscores.t() @ saved.read.float()
+            else:
+                router = weight_gradient(dscores.to(_BF16), saved.x[0], x_scales=saved.x[1])
             norm_weight = norm_bias = None
             if self.norm_weight is not None:
                 dx, norm_weight, norm_bias = layer_norm_backward(dx.to(_BF16), saved.kept[0], saved.rstd, x_scales=saved.kept[1],
