@@ -560,14 +560,18 @@ class ExpertTraining:
             out = combine(rows, r.slots, r.weights, out_dtype=out_dtype or _F32)
         return out, Saved(r, scores, q, kept, rstd, v, rows, x if self.exact_router else None)
 
-    def backward(self, saved: Saved, dout) -> ExpertGradients:
-        """``dout``: [B, D] of fp32, fp16 or bf16, the gradient of forward's output.  dx is of
-        bf16 behind a norm, else fp32."""
-        return self._backward(saved, dout)[0]
+    def backward(self, saved: Saved, dout, dx_dtype=None) -> ExpertGradients:
+        """``dout``: [B, D] of fp32, fp16 or bf16, the gradient of forward's output; ``dx_dtype``: the
+        type of x's gradient, and of the rows from which the norm's are made (behind a norm bf16,
+        else fp32)."""
+        return self._backward(saved, dout, dx_dtype)[0]
 
     @torch.no_grad()
-    def _backward(self, saved, dout):
+    def _backward(self, saved, dout, dx_dtype=None):
         r = saved.route
+        dx_dtype = dx_dtype or (_F32 if self.norm_weight is None else _BF16)
+        if _code(dx_dtype) == EB_FP8:
+            raise ValueError("dx_dtype must be fp32, fp16 or bf16")
         with torch.cuda.device(dout.device):
             g = combine_backward(dout, saved.rows, r.slots, r.weights, out_dtype=_FP8)
             dz = (g.dy, g.dy_scales)
@@ -577,17 +581,18 @@ class ExpertTraining:
             w_down = weight_gradient(dz[0], h[0], r.offsets, dy_scales=dz[1], x_scales=h[1])
             w_up = weight_gradient(dv[0], saved.x[0], r.offsets, r.tokens, dy_scales=dv[1], x_scales=saved.x[1])
             dslots = ex.product(*dv, *self._up_t, r.offsets, out_dtype=_BF16)
-            # In bf16, whose range is fp32's: the rows' gradients before and after they are joined
-            # (each comes of 4-bit values), and what the router's gradient and the norm's take.
+            # In bf16, whose range is fp32's: the rows' gradients before they are joined (each comes of
+            # 4-bit values) and, unless more is asked for, what the router's gradient and the norm's take.
             dscores = self._dscores(saved, g.dweights)
             dx = combine(dslots, r.slots, out_dtype=_F32) + dscores @ self.router
             if saved.read is not None:
                 router = dscores.t() @ saved.read.float()
             else:
                 router = weight_gradient(dscores.to(_BF16), saved.x[0], x_scales=saved.x[1])
+            dx = dx.to(dx_dtype)
             norm_weight = norm_bias = None
             if self.norm_weight is not None:
-                dx, norm_weight, norm_bias = layer_norm_backward(dx.to(_BF16), saved.kept[0], saved.rstd, x_scales=saved.kept[1],
+                dx, norm_weight, norm_bias = layer_norm_backward(dx, saved.kept[0], saved.rstd, x_scales=saved.kept[1],
                                                                  weight=self.norm_weight)
         return ExpertGradients(dx, w_up, w_down, router, norm_weight, norm_bias), dict(dz=dz, dh=dh, dv=dv, h=h, dslots=dslots, dweights=g.dweights, dscores=dscores)
 
