@@ -140,8 +140,8 @@ int eb_activation(int64_t rows, int64_t cols, int32_t act, const void *v, int32_
  *   EB_ACT_RELU: dv = dh where v > 0, else 0.  EB_ACT_SILU_GATE, with
  *   p = 1 / (1 + exp(-g)):  dg = dh * p * u * (1 + g * (1 - p)),  du = dh * p * g
  *
- * In fp32, rounded once; p as in eb_activation.  What of dh * p lies below 2^-126 may be
- * lost.  Errors as eb_activation.
+ * In fp32, rounded once; p as in eb_activation.  What p or dh * p holds below 2^-126 may
+ * be lost.  Errors as eb_activation.
  */
 int eb_activation_backward(int64_t rows, int64_t cols, int32_t act, const void *dh, int32_t dh_type, int64_t lddh,
                            const void *v, int32_t v_type, int64_t ldv, const float *v_scales, int64_t ldvs,

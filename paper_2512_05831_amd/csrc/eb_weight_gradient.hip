@@ -53,7 +53,8 @@ int check_sizes(const char *who, int64_t M, int32_t E, int64_t N, int64_t K)
 int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
 // How a call is cut up, from its sizes alone (so that its workspace is known without
-// types; tiles are counted with dy as the own operand, with x they are nearly as many).
+// types; tiles are counted with dy as the own operand: where x is that one and N small they
+// are fewer, of 32 x 1024 4 and not 16, and fill less of the GPU).
 // Measured in turn, us a call:
 //   Shared columns 64 or 128.  Narrow tiles let three workgroups share a compute unit,
 //   wide ones read less: one expert, 2048 slots by 1000 x 1512 in bf16 (1536 steps of 64
