@@ -502,7 +502,8 @@ class ExpertTraining:
     The router reads x (behind the norm) unrounded.  Its own gradient is made of x in 8 bits, as the
     experts' are, and of its outputs' gradients in bf16; ``exact_router``: of both as they are, in fp32,
     for which x waits too (a norm's output, else the caller's tensor, to be left as it is until ``backward``).
-    Torch records nothing of the calls, also where weights or inputs require gradients."""
+    Torch records nothing of the calls, also where weights or inputs require gradients, and casts none
+    of their products under ``torch.autocast``."""
 
     def __init__(self, w_up, w_down, router, top: int, act: int = EB_ACT_SILU_GATE, mode: int = ex.EB_SOFTMAX | ex.EB_RENORMALIZE,
                  norm_weight=None, norm_bias=None, eps: float = 1e-5, bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0,
@@ -546,7 +547,7 @@ class ExpertTraining:
         (float32), Saved)."""
         if x.dim() != 2 or x.shape[1] != self.K or not x.is_cuda:
             raise ValueError("x must be [B, K] on the GPU")
-        with torch.cuda.device(x.device):
+        with torch.cuda.device(x.device), torch.autocast("cuda", enabled=False):
             kept = rstd = None
             if self.norm_weight is not None:
                 n = layer_norm(x, self.norm_weight, self.norm_bias, self.eps, out_dtype=x.dtype, checkpoint=True)
@@ -572,7 +573,7 @@ class ExpertTraining:
         dx_dtype = dx_dtype or (_F32 if self.norm_weight is None else _BF16)
         if _code(dx_dtype) == EB_FP8:
             raise ValueError("dx_dtype must be fp32, fp16 or bf16")
-        with torch.cuda.device(dout.device):
+        with torch.cuda.device(dout.device), torch.autocast("cuda", enabled=False):
             g = combine_backward(dout, saved.rows, r.slots, r.weights, out_dtype=_FP8)
             dz = (g.dy, g.dy_scales)
             dh = ex.product(*dz, *self._down_t, r.offsets, out_dtype=_BF16)
