@@ -58,8 +58,8 @@ int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 // Measured in turn, us a call:
 //   Shared columns 64 or 128.  Narrow tiles let three workgroups share a compute unit,
 //   wide ones read less: one expert, 2048 slots by 1000 x 1512 in bf16 (1536 steps of 64
-//   slots in all) 28.8 and 29.5; 32 experts of 512 x 1024, 256 slots each (2048) 34.6 and
-//   37.3; 16384 by 512 x 512 in bf16 (2048) 32.8 and 39.4; 8192 by 1024 x 1024 in 8 bits (4096)
+//   slots in all) 28.8 and 29.5; 32 experts of 512 x 1024, 256 slots each, to bf16 (2048) 38.0
+//   and 41.7; 16384 by 512 x 512 in bf16 (2048) 32.8 and 39.4; 8192 by 1024 x 1024 in 8 bits (4096)
 //   55.2 and 54.8; 2048 by 2560 x 2048 (5120) 68.8 and 65.2; 16384 by 2048 x 2048 (32768) 300 and 250.
 //   Parts of an expert's slots.  They fill the GPU, and cost 8 bytes of traffic an
 //   output each: 2048 slots by 1000 x 1512 in 2, 4, 8 parts 31.6, 28.8, 32.2; 8192 by 1024 x 1024
